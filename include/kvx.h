@@ -447,6 +447,185 @@ int kvx_page_hashes(const void *payload, int64_t payload_positions, int32_t rec_
                     int32_t page_tokens, const kvx_hash_req *reqs, int32_t n_reqs,
                     uint64_t *out, int64_t out_len, uint32_t *dev_err, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * A decode step over a paged cache: the calls that compute with the cached
+ * values, where those above move them.  Take one layer of a pool.
+ *   kvx_append         puts new tokens' keys and values into their slots,
+ *                      rotated by their positions, and rotates their queries;
+ *   kvx_attend         attends with one query per request over its pages and
+ *                      can add every position's weight to an accumulator;
+ *   kvx_select_kept    chooses, by accumulated weight, the positions that each
+ *                      layer and head of a request keeps;
+ *   kvx_transfer_kept  moves the kept rows into pages of their own.
+ * Values: a pool of elem_bytes 2 holds the type of the rows passed with it
+ * (bfloat16 or IEEE half), a pool of elem_bytes 1 holds OCP e4m3 values that
+ * stand for themselves times scales[c * num_heads + h] (scales: device memory,
+ * num_kv * num_heads floats; NULL: all 1, and required to be NULL for a pool
+ * of elem_bytes 2).  Other widths are refused with KVX_ERR_SHAPE.
+ * Ownership, synchrony and errors are as above: nothing is allocated, all
+ * inputs must be device memory or mapped pinned host memory and all outputs,
+ * accumulators and workspaces device memory.  A page of the pool that cannot
+ * be resolved raises KVX_DERR_SRC_PAGE (read) or KVX_DERR_DST_PAGE (written),
+ * a table index out of range KVX_DERR_PT_RANGE, a malformed record
+ * KVX_DERR_BAD_REQ; only the elements involved are left out.
+ * max_tokens (each call), 0 .. KVX_MAX_TOKENS: no record holds more positions
+ * than this; read on the host to shape the launch.  A record that holds more
+ * is malformed.
+ * Sums, maxima and angles are held in 32 bits or more.
+ * ------------------------------------------------------------------------- */
+
+/* Most positions of a record of these calls. */
+#define KVX_MAX_TOKENS (1 << 22)
+
+/* Value types of rows. */
+#define KVX_BF16 0
+#define KVX_F16 1
+
+/* Rows [num_rows][num_heads][head_dim] of 16-bit values: element (r, h, d) is
+ * at base + r * row_stride + h * head_stride + d (elements).  base 16-byte
+ * aligned, strides >= 0 and multiples of 8, head_dim a multiple of 8
+ * (KVX_ERR_ALIGN).  Rows of a wider projection have its width as stride. */
+typedef struct kvx_rows {
+    void *base;
+    int64_t num_rows;
+    int64_t row_stride, head_stride;
+    int32_t num_heads, head_dim;
+    int32_t dtype;               /* KVX_BF16 or KVX_F16 */
+    int32_t reserved;            /* 0 */
+} kvx_rows;
+
+/* Rotation of rot_dim dimensions of each head from rot_off on.  With
+ * angle(p, j) = p * freq[j] for position p and j < rot_dim / 2, and A =
+ * amplitude, the pair (a, b) becomes
+ *   (A * (a cos - b sin), A * (b cos + a sin)),
+ * (a, b) = elements (rot_off + j, rot_off + j + rot_dim / 2), or with
+ * `interleaved` (rot_off + 2j, rot_off + 2j + 1).  The other dimensions stay
+ * as they are.  Long contexts: scale freq, and set the amplitude. */
+typedef struct kvx_rope {
+    const float *freq;           /* device, rot_dim / 2 radians per position */
+    int32_t rot_dim;             /* even, rot_off + rot_dim <= head_dim; 0: no rotation */
+    int32_t rot_off;             /* >= 0 */
+    int32_t interleaved;         /* 0 or 1 */
+    float amplitude;             /* factor on the rotated values */
+} kvx_rope;
+
+/* New tokens of a request (32 bytes): rows row_off .. row_off + n_tokens - 1
+ * go to slots start .. of its pages and are rotated for positions position ..
+ * (the two differ once positions have been evicted).  Malformed: a negative
+ * field, start or position + n_tokens above 2^31 - 1, rows past num_rows,
+ * n_tokens > max_tokens, reserved not 0.  Records must not share rows or
+ * slots. */
+typedef struct kvx_append_req {
+    int64_t pt_off;
+    int64_t row_off;
+    int32_t start;
+    int32_t position;
+    int32_t n_tokens;
+    int32_t reserved;            /* 0 */
+} kvx_append_req;
+
+/* For every record r, i < n_tokens, row x = row_off + i:
+ *   pool(layer, 0, start + i, h, :) := store(rotate(k[x, h], position + i))
+ *   pool(layer, 1, start + i, h, :) := store(v[x, h])        (num_kv 2)
+ *   q_out[x, h']                    := round(rotate(q[x, h'], position + i))
+ * store rounds to the pool's type; for e4m3 it divides by the scale first and
+ * saturates at +-448 (NaN stays NaN).  Values that are neither rotated nor
+ * e4m3 are copied bit for bit.
+ * q and q_out: both or neither NULL, equal shapes, any number of heads; q_out
+ * may be q itself (same base and strides), no other overlap is allowed.
+ * k: num_heads and head_dim of the pool; v the same, NULL when num_kv is 1.
+ * All rows have the same dtype and num_rows.  rope may be NULL. */
+int kvx_append(const kvx_pool *pool, int32_t layer, const float *scales,
+               const kvx_rows *q, const kvx_rows *q_out, const kvx_rows *k, const kvx_rows *v,
+               const kvx_rope *rope, const int32_t *pt, int64_t pt_len,
+               const kvx_append_req *reqs, int32_t n_reqs, int32_t max_tokens,
+               uint32_t *dev_err, void *stream);
+
+/* One query of a request (24 bytes): it attends over positions [start, end)
+ * of its pages.  Malformed (its outputs are then not written): start < 0,
+ * end < start, end - start > max_tokens, or, with accumulators, positions that
+ * reach outside them. */
+typedef struct kvx_attend_req {
+    int64_t pt_off;
+    int64_t acc_off;             /* accumulator of cache head 0's position 0 */
+    int32_t start, end;
+} kvx_attend_req;
+
+/* Attention of one query per record (row r of q belongs to record r).  With G
+ * = q heads / num_heads, cache head h = query head / G, K(t) = pool(layer, 0,
+ * t, h, :), V(t) = pool(layer, num_kv - 1, t, h, 0 .. v_dim - 1), where v_dim
+ * is out's head_dim (so that with num_kv 1 the values are the first part of
+ * the keys' rows):
+ *   s(t) = scale * q . K(t),  m = max s,  p(t) = exp(s(t) - m),  l = sum p
+ *   out[r, head] = sum p(t) V(t) / l,   lse[r * q heads + head] = m + log l,
+ *   acc[acc_off + h * acc_stride + t] += sum over the G heads of p(t) / l.
+ * Positions that cannot be resolved take no part.  A query without positions
+ * (or with every score -inf) gives zeros, lse -inf and adds nothing.
+ * p is rounded to the rows' type for its product with V; sums, maxima, l and
+ * the accumulated weights are not.
+ * q heads: a multiple of num_heads, at most 1024.  head_dim <= 576,
+ * v_dim <= 512, v_dim <= head_dim, and v_dim == head_dim when num_kv is 2.
+ * lse: n_reqs * q heads floats or NULL.
+ * acc: acc_len floats or NULL; records must not share accumulators.
+ * workspace: kvx_attend_workspace() bytes for the same arguments, or more,
+ * 16-byte aligned, zero before its first use; each call leaves it ready for
+ * the next one.  Calls that may run at the same time need one each. */
+int kvx_attend(const kvx_pool *pool, int32_t layer, const float *scales,
+               const kvx_rows *q, const kvx_rows *out, float *lse, float scale,
+               const int32_t *pt, int64_t pt_len,
+               const kvx_attend_req *reqs, int32_t n_reqs, int32_t max_tokens,
+               float *acc, int64_t acc_len, int64_t acc_stride,
+               void *workspace, int64_t workspace_bytes, uint32_t *dev_err, void *stream);
+
+/* Bytes kvx_attend needs as workspace for up to n_reqs records of up to
+ * max_tokens positions each (accumulate: whether acc is given); -1 on
+ * arguments that kvx_attend refuses. */
+int64_t kvx_attend_workspace(const kvx_pool *pool, int32_t n_reqs, int32_t q_heads, int32_t v_dim,
+                             int32_t max_tokens, int32_t accumulate);
+
+/* What a request keeps (40 bytes): of its positions [0, n_tokens) the first
+ * `sink`, the last `recent`, and of those between them the n_keep - sink -
+ * recent of the largest accumulated weight.  All are kept if n_tokens <=
+ * n_keep.  Malformed: a negative field, sink + recent > n_keep, n_tokens >
+ * max_tokens, or a range outside its array. */
+typedef struct kvx_select_req {
+    int64_t acc_off;             /* in acc: position 0 of row 0 */
+    int64_t kept_off;            /* in kept: entry 0 of row 0 */
+    int64_t out_off;             /* in acc_out: entry 0 of row 0 (not read without acc_out) */
+    int32_t n_tokens, n_keep, sink, recent;
+} kvx_select_req;
+
+/* For every record and row j < rows (a layer and head, say), with K =
+ * min(n_tokens, n_keep) and w(t) = acc[acc_off + j * acc_stride + t]:
+ *   kept[kept_off + j * kept_stride + i], i < K: the kept positions, ascending;
+ *   acc_out[out_off + j * acc_out_stride + i] := w(kept i)     (if not NULL).
+ * The choice is exact: equal weights go to the lower position (-0 equals 0),
+ * NaN counts as less than any number.  The arrays hold acc_len, kept_len and
+ * acc_out_len elements; acc_out must not overlap acc.  rows: 1 .. 2^20. */
+int kvx_select_kept(const float *acc, int64_t acc_len, int64_t acc_stride, int32_t rows,
+                    const kvx_select_req *reqs, int32_t n_reqs, int32_t max_tokens,
+                    int32_t *kept, int64_t kept_len, int64_t kept_stride,
+                    float *acc_out, int64_t acc_out_len, int64_t acc_out_stride,
+                    uint32_t *dev_err, void *stream);
+
+/* kvx_transfer_slice (slice NULL: everything, between equal shapes) of
+ * listed positions, a list for every layer and head: for every record,
+ * i < n_tokens, l, c, h and d of the slice,
+ *   dst(l, c, dst_start + i, h, d) := src(l, c, src_start + k, h, d),
+ *   k = kept[buf_off + (l * heads + h) * kept_stride + i],
+ * l and h counted within the slice, heads the slice's.  kept_stride >= 0.
+ * Every other rule is kvx_transfer_slice's (a record whose lists reach outside
+ * kept, with buf_off < 0 or n_tokens > max_tokens, is malformed).  A negative
+ * k, or src_start + k above 2^31 - 1, raises KVX_DERR_PT_RANGE.  Evicted rows
+ * go to pages that the call does not read: copies of pages that others share
+ * stay whole, and the old ones are free when the stream has passed. */
+int kvx_transfer_kept(const kvx_pool *src, const kvx_pool *dst, const kvx_slice *slice,
+                      const int32_t *src_pt, int64_t src_pt_len,
+                      const int32_t *dst_pt, int64_t dst_pt_len,
+                      const kvx_req *reqs, int32_t n_reqs, int32_t max_tokens,
+                      const int32_t *kept, int64_t kept_len, int64_t kept_stride,
+                      uint32_t *dev_err, void *stream);
+
 /* Bytes a pool described by *pool occupies (-1 if the descriptor is invalid). */
 int64_t kvx_pool_bytes(const kvx_pool *pool);
 

@@ -1,0 +1,116 @@
+// kvx_ops.h -- launch parameters of the kernels that compute with a paged
+// cache (append, attend, select, transfer of kept rows).  Not part of the
+// public interface (include/kvx.h).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "kvx.h"
+#include "kvx_internal.h"
+
+namespace kvx {
+
+// Most workgroups of one launch of these kernels: the work-items (up to 1024 a
+// workgroup) stay below 2^32.  More take several launches.
+constexpr int64_t kMaxBlocks = 1 << 21;
+
+// One layer of a pool: row (c, page, slot, h) is at base + c * s_c + page *
+// s_p + slot * s_t + h * s_h (bytes).
+struct Layer {
+    char *base;
+    int64_t s_p, s_c, s_t, s_h;
+    const int32_t *pt;
+    int64_t pt_len;
+    int32_t N, C, H, D;
+    FastDiv fd_T;
+};
+
+// Rows of 16-bit values (kvx_rows) with a device base.
+struct Rows {
+    char *base;                  // nullptr: not given
+    int64_t s_row, s_head;       // bytes
+    int32_t heads;
+};
+
+struct AppendParams {
+    Layer pool;
+    const float *scales;         // e4m3 pools: [c][h], or nullptr
+    Rows q, q_out, k, v;
+    int64_t num_rows;
+    const float *freq;
+    int32_t half, rot_off, interleaved;   // half: rotated pairs of a head, 0: none
+    float amplitude;
+    const kvx_append_req *reqs;
+    int32_t n_reqs, max_tokens;
+    uint32_t *err;
+    int32_t f16, e4m3;           // rows' and pool's types
+    // launch
+    int32_t tokens, blocks;      // tokens per workgroup, workgroups per record
+    int32_t vec;                 // 8 elements at a time, else a pair
+    int32_t items, items_v;      // of a q or k head, of a v head
+    FastDiv fd_items, fd_items_v, fd_token, fd_half;
+};
+
+struct AttendParams {
+    Layer pool;
+    const float *scales;
+    Rows q, out;
+    int32_t G, Dv;               // query heads per cache head; elements of a value
+    float scale_log2;            // softmax scale times log2(e)
+    float *lse;
+    const kvx_attend_req *reqs;
+    int32_t n_reqs, max_tokens;
+    float *acc;
+    int64_t acc_len, acc_stride;
+    uint32_t *err;
+    int32_t f16, e4m3;
+    // launch: chunk positions per workgroup, chunks per record and head block,
+    // waves along heads, head blocks (of waves_h * 16 query heads) per cache head
+    int32_t chunk, chunks, waves_h, head_blocks;
+    // workspace
+    float *lse2;                 // [record][q head]: m + log2 l, log2 units
+    float *part_ml;              // [record][q head][chunk][2]
+    float *part_o;               // [record][q head][chunk][Dv]
+    float *scores;               // [record][q head][score_stride], log2 units
+    int64_t score_stride;
+};
+
+// The division of a call's work, from the sizes alone.
+void plan_attend(AttendParams &p);
+// The workspace of a planned call: its parts at `base`, or without one the bytes
+// that serve it and every call of fewer records or positions.
+int64_t attend_workspace(AttendParams &p, char *base);
+
+struct SelectParams {
+    const float *acc;
+    int64_t acc_len, acc_stride;
+    int32_t rows;
+    const kvx_select_req *reqs;
+    int32_t n_reqs, max_tokens;
+    int32_t *kept;
+    int64_t kept_len, kept_stride;
+    float *out;
+    int64_t out_len, out_stride;
+    uint32_t *err;
+};
+
+struct KeptParams {
+    Side src, dst;
+    const kvx_req *reqs;
+    int32_t n_reqs, max_tokens;
+    int32_t L, C, H, vpr;
+    const int32_t *kept;
+    int64_t kept_len, kept_stride;
+    uint32_t *err;
+    int32_t blocks;              // workgroups per record, layer and head
+    FastDiv fd_Ts, fd_Td, fd_vpr;
+};
+
+// Each launches on `stream` and returns a hipError_t value.
+int launch_append(const AppendParams &p, hipStream_t stream);
+int launch_attend(const AttendParams &p, hipStream_t stream);
+int launch_select(const SelectParams &p, hipStream_t stream);
+int launch_kept(const KeptParams &p, hipStream_t stream);
+
+}  // namespace kvx

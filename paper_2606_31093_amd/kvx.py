@@ -6,8 +6,10 @@ kernels run on ``torch.cuda.current_stream()`` unless a stream is given.
 The functions keep the C names: ``kvx_transfer``, ``kvx_transfer_slice``,
 ``kvx_transfer_layered``, ``kvx_transfer_planned``,
 ``kvx_transfer_layered_planned``, ``kvx_gather``, ``kvx_scatter``,
-``kvx_gather_slice``, ``kvx_scatter_slice`` and ``kvx_page_hashes``.  A
-missing or unloadable library raises; there is no fallback path.
+``kvx_gather_slice``, ``kvx_scatter_slice`` and ``kvx_page_hashes``, and the
+calls of a decode step over a paged cache, ``kvx_append``, ``kvx_attend``,
+``kvx_select_kept`` and ``kvx_transfer_kept``.  A missing or unloadable
+library raises; there is no fallback path.
 
 Pool and buffer shapes are duck-typed: a pool shape has integer attributes
 ``L C H D T N e`` and a ``layout`` name; a buffer shape has ``L C H D e``
@@ -17,8 +19,11 @@ and ``cap`` (elements).  ``paper_2606_31093_amd.workloads.PoolSpec`` and
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import struct
+from dataclasses import dataclass
+from typing import Any
 
 import numpy as np
 
@@ -155,6 +160,17 @@ def load(path: str) -> ctypes.CDLL:
     L.kvx_launch_choice.restype = ctypes.c_int
     L.kvx_last_launch.argtypes = []
     L.kvx_last_launch.restype = ctypes.c_int
+    L.kvx_append.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp, i64, vp, i32, i32, vp, vp]
+    L.kvx_append.restype = ctypes.c_int
+    L.kvx_attend.argtypes = [vp, i32, vp, vp, vp, vp, ctypes.c_float, vp, i64, vp, i32, i32, vp, i64, i64, vp, i64, vp,
+                             vp]
+    L.kvx_attend.restype = ctypes.c_int
+    L.kvx_attend_workspace.argtypes = [vp, i32, i32, i32, i32, i32]
+    L.kvx_attend_workspace.restype = i64
+    L.kvx_select_kept.argtypes = [vp, i64, i64, i32, vp, i32, i32, vp, i64, i64, vp, i64, i64, vp, vp]
+    L.kvx_select_kept.restype = ctypes.c_int
+    L.kvx_transfer_kept.argtypes = [vp, vp, vp, vp, i64, vp, i64, vp, i32, i32, vp, i64, i64, vp, vp]
+    L.kvx_transfer_kept.restype = ctypes.c_int
     # The copy calls once more, with descriptors as packed bytes: a ctypes
     # structure per descriptor and call took half of a small call's time.
     for f in _PACKED:
@@ -603,3 +619,232 @@ def kvx_last_launch(library=None) -> int:
     """LAUNCH_NONE, LAUNCH_GRID or LAUNCH_SWEEP: the kind of the last kernel
     this thread's last copy call enqueued."""
     return int((library or lib()).kvx_last_launch())
+
+
+# ---------------------------------------------------------------------------
+# a decode step over a paged cache
+# ---------------------------------------------------------------------------
+
+APPEND_REQ_DTYPE = np.dtype([("pt_off", "<i8"), ("row_off", "<i8"), ("start", "<i4"), ("position", "<i4"),
+                             ("n_tokens", "<i4"), ("reserved", "<i4")])
+ATTEND_REQ_DTYPE = np.dtype([("pt_off", "<i8"), ("acc_off", "<i8"), ("start", "<i4"), ("end", "<i4")])
+SELECT_REQ_DTYPE = np.dtype([("acc_off", "<i8"), ("kept_off", "<i8"), ("out_off", "<i8"), ("n_tokens", "<i4"),
+                             ("n_keep", "<i4"), ("sink", "<i4"), ("recent", "<i4")])
+
+
+def _pack(rows, dtype) -> np.ndarray:
+    """Rows with a column per field of ``dtype`` (but ``reserved``) as records."""
+    names = [n for n in dtype.names if n != "reserved"]
+    rows = np.asarray(rows, dtype=np.int64).reshape(-1, len(names))
+    out = np.zeros(len(rows), dtype=dtype)
+    for i, name in enumerate(names):
+        col = rows[:, i]
+        if dtype[name].itemsize == 4 and ((col < -2**31) | (col >= 2**31)).any():
+            raise ValueError(f"{name} does not fit int32")
+        out[name] = col
+    return out
+
+
+def _device(records, device):
+    import torch
+    return torch.from_numpy(records.view(np.uint8).copy()).to(device)
+
+
+def device_append_reqs(rows, device="cuda"):
+    """(pt_off, row_off, start, position, n_tokens) rows as kvx_append_req
+    records on the device."""
+    return _device(_pack(rows, APPEND_REQ_DTYPE), device)
+
+
+def device_attend_reqs(rows, device="cuda"):
+    """(pt_off, acc_off, start, end) rows as kvx_attend_req records on the device."""
+    return _device(_pack(rows, ATTEND_REQ_DTYPE), device)
+
+
+def device_select_reqs(rows, device="cuda"):
+    """(acc_off, kept_off, out_off, n_tokens, n_keep, sink, recent) rows as
+    kvx_select_req records on the device."""
+    return _device(_pack(rows, SELECT_REQ_DTYPE), device)
+
+
+@dataclass(frozen=True)
+class Rope:
+    """A rotation (kvx_rope): ``freq`` a float32 device tensor of radians per
+    position, one for each rotated pair of a head; ``rot_off`` the first
+    rotated dimension; ``interleaved`` pairs (2j, 2j + 1) instead of (j, j +
+    pairs); ``amplitude`` a factor on the rotated values."""
+    freq: Any
+    rot_off: int = 0
+    interleaved: bool = False
+    amplitude: float = 1.0
+
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, factor: float = 1.0, scaling: str = "linear",
+                     trained: int = 0, fast: float = 32.0, slow: float = 1.0):
+    """(frequencies, amplitude) for ``Rope``: base ** (-2j / rot_dim) for the
+    rot_dim / 2 pairs, as a float32 numpy array, stretched for contexts
+    ``factor`` times as long as the trained ones:
+    - "linear": every frequency divided by factor;
+    - "base": the base raised to base * factor ** (rot_dim / (rot_dim - 2)), which
+      leaves the first frequency and divides the last by factor;
+    - "ramp": pairs that turn more than ``fast`` times within the ``trained``
+      length stay, those that turn less than ``slow`` times are divided by
+      factor, linearly in the pair's index between; the amplitude is
+      0.1 ln(factor) + 1."""
+    if rot_dim < 2 or rot_dim % 2 or base <= 1 or factor < 1:
+        raise ValueError("rot_dim must be even and >= 2, base above 1 and factor >= 1")
+    j = np.arange(0, rot_dim, 2, dtype=np.float64)
+    freq = base ** (-j / rot_dim)
+    if scaling == "linear":
+        return (freq / factor).astype(np.float32), 1.0
+    if scaling == "base":
+        if rot_dim < 4:
+            raise ValueError("scaling 'base' needs rot_dim >= 4")
+        return ((base * factor ** (rot_dim / (rot_dim - 2))) ** (-j / rot_dim)).astype(np.float32), 1.0
+    if scaling != "ramp":
+        raise ValueError(f"scaling must be 'linear', 'base' or 'ramp' (got {scaling!r})")
+    if trained < 1 or fast <= slow or slow <= 0:
+        raise ValueError("scaling 'ramp' needs the trained length and fast > slow > 0")
+
+    def pair(turns):                   # the (real) pair index that turns so often within `trained`
+        return rot_dim * math.log(trained / (2 * math.pi * turns)) / (2 * math.log(base))
+    lo, hi = max(0.0, math.floor(pair(fast))), min(rot_dim / 2 - 1.0, math.ceil(pair(slow)))
+    keep = 1 - np.clip((j / 2 - lo) / max(hi - lo, 1e-3), 0, 1)
+    return (freq * keep + freq / factor * (1 - keep)).astype(np.float32), 0.1 * math.log(factor) + 1
+
+
+_ROWS_PACK = struct.Struct("=Q3q4i").pack
+_ROPE_PACK = struct.Struct("=Q3if").pack
+_ROW_TYPES: dict = {}
+
+
+def _rows_arg(t, name: str) -> bytes:
+    """The kvx_rows of a [rows, heads, head_dim] tensor of 16-bit values,
+    packed; its last dimension must be contiguous."""
+    if not _ROW_TYPES:
+        import torch
+        _ROW_TYPES.update({torch.bfloat16: 0, torch.float16: 1})
+    code = _ROW_TYPES.get(t.dtype)
+    if code is None or t.dim() != 3:
+        raise ValueError(f"{name} must be a bfloat16 or float16 tensor [rows, heads, head_dim] "
+                         f"(got {t.dtype}, {t.dim()} dimensions)")
+    n, heads, d = t.shape
+    s_row, s_head, s_d = t.stride()
+    if s_d != 1 and d != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    # the stride of a dimension of one is never used, and torch leaves any value there
+    return _ROWS_PACK(t.data_ptr(), n, s_row if n > 1 else 0, s_head if heads > 1 else 0, heads, d, code, 0)
+
+
+def _floats(t, name: str):
+    """The address and length of an optional contiguous float32 tensor."""
+    if t is None:
+        return None, 0
+    if t.element_size() != 4 or not t.is_floating_point() or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous float32 tensor (got {t.dtype})")
+    return t.data_ptr(), t.numel()
+
+
+def _scales(t, spec):
+    if t is None:
+        return None
+    ptr, n = _floats(t, "scales")
+    if n != spec.C * spec.H:
+        raise ValueError(f"scales holds {n} values, the pool has {spec.C} x {spec.H}")
+    return ptr
+
+
+def _reqs_arg(reqs, dtype):
+    """The address and count of a tensor of records."""
+    n, rest = divmod(reqs.nbytes, dtype.itemsize)
+    if rest or not reqs.is_contiguous():
+        raise ValueError(f"reqs must be contiguous and hold whole records of {dtype.itemsize} bytes")
+    return reqs.data_ptr(), n
+
+
+def kvx_append(pool, spec, layer, k, v, pt, reqs, max_tokens, q=None, q_out=None, rope=None, scales=None,
+               dev_err=None, stream=None) -> None:
+    """New tokens' keys and values into their pages, rotated, and their
+    queries rotated (see kvx_append in include/kvx.h).  ``k``, ``v``, ``q`` and
+    ``q_out`` are [rows, heads, head_dim] tensors (slices of a fused projection
+    will do), ``v`` None for a pool of C 1; ``rope`` a ``Rope`` or None;
+    ``scales`` a float32 tensor [C, H] for an e4m3 pool (e 1)."""
+    P = _pool_arg(spec, pool, "pool")
+    table, n_pt = _table(pt, "pt")
+    rec, n = _reqs_arg(reqs, APPEND_REQ_DTYPE)
+    R = None
+    if rope is not None:
+        f, pairs = _floats(rope.freq, "rope.freq")
+        R = _ROPE_PACK(f or 0, 2 * pairs, int(rope.rot_off), int(bool(rope.interleaved)), float(rope.amplitude))
+    _check(lib().kvx_append(P, int(layer), _scales(scales, spec), None if q is None else _rows_arg(q, "q"),
+                            None if q_out is None else _rows_arg(q_out, "q_out"), _rows_arg(k, "k"),
+                            None if v is None else _rows_arg(v, "v"), R, table, n_pt, rec, n, int(max_tokens),
+                            _err_word(dev_err), _stream(stream)))
+
+
+def attend_workspace_bytes(spec, n_reqs: int, q_heads: int, max_tokens: int, v_dim=None,
+                           accumulate: bool = False) -> int:
+    """kvx_attend_workspace for a pool shape; ``v_dim`` defaults to head_dim."""
+    n = int(lib().kvx_attend_workspace(bytes(pool_desc(spec, 0)), int(n_reqs), int(q_heads),
+                                       int(spec.D if v_dim is None else v_dim), int(max_tokens), int(bool(accumulate))))
+    if n < 0:
+        raise KvxError(-5, lib().kvx_last_error().decode())
+    return n
+
+
+def attend_workspace(spec, n_reqs: int, q_heads: int, max_tokens: int, v_dim=None, accumulate: bool = False,
+                     device="cuda"):
+    """A workspace for kvx_attend calls of up to ``n_reqs`` records and
+    ``max_tokens`` positions, as a zeroed device tensor."""
+    import torch
+    return torch.zeros(attend_workspace_bytes(spec, n_reqs, q_heads, max_tokens, v_dim, accumulate),
+                       dtype=torch.uint8, device=device)
+
+
+def kvx_attend(q, out, pool, spec, layer, pt, reqs, max_tokens, workspace, scale=None, scales=None, lse=None,
+               acc=None, acc_stride=0, dev_err=None, stream=None) -> None:
+    """Attention of one query per record over a layer's pages (see kvx_attend
+    in include/kvx.h).  ``q`` [records, q heads, head_dim] and ``out``
+    [records, q heads, v_dim]; ``scale`` defaults to head_dim ** -0.5;
+    ``workspace`` from ``attend_workspace``; ``lse`` and ``acc`` optional float32
+    tensors."""
+    P = _pool_arg(spec, pool, "pool")
+    table, n_pt = _table(pt, "pt")
+    rec, n = _reqs_arg(reqs, ATTEND_REQ_DTYPE)
+    lse_ptr, n_lse = _floats(lse, "lse")
+    if lse is not None and n_lse < n * q.shape[1]:
+        raise ValueError(f"lse holds {n_lse} values, {n} records x {q.shape[1]} heads need more")
+    acc_ptr, n_acc = _floats(acc, "acc")
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    _check(lib().kvx_attend(P, int(layer), _scales(scales, spec), _rows_arg(q, "q"), _rows_arg(out, "out"), lse_ptr,
+                            float(spec.D ** -0.5 if scale is None else scale), table, n_pt, rec, n, int(max_tokens),
+                            acc_ptr, n_acc, int(acc_stride), workspace.data_ptr(), workspace.nbytes,
+                            _err_word(dev_err), _stream(stream)))
+
+
+def kvx_select_kept(acc, acc_stride, rows, reqs, max_tokens, kept, kept_stride, acc_out=None, acc_out_stride=0,
+                    dev_err=None, stream=None) -> None:
+    """The positions that each of ``rows`` lists of every record keeps, by
+    accumulated weight (see kvx_select_kept in include/kvx.h): ``acc`` and
+    ``acc_out`` float32, ``kept`` an int32 tensor."""
+    a, n_a = _floats(acc, "acc")
+    o, n_o = _floats(acc_out, "acc_out")
+    kp, n_k = _table(kept, "kept")
+    rec, n = _reqs_arg(reqs, SELECT_REQ_DTYPE)
+    _check(lib().kvx_select_kept(a, n_a, int(acc_stride), int(rows), rec, n, int(max_tokens), kp, n_k,
+                                 int(kept_stride), o, n_o, int(acc_out_stride), _err_word(dev_err), _stream(stream)))
+
+
+def kvx_transfer_kept(src, src_spec, dst, dst_spec, src_pt, dst_pt, reqs, max_tokens, kept, kept_stride, sl=None,
+                      dev_err=None, stream=None) -> None:
+    """Listed positions of every layer and head, pool -> pool (see
+    kvx_transfer_kept in include/kvx.h); ``reqs`` from ``device_reqs``, whose
+    buf_off is the record's first list in ``kept``; ``sl`` an optional slice."""
+    S, D = _pool_arg(src_spec, src, "src"), _pool_arg(dst_spec, dst, "dst")
+    X = None if sl is None else _slice_arg(sl)
+    spt, n_spt = _table(src_pt, "src_pt")
+    dpt, n_dpt = _table(dst_pt, "dst_pt")
+    kp, n_k = _table(kept, "kept")
+    _check(lib().kvx_transfer_kept(S, D, X, spt, n_spt, dpt, n_dpt, reqs.data_ptr(), _n_reqs(reqs), int(max_tokens),
+                                   kp, n_k, int(kept_stride), _err_word(dev_err), _stream(stream)))

@@ -1,0 +1,633 @@
+"""A decode step over a paged cache on the GPU (kvx_append, kvx_attend,
+kvx_select_kept, kvx_transfer_kept) against the definitions in 64 bits
+(np_decode), at the sizes, masks and strides where kernels go wrong.
+
+Bounds.  u is the unit roundoff of the rows' type, half its epsilon.
+- A rotated value is one rounding of a sum of two products in 32 bits with
+  cosine and sine good to 2^-22: u |x| + 2^-20 A (|a| + |b|).
+- e4m3 rounds to 4 bits: 2^-4 |x|, or half its smallest step, 2^-10.
+- A score's sum of D products is off by at most (D + 8) 2^-24 sum |q k|: call
+  that ds.  Weights are off by 2 ds + 2^-20 relatively, and rounded to the
+  rows' type, so out is off by u |out| + (u + 2 ds + 2^-20) sum w |v|, lse by ds +
+  2^-20 (1 + |lse|), an accumulator by (2 ds + 2^-20) w + 2^-23 (|acc| + w).
+- The choice of positions and the move of rows are exact."""
+import numpy as np
+import pytest
+import torch
+
+import np_decode as ref
+from paper_2606_31093_amd import kvx
+from paper_2606_31093_amd.workloads import LAYOUTS, PoolSpec
+
+pytestmark = pytest.mark.gpu
+
+U = {"bf16": torch.finfo(torch.bfloat16).eps / 2, "f16": torch.finfo(torch.float16).eps / 2}
+
+
+def tensor(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def rows_tensor(b, kind):
+    """16-bit values as a device tensor of their type."""
+    return tensor(np.ascontiguousarray(b).view(np.int16)).view(torch.bfloat16 if kind == "bf16" else torch.float16)
+
+
+def rows_values(t, kind):
+    return ref.values(t.contiguous().view(torch.int16).cpu().numpy().view(np.uint16), kind)
+
+
+def error_word():
+    return torch.zeros(1, dtype=torch.int32, device="cuda")
+
+
+def make_pool(rng, spec, kind, size=1.0):
+    """Random stored values of a pool, as bytes."""
+    n = spec.elems
+    if kind == "e4m3":
+        b = rng.integers(0, 256, n).astype(np.uint8)
+        b[(b & 127) == 127] = 0x20
+        return b
+    return ref.bits((rng.standard_normal(n) * size).astype(np.float32), kind).view(np.uint8)
+
+
+def make_table(rng, spec, ends):
+    count = [-(-e // spec.T) for e in ends]
+    assert sum(count) <= spec.N
+    off = np.concatenate([[0], np.cumsum(count)[:-1]]).astype(int) if len(count) else []
+    return rng.permutation(spec.N)[:max(1, sum(count))].astype(np.int32), [int(x) for x in off]
+
+
+# ---------------------------------------------------------------------------
+# kvx_append
+# ---------------------------------------------------------------------------
+
+def append_case(seed, spec, kind, cache, lens, starts, positions, Hq, rot, off, inter, amplitude, in_place=False,
+                fused=False):
+    rng = np.random.default_rng(seed)
+    total = sum(lens)
+    H, C, D = spec.H, spec.C, spec.D
+    xb = ref.bits(rng.standard_normal((total, Hq + C * H, D)).astype(np.float32), kind)
+    x = ref.values(xb, kind)
+    pool = make_pool(rng, spec, cache)
+    pt, offs = make_table(rng, spec, [s + n for s, n in zip(starts, lens)])
+    first = np.concatenate([[0], np.cumsum(lens)[:-1]]).astype(int)
+    rows = [[offs[r], first[r], starts[r], positions[r], lens[r]] for r in range(len(lens))]
+    freq = (10000.0 ** (-np.arange(rot // 2) * 2 / max(rot, 1))).astype(np.float32)
+    scales = (rng.random((C, H)) * 0.02 + 0.005).astype(np.float32) if cache == "e4m3" else None
+    xt = rows_tensor(xb, kind)
+    parts = [xt[:, :Hq], xt[:, Hq:Hq + H], xt[:, Hq + H:]]
+    if not fused:
+        parts = [p.contiguous() for p in parts]
+    q, k, v = parts
+    q_out = q if in_place else torch.zeros(total, Hq, D, dtype=q.dtype, device="cuda")
+    tp, err = tensor(pool), error_word()
+    rope = kvx.Rope(tensor(freq), off, inter, amplitude) if rot else None
+    kvx.kvx_append(tp, spec, spec.L - 1, k, v if C == 2 else None, tensor(pt), kvx.device_append_reqs(rows),
+                   max(lens + [0]), q=q if Hq else None, q_out=q_out if Hq else None, rope=rope,
+                   scales=None if scales is None else tensor(scales), dev_err=err)
+    torch.cuda.synchronize()
+    assert int(err.item()) == 0
+    got_q = rows_values(q_out, kind)
+    got, before = ref.canonical(tp.cpu().numpy(), spec), ref.canonical(pool, spec)
+    written = np.zeros(before.shape, bool)
+    size = x.copy()                       # |a| + |b| of each element's pair, where it rotates
+    u = U[kind]
+    for r, n in enumerate(lens):
+        for i in range(n):
+            row, p = first[r] + i, positions[r] + i
+            y = x[row].copy()
+            y[:Hq + H] = ref.rotate(x[row, :Hq + H], p, freq, off, inter, amplitude)
+            big = np.zeros_like(y)
+            big[:Hq + H, off:off + rot] = 1
+            size = big * amplitude * 2 * np.abs(x[row]).max()
+            tol = 2.0 ** -20 * size
+            assert (np.abs(got_q[row] - y[:Hq]) <= u * np.abs(y[:Hq]) + tol[:Hq]).all()
+            page, slot = ref.resolve(pt, offs[r], starts[r] + i, spec.T, spec.N)
+            for c in range(C):
+                written[spec.L - 1, page, c, slot] = True
+                z, t = y[Hq + c * H:Hq + (c + 1) * H], tol[Hq + c * H:Hq + (c + 1) * H]
+                have = ref.values(got[spec.L - 1, page, c, slot], cache)
+                if cache == "e4m3":
+                    z, t = z / scales[c][:, None].astype(np.float64), t / scales[c][:, None]
+                    z = np.clip(z, -448, 448)
+                    assert (np.abs(have - z) <= np.maximum(2.0 ** -4 * np.abs(z), 2.0 ** -10) + t).all()
+                else:
+                    assert (np.abs(have - z) <= u * np.abs(z) + t).all()
+                    if c == 1:
+                        assert (have == z).all()        # values are copied
+    assert (got[~written] == before[~written]).all()
+
+
+SHAPES = [
+    # (C, H, D, Hq, rot, off): full, part, part at the end, odd pairs, none, MLA
+    (2, 2, 64, 8, 64, 0), (2, 3, 128, 3, 64, 0), (2, 1, 80, 4, 20, 4), (2, 2, 96, 2, 32, 64), (2, 1, 16, 1, 2, 3),
+    (2, 2, 32, 6, 0, 0), (1, 1, 576, 5, 64, 512), (2, 4, 48, 0, 48, 0),
+]
+
+
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("kind,cache", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "e4m3"), ("f16", "e4m3")])
+@pytest.mark.parametrize("C,H,D,Hq,rot,off", SHAPES)
+def test_append(C, H, D, Hq, rot, off, kind, cache, inter):
+    spec = PoolSpec(2, C, H, D, T=16, N=20, e=1 if cache == "e4m3" else 2, layout=LAYOUTS[(D + Hq) % 4])
+    append_case(7, spec, kind, cache, [1, 0, 17, 33, 2], [15, 0, 3, 0, 40], [0, 5, 131000, 7, 1 << 30], Hq, rot, off,
+                inter, 1.0 if inter else 1.25)
+
+
+@pytest.mark.parametrize("T", [1, 7, 64])
+@pytest.mark.parametrize("layout", LAYOUTS)
+def test_append_pages(layout, T):
+    spec = PoolSpec(1, 2, 2, 64, T=T, N=-(-200 // T) + 4, e=2, layout=layout)
+    append_case(8, spec, "bf16", "bf16", [70, 1, 90], [0, 5, 6], [10, 20, 30], 4, 64, 0, False, 1.0)
+
+
+@pytest.mark.parametrize("rot,off,inter", [(64, 0, False), (64, 0, True), (20, 4, False), (20, 4, True), (8, 3, True)])
+def test_append_in_place_and_fused_rows(rot, off, inter):
+    spec = PoolSpec(1, 2, 2, 64, T=16, N=20, e=2)
+    append_case(9, spec, "bf16", "bf16", [40, 3], [0, 5], [10, 20], 4, rot, off, inter, 1.0, in_place=True, fused=True)
+
+
+def test_append_saturates_and_keeps_nan():
+    spec = PoolSpec(1, 1, 1, 16, T=16, N=1, e=1)
+    x = torch.tensor([1e6, -1e6, float("nan"), 448, 449, -464, 465, 1.0625, 0, -0.0, 2.0 ** -9, 2.0 ** -10, 3 * 2.0 ** -11,
+                      -1.1875, float("inf"), float("-inf")], dtype=torch.bfloat16,
+                     device="cuda").view(1, 1, 16)
+    pool, err = torch.zeros(spec.nbytes, dtype=torch.uint8, device="cuda"), error_word()
+    kvx.kvx_append(pool, spec, 0, x, None, tensor(np.zeros(1, np.int32)), kvx.device_append_reqs([[0, 0, 0, 0, 1]]), 1,
+                   dev_err=err)
+    want = x.float().clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8).flatten()
+    got = pool[:16]
+    nan = torch.isnan(x.flatten())
+    assert (got[~nan] == want[~nan]).all() and ((got[nan] & 127) == 127).all() and int(err.item()) == 0
+
+
+def test_append_device_errors():
+    spec = PoolSpec(1, 2, 1, 16, T=4, N=3, e=2)
+    k = torch.ones(40, 1, 16, dtype=torch.bfloat16, device="cuda")
+    rec = kvx._pack([[0, 0, 0, 0, 4], [1, 4, 0, 0, 4], [2, 8, 0, 0, 8], [0, 20, 4, 0, 4]], kvx.APPEND_REQ_DTYPE)
+
+    def run(rec, most=8):
+        pool, err = torch.zeros(spec.nbytes, dtype=torch.uint8, device="cuda"), error_word()
+        kvx.kvx_append(pool, spec, 0, k, k, tensor(np.array([2, 3, 1], np.int32)), tensor(rec.view(np.uint8)), most,
+                       dev_err=err)
+        return int(err.item()), ref.canonical(pool.cpu().numpy(), spec)
+    # record 1: page 3 of 3; record 2: its second page past the table; record 3: page 3 again
+    bits, got = run(rec)
+    assert bits == kvx.DERR_DST_PAGE | kvx.DERR_PT_RANGE
+    want = np.zeros_like(got)
+    want[0, 2], want[0, 1] = 0x3f80, 0x3f80
+    assert (got == want).all()
+    for field, x in (("pt_off", -1), ("row_off", -1), ("row_off", 37), ("start", -1), ("position", -1), ("n_tokens", -1),
+                     ("n_tokens", 9), ("reserved", 1), ("start", 2**31 - 4), ("position", 2**31 - 4)):
+        bad = rec[:1].copy()
+        bad[field] = x
+        bits, got = run(bad)
+        assert bits == kvx.DERR_BAD_REQ and (got == 0).all(), field
+
+
+# ---------------------------------------------------------------------------
+# kvx_attend
+# ---------------------------------------------------------------------------
+
+def attend_case(seed, spec, kind, cache, ranges, G, v_dim=None, acc=False, lse=True, scale=None, spoil=False,
+                strided=False, q_size=2.0, stream=None, bad=False):
+    rng = np.random.default_rng(seed)
+    H, D = spec.H, spec.D
+    Hq, v_dim, n = H * G, v_dim or D, len(ranges)
+    layer = spec.L - 1
+    pool = make_pool(rng, spec, cache)
+    ends = [e for _, e in ranges]
+    pt, offs = make_table(rng, spec, ends)
+    cap = max(ends + [1]) + 5
+    rows = [[offs[r], r * H * cap, s, e] for r, (s, e) in enumerate(ranges)]
+    canon = ref.canonical(pool, spec)
+    if spoil:        # everything that no request owns is NaN or infinite
+        nan = {"e4m3": [0x7f, 0xff], "bf16": [0x7fc0, 0x7f80, 0xff80], "f16": [0x7e00, 0x7c00, 0xfc00]}[cache]
+        own = np.zeros(canon.shape, bool)
+        for r, (s, e) in enumerate(ranges):
+            for t in range(s, e):
+                page, slot = ref.resolve(pt, offs[r], t, spec.T, spec.N)
+                own[layer, page, :, slot] = True
+        canon[~own] = rng.choice(nan, int((~own).sum()))
+    if bad:
+        pt[1], pt[2] = spec.N, -1
+    qb = ref.bits((rng.standard_normal((n, Hq, D)) * q_size).astype(np.float32), kind)
+    scales = (rng.random((spec.C, H)) * 0.02 + 0.01).astype(np.float32) if cache == "e4m3" else None
+    acc0 = rng.random((n, H, cap)).astype(np.float32)
+    scale = D ** -0.5 if scale is None else scale
+    q = rows_tensor(qb, kind)
+    out = torch.full((n, Hq, v_dim), 7.0, dtype=q.dtype, device="cuda")
+    if strided:
+        wide = torch.zeros(n, Hq + 2, D + 16, dtype=q.dtype, device="cuda")
+        wide[:, 1:-1, 8:-8] = q
+        q = wide[:, 1:-1, 8:-8]
+        room = torch.full((n, Hq + 3, v_dim + 24), 7.0, dtype=q.dtype, device="cuda")
+        out = room[:, 2:-1, 16:-8]
+    tl = torch.full((n, Hq), 5.0, device="cuda") if lse else None
+    ta, err = tensor(acc0) if acc else None, error_word()
+    most = max([e - s for s, e in ranges] + [0])
+    ws = kvx.attend_workspace(spec, n, Hq, most, v_dim, accumulate=acc)
+    kvx.kvx_attend(q, out, tensor(pool), spec, layer, tensor(pt), kvx.device_attend_reqs(rows), most, ws, scale=scale,
+                   scales=None if scales is None else tensor(scales), lse=tl, acc=ta, acc_stride=cap, dev_err=err,
+                   stream=stream)
+    torch.cuda.synchronize()
+    assert int(err.item()) == (kvx.DERR_SRC_PAGE if bad else 0)
+    with np.errstate(all="ignore"):
+        cv = ref.values(canon, cache)
+    want, want_lse, weights, mag, dots = ref.attend(ref.values(qb, kind), cv, spec, layer, pt, rows, scale, v_dim,
+                                                    None if scales is None else scales.astype(np.float64))
+    u, ds = U[kind], ((D + 8) * 2.0 ** -24 * dots)[:, None]
+    got = rows_values(out, kind)
+    tol = u * np.abs(want) + (u + 2 * ds + 2.0 ** -20)[..., None] * mag
+    if kind == "f16":                     # half's smallest steps, of outputs and of weights (against a maximum of 2^-8 or more)
+        tol += 2.0 ** -24 + 2.0 ** -17 * mag * max(most, 1) ** 0.5
+    assert (np.abs(got - want) <= tol).all(), (np.abs(got - want) - tol).max()
+    if lse:
+        g = tl.cpu().numpy().astype(np.float64)
+        none = np.isinf(want_lse)
+        assert (g[none] == -np.inf).all()
+        tol = np.broadcast_to(ds, none.shape)[~none] + 2.0 ** -20 * (1 + np.abs(want_lse[~none]))
+        assert (np.abs(g[~none] - want_lse[~none]) <= tol).all()
+    if acc:
+        a = ta.cpu().numpy().astype(np.float64)
+        full = acc0.astype(np.float64)
+        tol = np.zeros_like(full)
+        for r, (s, e) in enumerate(ranges):
+            full[r, :, s:e] += weights[r]
+            tol[r, :, s:e] = (2 * ds[r] + 2.0 ** -20) * weights[r] + 2.0 ** -23 * np.abs(full[r, :, s:e])
+        assert (np.abs(a - full) <= tol).all()
+    if strided:
+        room[:, 2:-1, 16:-8] = 7.0
+        assert (room == 7.0).all()
+
+
+LENGTHS = [(0, 1), (0, 0), (0, 31), (0, 32), (0, 33), (0, 100), (5, 5), (40, 41), (31, 97), (3, 260)]
+
+
+@pytest.mark.parametrize("kind,cache", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "e4m3"), ("f16", "e4m3")])
+@pytest.mark.parametrize("C,H,D,G,v", [(2, 2, 64, 4, 0), (2, 1, 128, 1, 0), (2, 3, 128, 7, 0), (2, 2, 80, 3, 0),
+                                       (2, 1, 16, 8, 0), (2, 1, 192, 16, 0), (2, 2, 256, 5, 0), (2, 1, 128, 17, 0),
+                                       (2, 2, 96, 40, 0), (2, 1, 160, 64, 0), (1, 1, 576, 16, 512), (1, 1, 576, 20, 512),
+                                       (1, 1, 576, 128, 512), (1, 2, 320, 4, 256), (1, 1, 64, 4, 48), (2, 1, 512, 3, 0)])
+def test_attend(C, H, D, G, v, kind, cache):
+    if cache == "e4m3" and D % 16:
+        pytest.skip("rows of 16 bytes")
+    spec = PoolSpec(2, C, H, D, T=16, N=60, e=1 if cache == "e4m3" else 2, layout=LAYOUTS[(D // 16 + G) % 4])
+    attend_case(D + G, spec, kind, cache, LENGTHS, G, v or None, acc=True, spoil=True)
+
+
+@pytest.mark.parametrize("T", [1, 5, 24, 64, 128])
+@pytest.mark.parametrize("layout", LAYOUTS)
+def test_attend_pages(layout, T):
+    spec = PoolSpec(1, 2, 2, 128, T=T, N=-(-900 // T) + 12, e=2, layout=layout)
+    attend_case(T, spec, "bf16", "bf16", LENGTHS + [(17, 300)], 4, acc=True, spoil=True)
+
+
+@pytest.mark.parametrize("C,H,D,G,v", [(2, 1, 128, 4, 0), (2, 2, 64, 8, 0), (1, 1, 576, 128, 512), (1, 1, 576, 32, 512)])
+def test_attend_long(C, H, D, G, v):
+    """Many chunks, of one long and of ragged requests; peaked and flat scores."""
+    spec = PoolSpec(1, C, H, D, T=64, N=240, e=2)
+    attend_case(1, spec, "bf16", "bf16", [(0, 6000)], G, v or None, acc=True, spoil=True)
+    attend_case(2, spec, "bf16", "bf16", [(4000, 4500), (0, 1), (0, 0), (77, 5000)], G, v or None, q_size=10.0)
+
+
+def test_attend_strides_and_no_lse():
+    spec = PoolSpec(2, 2, 2, 80, T=16, N=60, e=2)
+    attend_case(3, spec, "bf16", "bf16", LENGTHS, 4, strided=True, lse=False)
+
+
+def test_attend_pages_out_of_range_take_no_part():
+    spec = PoolSpec(1, 2, 2, 64, T=16, N=30, e=2)
+    attend_case(4, spec, "bf16", "bf16", [(0, 200), (0, 20)], 4, acc=True, bad=True)
+
+
+def test_attend_large_scores():
+    """Maxima that rise from tile to tile, and fall."""
+    spec = PoolSpec(1, 2, 1, 64, T=16, N=40, e=2)
+    attend_case(5, spec, "bf16", "bf16", [(0, 500), (3, 77)], 8, q_size=60.0, acc=True)
+
+
+def test_attend_on_another_stream():
+    s = torch.cuda.Stream()
+    spec = PoolSpec(1, 2, 2, 64, T=16, N=60, e=2)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        attend_case(6, spec, "bf16", "bf16", LENGTHS, 4, acc=True)
+
+
+def test_attend_nan_and_infinity_that_are_seen():
+    """NaN in a key reaches every output of its cache head, an infinite value only
+    its element; -inf scores weigh nothing, and alone they give zeros."""
+    spec = PoolSpec(1, 2, 2, 64, T=16, N=3, e=2)
+    pool = torch.zeros(spec.nbytes, dtype=torch.uint8, device="cuda")
+    p = pool.view(torch.bfloat16).view(1, 3, 2, 16, 2, 64)
+    p[:] = 0.25
+    p[0, 0, 0, 3, 0, 5] = float("nan")
+    p[0, 0, 1, 4, 1, 6] = float("inf")
+    p[0, 1, 0, :, :, 0] = float("-inf")
+    q = torch.ones(2, 4, 64, dtype=torch.bfloat16, device="cuda")
+    out, lse = torch.zeros_like(q), torch.zeros(2, 4, device="cuda")
+    ws = kvx.attend_workspace(spec, 2, 4, 16)
+    kvx.kvx_attend(q, out, pool, spec, 0, tensor(np.array([0, 1, 2], np.int32)),
+                   kvx.device_attend_reqs([[0, 0, 0, 16], [1, 0, 0, 16]]), 16, ws, lse=lse)
+    assert torch.isnan(out[0, :2]).all() and torch.isnan(lse[0, :2]).all()
+    assert torch.isinf(out[0, 2:, 6]).all() and torch.isfinite(lse[0, 2:]).all()
+    rest = [d for d in range(64) if d != 6]
+    assert (out[0, 2:][:, rest] == 0.25).all()
+    assert (out[1] == 0).all() and (lse[1] == float("-inf")).all()
+    kvx.kvx_attend(q, out, pool, spec, 0, tensor(np.array([0, 1, 2], np.int32)),
+                   kvx.device_attend_reqs([[0, 0, 0, 0], [1, 0, 8, 32]]), 24, ws, lse=lse)
+    assert (out[0] == 0).all() and (out[1] == 0.25).all() and torch.isfinite(lse[1]).all()
+
+
+def test_attend_malformed_records():
+    spec = PoolSpec(1, 2, 2, 64, T=16, N=10, e=2)
+    pool = torch.zeros(spec.nbytes, dtype=torch.uint8, device="cuda")
+    q = torch.ones(1, 4, 64, dtype=torch.bfloat16, device="cuda")
+    ws = kvx.attend_workspace(spec, 1, 4, 100, accumulate=True)
+    pt = tensor(np.arange(10, dtype=np.int32))
+    good = [0, 0, 3, 90]
+    for change, acc_len in (({}, 2 * 100), ({2: -1}, 200), ({3: 2}, 200), ({3: 104}, 300), ({1: -1}, 200), ({1: 11}, 200),
+                            ({}, 189), ({1: 2**40}, 200)):
+        row = [change.get(i, x) for i, x in enumerate(good)]
+        out, err = torch.full_like(q, 7.0), error_word()
+        acc = torch.zeros(acc_len, device="cuda")
+        kvx.kvx_attend(q, out, pool, spec, 0, pt, kvx.device_attend_reqs([row]), 100, ws, acc=acc, acc_stride=100,
+                       dev_err=err)
+        ok = not change and acc_len == 200
+        assert int(err.item()) == (0 if ok else kvx.DERR_BAD_REQ), (change, acc_len)
+        assert bool((out == 7.0).all()) != ok
+        assert bool((acc == 0).all()) != ok
+
+
+def test_attend_offsets_past_32_bits():
+    """Pages beyond 4 GiB of a layer's memory."""
+    spec = PoolSpec(1, 2, 8, 128, T=64, N=18000, e=2)          # 4.7 GB
+    pool = torch.zeros(spec.nbytes, dtype=torch.uint8, device="cuda")
+    p = pool.view(torch.bfloat16).view(18000, 2, 64, 8, 128)
+    pt = np.array([17999, 3, 17000, 16500], np.int32)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    for x in pt:
+        p[int(x)] = torch.randn(2, 64, 8, 128, generator=g, device="cuda").to(torch.bfloat16)
+    q = torch.randn(1, 8, 128, generator=g, device="cuda").to(torch.bfloat16)
+    out = torch.zeros_like(q)
+    kvx.kvx_attend(q, out, pool, spec, 0, tensor(pt), kvx.device_attend_reqs([[0, 0, 0, 250]]), 250,
+                   kvx.attend_workspace(spec, 1, 8, 250))
+    kv = torch.cat([p[int(x)] for x in pt], dim=1)[:, :250].double().cpu()        # 2, t, H, D
+    s = (q[0].double().cpu()[:, None] * kv[0].transpose(0, 1)).sum(-1) * 128 ** -0.5
+    w = torch.softmax(s, dim=1)
+    want = (w[:, :, None] * kv[1].transpose(0, 1)).sum(1)
+    mag = (w[:, :, None] * kv[1].transpose(0, 1).abs()).sum(1)
+    assert ((out[0].double().cpu() - want).abs() <= U["bf16"] * want.abs() + (U["bf16"] + 2.0 ** -15) * mag).all()
+    # and what is appended there
+    k = torch.randn(1, 8, 128, generator=g, device="cuda").to(torch.bfloat16)
+    kvx.kvx_append(pool, spec, 0, k, k, tensor(pt), kvx.device_append_reqs([[0, 0, 40, 9, 1]]), 1)
+    assert (p[17999, 0, 40] == k[0]).all() and (p[17999, 1, 40] == k[0]).all()
+
+
+def test_attend_workspace_serves_smaller_calls():
+    """One workspace, used in turn by calls of several sizes, gives each the results of a fresh one."""
+    spec = PoolSpec(1, 2, 2, 64, T=16, N=300, e=2)
+    rng = np.random.default_rng(3)
+    pool, pt = tensor(make_pool(rng, spec, "bf16")), tensor(rng.permutation(300).astype(np.int32))
+    q = rows_tensor(ref.bits(rng.standard_normal((20, 8, 64)).astype(np.float32), "bf16"), "bf16")
+    shared = kvx.attend_workspace(spec, 20, 8, 3000, accumulate=True)
+    for n, most, acc in ((20, 3000, True), (1, 3000, False), (3, 100, True), (20, 1, False), (2, 2999, True)):
+        res = []
+        for ws in (shared, kvx.attend_workspace(spec, n, 8, most, accumulate=acc)):
+            out, lse = torch.zeros(n, 8, 64, dtype=q.dtype, device="cuda"), torch.zeros(n, 8, device="cuda")
+            a = torch.zeros(n, 2, most, device="cuda") if acc else None
+            kvx.kvx_attend(q[:n], out, pool, spec, 0, pt,
+                           kvx.device_attend_reqs([[r, 2 * most * r, 0, most - r % 2] for r in range(n)]), most, ws, lse=lse,
+                           acc=a, acc_stride=most)
+            res.append([x.cpu() for x in ([out, lse] + ([a] if acc else []))])
+        assert all(torch.equal(x, y) for x, y in zip(*res))
+
+
+# ---------------------------------------------------------------------------
+# kvx_select_kept and kvx_transfer_kept
+# ---------------------------------------------------------------------------
+
+def select_case(seed, lens, keeps, sinks, recents, rows, make, with_out=True):
+    rng = np.random.default_rng(seed)
+    n, cap = len(lens), max(lens + [1]) + 3
+    kcap = max([min(a, b) for a, b in zip(lens, keeps)] + [1]) + 2
+    acc = np.stack([np.stack([make(rng, cap) for _ in range(rows)]) for _ in range(n)]).astype(np.float32)
+    rec = [[r * rows * cap, r * rows * kcap, r * rows * (kcap + 1), lens[r], keeps[r], sinks[r], recents[r]]
+           for r in range(n)]
+    kept = torch.full((n, rows, kcap), -7, dtype=torch.int32, device="cuda")
+    out = torch.full((n, rows, kcap + 1), -3.0, device="cuda") if with_out else None
+    err = error_word()
+    kvx.kvx_select_kept(tensor(acc), cap, rows, kvx.device_select_reqs(rec), max(lens + [0]), kept, kcap, out,
+                        kcap + 1 if with_out else 0, err)
+    assert int(err.item()) == 0
+    got, w = kept.cpu().numpy(), out.cpu().numpy() if with_out else None
+    for r in range(n):
+        for j in range(rows):
+            want = ref.select(acc[r, j, :lens[r]], keeps[r], sinks[r], recents[r])
+            m = len(want)
+            assert got[r, j, :m].tolist() == want, (r, j)
+            assert (got[r, j, m:] == -7).all()
+            if with_out:
+                np.testing.assert_array_equal(w[r, j, :m], acc[r, j, want])
+                assert (w[r, j, m:] == -3.0).all()
+
+
+WEIGHTS = {
+    "heavy": lambda rng, n: np.exp(3 * rng.standard_normal(n)),
+    "ties": lambda rng, n: rng.integers(0, 4, n),
+    "equal": lambda rng, n: np.ones(n),
+    "signed": lambda rng, n: np.where(rng.random(n) < 0.3, rng.choice([0.0, -0.0], n), rng.standard_normal(n)),
+    "special": lambda rng, n: rng.choice([np.nan, np.inf, -np.inf, 0.0, -0.0, 1e-45, -1e-45, 3.0], n),
+    "near": lambda rng, n: np.float32(1) + rng.integers(0, 9, n) * np.float32(2.0 ** -23),
+}
+
+
+@pytest.mark.parametrize("kind", sorted(WEIGHTS))
+def test_select(kind):
+    lens = [0, 1, 2, 64, 255, 256, 257, 1000, 3000, 700, 700, 5]
+    keeps = [4, 1, 1, 63, 255, 100, 1, 999, 1024, 30, 0, 5]
+    sinks = [1, 0, 0, 3, 0, 4, 0, 4, 4, 20, 0, 2]
+    recents = [1, 0, 1, 60, 5, 16, 1, 0, 128, 10, 0, 3]
+    select_case(11, lens, keeps, sinks, recents, 5, WEIGHTS[kind])
+
+
+@pytest.mark.parametrize("n,keep", [(9000, 2048), (20000, 19999), (40000, 7), (70000, 30000)])
+def test_select_long(n, keep):
+    select_case(12, [n, n // 2 + 1], [keep, keep // 2], [4, 0], [3, 0], 2, WEIGHTS["heavy"])
+    select_case(13, [n], [keep], [0], [0], 1, WEIGHTS["ties"], with_out=False)
+
+
+def test_select_malformed_records():
+    good = dict(acc_off=0, kept_off=0, out_off=0, n_tokens=50, n_keep=20, sink=2, recent=3)
+    acc = torch.rand(2 * 64, device="cuda")
+    for change in ({}, dict(acc_off=-1), dict(acc_off=15), dict(kept_off=-1), dict(kept_off=13), dict(out_off=7),
+                   dict(n_tokens=-1), dict(n_tokens=61), dict(n_keep=-1), dict(sink=18), dict(recent=-1), dict(sink=-2),
+                   dict(kept_off=2**40)):
+        row = dict(good, **change)
+        kept, out = torch.full((2 * 32,), -1, dtype=torch.int32, device="cuda"), torch.zeros(2 * 26, device="cuda")
+        err = error_word()
+        kvx.kvx_select_kept(acc, 64, 2, kvx.device_select_reqs([list(row.values())]), 60, kept[:64], 32, out, 26, err)
+        assert int(err.item()) == (kvx.DERR_BAD_REQ if change else 0), change
+        assert bool((kept == -1).all()) == bool(change) and bool((out == 0).all()) == bool(change)
+
+
+def kept_case(seed, S, D, lens, keeps, src_start, dst_start, sl=None, edit=None, want_bits=0):
+    rng = np.random.default_rng(seed)
+    l0, m0, nl, c0, d0, nc, h0, g0, nh = sl or (0, 0, S.L, 0, 0, S.C, 0, 0, S.H)
+    src = rng.integers(0, 256, S.nbytes).astype(np.uint8)
+    dst = rng.integers(0, 256, D.nbytes).astype(np.uint8)
+    spt, soff = make_table(rng, S, [s + n for s, n in zip(src_start, lens)])
+    dpt, doff = make_table(rng, D, [s + n for s, n in zip(dst_start, keeps)])
+    cap = max(keeps + [1]) + 1
+    kept = np.full((len(lens), nl, nh, cap), 1 << 30, np.int32)
+    for r in range(len(lens)):
+        for l in range(nl):
+            for h in range(nh):
+                kept[r, l, h, :keeps[r]] = np.sort(rng.choice(lens[r], keeps[r], replace=False))
+    rows = [[soff[r], doff[r], r * nl * nh * cap, src_start[r], dst_start[r], keeps[r]] for r in range(len(lens))]
+    if edit:
+        edit(kept, spt, dpt)
+    ts, td, err = tensor(src), tensor(dst), error_word()
+    kvx.kvx_transfer_kept(ts, S, td, D, tensor(spt), tensor(dpt), kvx.device_reqs(rows), max(keeps + [0]), tensor(kept),
+                          cap, sl, err)
+    assert int(err.item()) == want_bits
+    # bytes: rows of D * e, whatever they stand for
+    size = dict(S=(S, src), D=(D, dst.copy()))
+
+    def rows_of(spec, b):
+        dims = dict(l=spec.L, p=spec.N, c=spec.C, t=spec.T, h=spec.H)
+        have = ref.ORDER[spec.layout][:-1]
+        return b.reshape([dims[x] for x in have] + [spec.D * spec.e]).transpose([have.index(x) for x in "lpcth"] + [5])
+    want = size["D"][1]
+    s, d = rows_of(*size["S"]), rows_of(D, want)
+    for r in range(len(lens)):
+        for l in range(nl):
+            for h in range(nh):
+                for i in range(keeps[r]):
+                    k = int(kept[r, l, h, i])
+                    to = ref.resolve(dpt, doff[r], dst_start[r] + i, D.T, D.N)
+                    at = ref.resolve(spt, soff[r], src_start[r] + k, S.T, S.N) if k >= 0 else None
+                    if to and at:
+                        d[m0 + l, to[0], d0:d0 + nc, to[1], g0 + h] = s[l0 + l, at[0], c0:c0 + nc, at[1], h0 + h]
+    assert np.array_equal(td.cpu().numpy(), want)
+    assert np.array_equal(ts.cpu().numpy(), src)
+
+
+@pytest.mark.parametrize("e", [1, 2, 4, 8])
+@pytest.mark.parametrize("T,Td", [(16, 64), (64, 16), (24, 7), (1, 1)])
+@pytest.mark.parametrize("src,dst", [("LPCTHD", "LPCTHD"), ("LPCHTD", "PLCTHD"), ("PLCTHD", "PLCHTD"), ("PLCHTD", "LPCHTD")])
+def test_transfer_kept(src, dst, T, Td, e):
+    S = PoolSpec(2, 2, 3, 16, T=T, N=-(-400 // T) + 6, e=e, layout=src)
+    D = PoolSpec(2, 2, 3, 16, T=Td, N=-(-300 // Td) + 6, e=e, layout=dst)
+    kept_case(T + Td, S, D, [100, 1, 30, 200, 3], [64, 1, 0, 130, 3], [0, 5, 0, 3, 0], [0, 0, 0, 9, 1])
+
+
+@pytest.mark.parametrize("C,H,D", [(1, 1, 576), (2, 1, 8), (2, 5, 72), (2, 2, 128)])
+def test_transfer_kept_rows(C, H, D):
+    S = PoolSpec(2, C, H, D, T=16, N=40, e=2)
+    kept_case(D, S, S, [300, 70], [150, 69], [0, 0], [0, 2])
+
+
+def test_transfer_kept_slice():
+    S = PoolSpec(4, 2, 6, 32, T=16, N=40, e=2, layout="PLCTHD")
+    D = PoolSpec(3, 1, 4, 32, T=32, N=20, e=2, layout="LPCHTD")
+    kept_case(5, S, D, [300, 70], [150, 69], [0, 0], [0, 2], sl=(1, 0, 2, 1, 0, 1, 2, 1, 3))
+
+
+def test_transfer_kept_device_errors():
+    S = PoolSpec(2, 2, 2, 16, T=16, N=40, e=2)
+
+    def entries(kept, spt, dpt):
+        kept[0, 0, 0, 3], kept[0, 1, 1, 0] = -1, 1 << 29
+    kept_case(6, S, S, [200], [100], [0], [0], edit=entries, want_bits=kvx.DERR_PT_RANGE)
+
+    def pages(kept, spt, dpt):
+        spt[1], dpt[0] = -1, 40
+    kept_case(7, S, S, [200], [100], [0], [0], edit=pages, want_bits=kvx.DERR_SRC_PAGE | kvx.DERR_DST_PAGE)
+
+
+def test_transfer_kept_malformed_records():
+    S = PoolSpec(1, 1, 1, 16, T=4, N=4, e=1)
+    src, pt = torch.ones(S.nbytes, dtype=torch.uint8, device="cuda"), tensor(np.arange(4, dtype=np.int32))
+    kept = tensor(np.arange(12, dtype=np.int32))
+    for i, x in ((2, -1), (2, 5), (3, -1), (4, -1), (5, -1), (5, 9), (3, 2**31 - 4)):
+        row = [0, 0, 0, 0, 0, 8]
+        row[i] = x
+        dst, err = torch.zeros(S.nbytes, dtype=torch.uint8, device="cuda"), error_word()
+        kvx.kvx_transfer_kept(src, S, dst, S, pt, pt, kvx.device_reqs([row]), 8, kept, 12, None, err)
+        assert int(err.item()) == kvx.DERR_BAD_REQ and (dst == 0).all(), (i, x)
+
+
+# ---------------------------------------------------------------------------
+# together
+# ---------------------------------------------------------------------------
+
+def test_a_captured_step_replays():
+    """Append, attend with accumulators, select and move in one graph: every
+    replay gives what the same calls give."""
+    spec = PoolSpec(1, 2, 2, 64, T=16, N=64, e=2)
+    n, Hq, cap, keep = 4, 8, 200, 96
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    first = torch.randn(spec.elems, generator=g, device="cuda").to(torch.bfloat16).view(torch.uint8)
+    x = torch.randn(n, Hq + 4, 64, generator=g, device="cuda").to(torch.bfloat16)
+    freq = tensor(kvx.rope_frequencies(64)[0])
+    pt = tensor(np.random.default_rng(1).permutation(64)[:52].astype(np.int32))
+    lens = [180, 33, 97, 150]
+    areq = kvx.device_append_reqs([[13 * r, r, m - 1, m - 1, 1] for r, m in enumerate(lens)])
+    treq = kvx.device_attend_reqs([[13 * r, r * 2 * cap, 0, m] for r, m in enumerate(lens)])
+    sreq = kvx.device_select_reqs([[r * 2 * cap, r * 2 * keep, r * 2 * keep, m, keep, 4, 16] for r, m in enumerate(lens)])
+    mreq = kvx.device_reqs([[13 * r, 6 * r, r * 2 * keep, 0, 0, min(m, keep)] for r, m in enumerate(lens)])
+    dpt = tensor(np.arange(24, dtype=np.int32))
+    ws = kvx.attend_workspace(spec, n, Hq, 180, accumulate=True)
+
+    def state():
+        return dict(pool=first.clone(), q=torch.zeros(n, Hq, 64, dtype=torch.bfloat16, device="cuda"),
+                    out=torch.zeros(n, Hq, 64, dtype=torch.bfloat16, device="cuda"),
+                    acc=torch.zeros(n, 2, cap, device="cuda"),
+                    kept=torch.zeros(n, 2, keep, dtype=torch.int32, device="cuda"),
+                    left=torch.zeros(n, 2, keep, device="cuda"),
+                    dst=torch.zeros(spec.nbytes, dtype=torch.uint8, device="cuda"), err=error_word())
+
+    def step(s):
+        kvx.kvx_append(s["pool"], spec, 0, x[:, Hq:Hq + 2], x[:, Hq + 2:], pt, areq, 1, q=x[:, :Hq], q_out=s["q"],
+                       rope=kvx.Rope(freq), dev_err=s["err"])
+        kvx.kvx_attend(s["q"], s["out"], s["pool"], spec, 0, pt, treq, 180, ws, acc=s["acc"], acc_stride=cap,
+                       dev_err=s["err"])
+        kvx.kvx_select_kept(s["acc"], cap, 2, sreq, 180, s["kept"], keep, s["left"], keep, s["err"])
+        kvx.kvx_transfer_kept(s["pool"], spec, s["dst"], spec, pt, dpt, mreq, keep, s["kept"], keep, dev_err=s["err"])
+    eager, graphed = state(), state()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step(state())                    # what the runtime sets up on first use stays out of the capture
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step(graphed)
+    for _ in range(4):
+        graph.replay()
+        step(eager)
+        torch.cuda.synchronize()
+        assert int(eager["err"].item()) == 0
+        for k in eager:
+            assert torch.equal(eager[k], graphed[k]), k
+
+
+def test_example_decodes_with_a_bounded_cache():
+    """The example's loop: every step's weights add up to one a query head, what
+    eviction keeps is what the lists say, and the outputs of a step after
+    evictions are attention over the kept rows."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import decode_step
+    s, outs = decode_step.run(steps=150, n=3, budget=64, limit=100, verbose=False)
+    assert s.position == [150] * 3 and s.length == [150 - 2 * 36] * 3
+    assert sorted(s.free + sum(s.pages, [])) == list(range(s.spec.N))
+    s, outs = decode_step.run(steps=90, n=2, budget=64, limit=100, verbose=False)
+    total = s.acc.double().sum(dim=3)
+    assert ((total - 90 * 4).abs() < 90 * 4 * 2.0 ** -16).all()        # 4 query heads a cache head, no eviction yet
+    assert all(torch.isfinite(o).all() for o in outs)
