@@ -26,10 +26,10 @@ TEST_LIBRARY = os.path.join(PKG, "libkvx_test.so")
 TEST_DEFINES = ("KVX_HASH_IDLE_POLLS=1", "KVX_SWEEP_MIN_BYTES=0", "KVX_SWEEP_MAX_BLOCKS=2048",
                 "KVX_LAUNCH_CHOICE_DEFAULT=1", "KVX_ORDER_PAGES=0", "KVX_ORDER_PIECES=0",
                 "KVX_ORDER_QUARTERS=0", "KVX_ORDER_TURNS=0", "KVX_TEAM_KIB=0", "KVX_TEAM_UNIT=0")
-SOURCES = [os.path.join(CSRC, f) for f in ("kvx_kernels.hip", "kvx_hash.hip", "kvx_append.hip", "kvx_attend.hip",
+SOURCES = [os.path.join(CSRC, f) for f in ("kvx_kernels.hip", "kvx_hash.hip", "kvx_append.hip", "kvx_attend.hip", "kvx_attend_wide.hip",
                                            "kvx_kept.hip", "kvx_api.cpp", "kvx_ops_api.cpp")]
 HEADERS = [os.path.join(INCLUDE, "kvx.h")] + [os.path.join(CSRC, f) for f in (
-    "kvx_internal.h", "kvx_hash.h", "kvx_host.h", "kvx_ops.h", "kvx_values.h")]
+    "kvx_internal.h", "kvx_hash.h", "kvx_host.h", "kvx_ops.h", "kvx_attend.h", "kvx_values.h")]
 ARCH = "gfx950"
 
 

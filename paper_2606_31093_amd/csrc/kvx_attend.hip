@@ -2,10 +2,17 @@
 // (gfx950).
 //
 // Mathematics.  s = scale q.K, softmax over the positions, out = p V, in one
-// pass over the cache with a running maximum m and sum l.  A workgroup takes
-// `chunk` positions of one record and cache head; the chunks of a record are
+// pass over the cache with a running maximum m and sum l.  Scores are kept in
+// units of log2, so that a weight is one exp2.
+//
+// Division of the work.  A unit is a record and some of its cache heads (or a
+// part of their query heads); it takes a step for every 32 to 128 positions.
+// Only the device knows the lengths, so the workgroups, as many as the device
+// holds at a time, add them up and take equal shares of all steps in order.  A
+// unit that lies in one share is finished there; the parts of the others are
 // joined by a second launch: out = sum 2^(m_c - M) o_c / sum 2^(m_c - M) l_c.
-// Scores are kept in units of log2, so that a weight is one exp2.
+// Where no record takes more than a few steps, each unit has its own workgroup
+// instead, and there is no second launch.
 //
 // Matrix products without a move between lanes.  A wavefront takes 32
 // positions at a time against 16 query heads of one cache head (a group of
@@ -23,220 +30,284 @@
 // So neither scores, weights nor values pass through LDS or between lanes,
 // except the row offsets that lanes resolve for each other, and the maxima.
 
-#include "kvx_ops.h"
-#include "kvx_values.h"
+#include "kvx_attend.h"
 
 namespace kvx {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr int kTile = 32;               // positions a wavefront takes at a time
-// Weights are taken against a reference that follows the running maximum: it
-// starts kLift below it and is raised when a tile's maximum is more than kSlack
-// above where that leaves it, so that the sums are seldom rescaled.  Half has
-// 2^-14 as smallest normal value and 65504 as largest: lifted by 7, weights up
-// to 2^15, the small ones keep their digits 7 binades longer.
-constexpr float kSlack = 8.0f;
-template <bool F16>
-constexpr float kLift = F16 ? 7.0f : 0.0f;
-constexpr float kLn2 = 0.6931471805599453f;
 
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+// A tile's rows while they are on their way: K in the shape of the first
+// product's A operand, V as the second product's B operand before its
+// transposition.
+template <bool E4M3, int DC, int W, int NB, int TT>
+struct Tile {
+    static constexpr int KL = E4M3 ? DC / 2 : DC;    // 16-byte loads of a row's quarter
+    static constexpr int VD = E4M3 ? W / 4 : W / 2;  // dwords of W elements
+    uint32_t k[2 * TT][KL][4];
+    uint32_t v[TT][NB][8][VD];
+};
 
-// 2^(x - m), 0 where nothing has been seen (m = -inf).
-__device__ __forceinline__ float weight(float x, float m) { return m == -INFINITY ? 0.f : exp2_fast(x - m); }
-
-__device__ __forceinline__ bool valid(const kvx_attend_req &q, const AttendParams &p) {
-    if (q.start < 0 || q.end < q.start || q.end - q.start > p.max_tokens) return false;
-    if (!p.acc) return true;
-    // accumulators [acc_off + start, acc_off + (H - 1) * stride + end) lie inside
-    return q.acc_off >= 0 && q.acc_off <= p.acc_len && q.end <= p.acc_len - q.acc_off &&
-           (p.pool.H == 1 || p.acc_stride <= (p.acc_len - q.acc_off - q.end) / (p.pool.H - 1));
+template <int N>
+__device__ __forceinline__ void load_dwords(uint32_t *to, const char *from) {
+    typedef __attribute__((ext_vector_type(N))) uint32_t vec;
+    const vec v = __builtin_nontemporal_load(reinterpret_cast<const vec *>(from));
+#pragma unroll
+    for (int i = 0; i < N; ++i) to[i] = v[i];
 }
 
-// Chunks of a record that hold positions (at least one, for its zeros).
-__device__ __forceinline__ int used_chunks(const kvx_attend_req &q, int chunk) {
-    const int n = q.end - (q.start & -kTile);
-    return q.end > q.start ? (n + chunk - 1) / chunk : 1;
+template <>
+__device__ __forceinline__ void load_dwords<1>(uint32_t *to, const char *from) {
+    to[0] = *reinterpret_cast<const uint32_t *>(from);
 }
 
-template <bool F16, bool E4M3, int DC, int W, int NB>
-__global__ void __launch_bounds__(64 * kWaves) kvx_attend_kernel(AttendParams p, int32_t r0) {
+// EXACT: head_dim and v_dim are 32 DC and 16 W NB; else the elements past them
+// are read from the row's begin and taken as 0.  TT: 32 positions a wavefront
+// takes at a time.
+template <bool F16, bool E4M3, int DC, int W, int NB, int TT, bool EXACT, bool ACC>
+__device__ __forceinline__ void attend_part(const AttendParams &p, const Part part, int64_t (*row_off)[64],
+                                            float (*ml)[16][2], float *joined) {
+    const kvx_attend_req rec = part.rec;
+    const int r = part.r, hb = part.hb;
+    const int64_t place = part.place;
     typedef Half<F16> V;
-    __shared__ int64_t row_off[kWaves][kTile];
-    __shared__ float ml[kWaves][16][2];
-    extern __shared__ float joined[];            // [waves_h][16][Dv], waves of the same heads only
-
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = lane & 15, quad = lane >> 4;
-    uint32_t b = blockIdx.x;
-    const uint32_t hb = b % (uint32_t)(p.pool.H * p.head_blocks);
-    b /= (uint32_t)(p.pool.H * p.head_blocks);
-    const int chunk = (int)(b % (uint32_t)p.chunks);
-    const int r = r0 + (int)(b / (uint32_t)p.chunks);
-    const int h = (int)hb / p.head_blocks;
-    const int wh = wave % p.waves_h, wt = wave / p.waves_h, waves_t = kWaves / p.waves_h;
+    constexpr int ES = E4M3 ? 1 : 2, TILE = 32 * TT;
+    constexpr uint64_t ALL = TT == 2 ? ~0ull : 0xffffffffull;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int c = lane & 15, quad = lane >> 4;
+    // waves along cache heads, blocks of 16 of their query heads, and positions
+    const int waves_t = kWaves / (p.waves_h * p.waves_k);
+    const int wt = wave % waves_t, wh = wave / waves_t % p.waves_h, wk = wave / (waves_t * p.waves_h);
+    const int h = hb / p.head_blocks * p.waves_k + wk;
     // first of this wave's 16 heads, within the group
-    const int g0 = (((int)hb % p.head_blocks) * p.waves_h + wh) * 16;
+    const int g0 = ((hb % p.head_blocks) * p.waves_h + wh) * 16;
 
-    const kvx_attend_req rec = p.reqs[r];
-    if (!valid(rec, p)) {
-        if (blockIdx.x % (uint32_t)(p.pool.H * p.head_blocks * p.chunks) == 0 && threadIdx.x == 0 && p.err)
-            atomicOr(p.err, KVX_DERR_BAD_REQ);
-        return;
-    }
-    if (chunk >= used_chunks(rec, p.chunk)) return;
-    const int begin = (rec.start & -kTile) + chunk * p.chunk;
-    const int end = rec.end - begin < p.chunk ? rec.end : begin + p.chunk;
+    // unsigned: a tile may begin past 2^31 - 1, the last position there is
+    const uint32_t begin = part.begin, end = part.end, first = rec.start;
+    const uint32_t step = waves_t * TILE;
 
-    // queries: head g0 + c, elements 8 quad.. of every 32
+    // A lane resolves position t0 + lane: its page id, and a tile later the row
+    // offset.  The load is unconditional, so that nothing waits for it early.
+    uint32_t bad = 0;
+    const auto entry = [&](uint32_t t) { return (uint64_t)rec.pt_off + fd_div(p.pool.fd_T, t); };
+    const auto look = [&](uint32_t t0) {
+        const uint32_t t = t0 + lane;
+        const uint64_t idx = entry(t < end ? t : end - 1);
+        return p.pool.pt[idx < (uint64_t)p.pool.pt_len ? idx : 0];
+    };
+    // The row offsets of a tile to LDS; returns the positions that take part.
+    const auto resolve = [&](uint32_t t0, int32_t page, int64_t *to) {
+        const uint32_t t = t0 + lane;
+        const bool in = lane < TILE && t >= first && t < end;
+        const uint32_t at = t < end ? t : end - 1;
+        const bool known = entry(at) < (uint64_t)p.pool.pt_len;
+        const bool ok = in && known && (uint32_t)page < (uint32_t)p.pool.N;
+        if (in && !ok) bad |= known ? KVX_DERR_SRC_PAGE : KVX_DERR_PT_RANGE;
+        // every lane writes: a branch for some would split the loop's registers' lives
+        const int64_t off = page * p.pool.s_p + (int64_t)(at - fd_div(p.pool.fd_T, at) * p.pool.fd_T.d) * p.pool.s_t;
+        to[lane] = ok ? off : 0;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        return (uint64_t)__ballot(ok);
+    };
+
+    const char *kbase = p.pool.base + h * p.pool.s_h;
+    const char *vbase = kbase + (p.pool.C - 1) * p.pool.s_c;
+    Tile<E4M3, DC, W, NB, TT> tile;
+    const auto load_k = [&](const int64_t *off) {
+#pragma unroll
+        for (int half = 0; half < 2 * TT; ++half) {
+            const char *row = kbase + off[16 * half + c];
+#pragma unroll
+            for (int j = 0; j < tile.KL; ++j) {
+                const int at = j * 64 + quad * 16;         // bytes
+                load_dwords<4>(tile.k[half][j], row + (EXACT || at < ES * p.pool.D ? at : 0));
+            }
+        }
+    };
+    const auto load_v = [&](const int64_t *off) {
+#pragma unroll
+        for (int i = 0; i < 8 * TT; ++i) {
+            const char *row = vbase + off[16 * (i / 4) + 4 * quad + i % 4];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const int d = (nb * 16 + c) * W;
+                load_dwords<tile.VD>(tile.v[i / 8][nb][i % 8], row + ES * (EXACT || d < p.Dv ? d : 0));
+            }
+        }
+    };
+
+    // Step j of the first product contracts 8 elements from dim(j) on: any order
+    // serves that gives a lane 16 consecutive bytes of its row.
+    const auto dim = [&](int j) { return E4M3 ? j / 2 * 64 + quad * 16 + j % 2 * 8 : j * 32 + quad * 8; };
+    // Heads of this wave.  Where they are 8 or fewer, bfloat16 weights take two
+    // columns: head c in column c, and in column c + 8 what its rounding to 8 bits
+    // left, whose product is added at the end.  (Half keeps 11 bits.)
+    const int heads = p.G - g0 < 16 ? p.G - g0 : 16;
+    const bool twice = !F16 && heads <= 8;
+    // queries
     u32x4 qv[DC];
     {
-        const bool on = g0 + c < p.G;
-        const char *src = p.q.base + r * p.q.s_row + (int64_t)(h * p.G + (on ? g0 + c : 0)) * p.q.s_head;
+        const int g = twice ? c & 7 : c;
+        const bool on = g < heads;
+        const char *src = p.q.base + r * p.q.s_row + (int64_t)(h * p.G + (on ? g0 + g : 0)) * p.q.s_head;
 #pragma unroll
         for (int j = 0; j < DC; ++j) {
-            const int d = j * 32 + quad * 8;
-            qv[j] = u32x4{0, 0, 0, 0};
-            if (on && d < p.pool.D) qv[j] = *reinterpret_cast<const u32x4 *>(src + 2 * d);
+            const int d = dim(j);
+            qv[j] = *reinterpret_cast<const u32x4 *>(src + 2 * (EXACT || d < p.pool.D ? d : 0));
         }
+#pragma unroll
+        for (int j = 0; j < DC; ++j)
+            if (!on || (!EXACT && dim(j) >= p.pool.D)) qv[j] = u32x4{0, 0, 0, 0};
     }
     const float k_scale = p.scales ? p.scales[h] : 1.f;
     const float v_scale = p.scales ? p.scales[(p.pool.C - 1) * p.pool.H + h] : 1.f;
     const float unit = p.scale_log2 * k_scale;
-    const char *kbase = p.pool.base + h * p.pool.s_h;
-    const char *vbase = kbase + (p.pool.C - 1) * p.pool.s_c;
 
     f32x4 o[NB * W];
 #pragma unroll
     for (int j = 0; j < NB * W; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
-    float *scores = p.scores ? p.scores + ((int64_t)r * p.pool.H * p.G + h * p.G + g0 + c) * p.score_stride -
-                                   (rec.start & -kTile)
-                             : nullptr;
+    // Scores of head c from the position 4 quad on; the other columns' go to a
+    // line of their own that nothing reads (64 spare floats a row of threads).
+    float *scores = nullptr;
+    if (ACC)
+        scores = (c < heads ? p.scores + ((int64_t)r * p.pool.H * p.G + h * p.G + g0 + c) * p.score_stride - (rec.start & -kTile)
+                            : p.spare) + 4 * quad;
 
-    // unsigned: a tile may begin past 2^31 - 1, the last position there is
-    for (uint32_t t0 = begin + wt * kTile; t0 < (uint32_t)end; t0 += waves_t * kTile) {
-        // row offsets of the tile's positions, and which of them take part
-        bool ok = false;
-        if (lane < kTile) {
-            const uint32_t t = t0 + lane;
-            int64_t off = 0;
-            ok = t >= (uint32_t)rec.start && t < (uint32_t)end;
-            if (ok) {
-                const uint32_t page_no = fd_div(p.pool.fd_T, t);
-                const uint64_t idx = (uint64_t)rec.pt_off + page_no;
-                if (idx >= (uint64_t)p.pool.pt_len) {
-                    ok = false;
-                    if (p.err) atomicOr(p.err, KVX_DERR_PT_RANGE);
-                } else {
-                    const int32_t page = p.pool.pt[idx];
-                    if (page < 0 || page >= p.pool.N) {
-                        ok = false;
-                        if (p.err) atomicOr(p.err, KVX_DERR_SRC_PAGE);
-                    } else {
-                        off = page * p.pool.s_p + (int64_t)(t - page_no * p.pool.fd_T.d) * p.pool.s_t;
-                    }
+    uint32_t t0 = begin + wt * TILE;
+    if (t0 < end) {
+        uint64_t mask = resolve(t0, look(t0), row_off[2 * wave]);
+        int32_t page = look(t0 + step);
+        // Page id, keys, values: asked for in the loop's order, which the loop's waits
+        // count on (in another order the first turn's wait would be one for all).
+        __builtin_amdgcn_sched_barrier(0);
+        load_k(row_off[2 * wave]);
+        __builtin_amdgcn_sched_barrier(0);
+        load_v(row_off[2 * wave]);
+        for (int turn = 0; t0 < end; t0 += step, turn ^= 1) {
+            // Keys and values of this tile are on their way.  Those of the next are
+            // asked for as soon as this tile's have been used, and its page ids were
+            // a tile earlier, so that loads are in flight at all times.  Behind the
+            // last tile they are asked for once more, from the layer's first row: a
+            // branch around them would make the wait for this tile's loads one for all.
+            int64_t *next = row_off[2 * wave + (turn ^ 1)];
+            const uint64_t next_mask = resolve(t0 + step, page, next);
+            page = look(t0 + 2 * step);
+
+            // x[i]: the score of position 16 (i / 4) + 4 quad + i % 4
+            float x[8 * TT];
+#pragma unroll
+            for (int half = 0; half < 2 * TT; ++half) {
+                f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < DC; ++j) {
+                    u32x4 a = widen<F16, E4M3>(E4M3 ? tile.k[half][j / 2] + j % 2 * 2 : tile.k[half][j]);
+                    if (!EXACT && dim(j) >= p.pool.D) a = u32x4{0, 0, 0, 0};
+                    s = V::mfma(a, qv[j], s);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[4 * half + i] = s[i] * unit;
+            }
+            load_k(next);
+
+            if (mask != ALL) {
+                // positions that take no part: no weight, and values that bring no NaN
+                const uint64_t mine = mask >> (4 * quad);
+#pragma unroll
+                for (int i = 0; i < 8 * TT; ++i) {
+                    if ((mine >> (16 * (i / 4) + i % 4)) & 1) continue;
+                    x[i] = -INFINITY;
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                        for (int e = 0; e < tile.VD; ++e) tile.v[i / 8][nb][i % 8][e] = 0;
                 }
             }
-            row_off[wave][lane] = off;
-        }
-        const uint32_t mask = (uint32_t)__ballot(ok);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 
-        // scores of positions 4 quad + i and 16 + 4 quad + i
-        f32x4 s[2];
+            // the maximum of head c over the tile
+            float top = x[0];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const char *row = kbase + row_off[wave][16 * half + c];
-            s[half] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int i = 1; i < 8 * TT; ++i) top = fmaxf(top, x[i]);
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            if (__any(top - kLift<F16> > m + kSlack)) {
+                const float raised = fmaxf(m, top - kLift<F16>), f = weight(m, raised);
+                m = raised;
+                l *= f;
+                f32x4 fr;
 #pragma unroll
-            for (int j = 0; j < DC; ++j) {
-                const int d = j * 32 + quad * 8;
-                u32x4 a = {0, 0, 0, 0};
-                if (d < p.pool.D) {
-                    if (E4M3) {
-                        const u32x2 w = *reinterpret_cast<const u32x2 *>(row + d);
-                        a = u32x4{V::template from_e4m3<false>(w[0]), V::template from_e4m3<true>(w[0]),
-                                  V::template from_e4m3<false>(w[1]), V::template from_e4m3<true>(w[1])};
-                    } else {
-                        a = *reinterpret_cast<const u32x4 *>(row + 2 * d);
-                    }
-                }
-                s[half] = V::mfma(a, qv[j], s[half]);
+                for (int i = 0; i < 4; ++i) fr[i] = __shfl(f, 4 * quad + i);
+#pragma unroll
+                for (int j = 0; j < NB * W; ++j) o[j] *= fr;
             }
-        }
-        float x[8];
+            const float from = m == -INFINITY ? 0.f : m;       // then every x is -inf
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = s[i / 4][i % 4] * unit;
-        if (mask != 0xffffffffu) {
+            for (int u = 0; u < TT; ++u) {
+                float w[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (!((mask >> (16 * (i / 4) + 4 * quad + i % 4)) & 1)) x[i] = -INFINITY;
-        }
-        if (scores && g0 + c < p.G) {
-            *reinterpret_cast<f32x4 *>(scores + t0 + 4 * quad) = f32x4{x[0], x[1], x[2], x[3]};
-            *reinterpret_cast<f32x4 *>(scores + t0 + 16 + 4 * quad) = f32x4{x[4], x[5], x[6], x[7]};
-        }
+                for (int i = 0; i < 8; ++i) {
+                    w[i] = exp2_fast(x[8 * u + i] - from);
+                    l += w[i];
+                }
+                u32x4 a = {V::pack(w[0], w[1]), V::pack(w[2], w[3]), V::pack(w[4], w[5]), V::pack(w[6], w[7])};
+                if (twice && c >= 8) {
+                    // what the rounding of head c - 8 left
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) a[i] = V::pack(w[2 * i] - V::lo(a[i]), w[2 * i + 1] - V::hi(a[i]));
+                }
 
-        // the maximum of head c over the tile
-        float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        if (__any(top - kLift<F16> > m + kSlack)) {
-            const float next = fmaxf(m, top - kLift<F16>), f = weight(m, next);
-            m = next;
-            l *= f;
-            f32x4 fr;
+                // values: 8 positions x W elements a lane, transposed
 #pragma unroll
-            for (int i = 0; i < 4; ++i) fr[i] = __shfl(f, 4 * quad + i);
+                for (int nb = 0; nb < NB; ++nb) {
+                    uint32_t v[8][W / 2];
 #pragma unroll
-            for (int j = 0; j < NB * W; ++j) o[j] *= fr;
-        }
-        float w[8];
+                    for (int i = 0; i < 8; ++i) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            w[i] = weight(x[i], m);
-            l += w[i];
-        }
-        const u32x4 a = {V::pack(w[0], w[1]), V::pack(w[2], w[3]), V::pack(w[4], w[5]), V::pack(w[6], w[7])};
-
-        // values: 8 positions x W elements a lane
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            uint32_t v[8][W / 2];
-            const int d = (nb * 16 + c) * W;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const char *row = vbase + row_off[wave][16 * (i / 4) + 4 * quad + i % 4];
-#pragma unroll
-                for (int e = 0; e < W / 2; ++e) v[i][e] = 0;
-                // a position that takes no part must not bring its NaN
-                const bool use = d < p.Dv && ((mask >> (16 * (i / 4) + 4 * quad + i % 4)) & 1);
-                if (use) {
-                    if (E4M3) {
-#pragma unroll
-                        for (int e = 0; e < W / 4; ++e) {
-                            const uint32_t y = *reinterpret_cast<const uint32_t *>(row + d + 4 * e);
-                            v[i][2 * e] = V::template from_e4m3<false>(y);
-                            v[i][2 * e + 1] = V::template from_e4m3<true>(y);
+                        for (int e = 0; e < W / 2; ++e) {
+                            if (E4M3)
+                                v[i][e] = e % 2 ? V::template from_e4m3<true>(tile.v[u][nb][i][e / 2])
+                                                : V::template from_e4m3<false>(tile.v[u][nb][i][e / 2]);
+                            else
+                                v[i][e] = tile.v[u][nb][i][e];
+                            if (!EXACT && (nb * 16 + c) * W >= p.Dv) v[i][e] = 0;
                         }
-                    } else {
-                        __builtin_memcpy(v[i], __builtin_assume_aligned(row + 2 * d, 2 * W), 2 * W);
+                    }
+#pragma unroll
+                    for (int j = 0; j < W; ++j) {
+                        const uint32_t pick = j % 2 ? 0x07060302u : 0x05040100u;
+                        u32x4 bv;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            bv[i] = __builtin_amdgcn_perm(v[2 * i + 1][j / 2], v[2 * i][j / 2], pick);
+                        o[nb * W + j] = V::mfma(a, bv, o[nb * W + j]);
                     }
                 }
             }
+            load_v(next);
+            // Behind the loads, so that what waits for them does not wait for the
+            // stores; by all lanes, so that the waits count on them.
+            if (ACC) {
+                float *to = scores + (c < heads ? t0 : 0);
 #pragma unroll
-            for (int j = 0; j < W; ++j) {
-                const uint32_t pick = j % 2 ? 0x07060302u : 0x05040100u;
-                u32x4 bv;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) bv[i] = __builtin_amdgcn_perm(v[2 * i + 1][j / 2], v[2 * i][j / 2], pick);
-                o[nb * W + j] = V::mfma(a, bv, o[nb * W + j]);
+                for (int i = 0; i < 2 * TT; ++i)
+                    *reinterpret_cast<f32x4 *>(to + 16 * i) = f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
             }
+            mask = next_mask;
         }
     }
+    if (bad && p.err) atomicOr(p.err, bad);
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
+    if (twice) {
+#pragma unroll
+        for (int j = 0; j < NB * W; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                // an infinite value times a rest of 0 is NaN, and no part of the sum
+                const float rest = __shfl_xor(o[j][i], 32);
+                if (__builtin_fabsf(o[j][i]) < INFINITY) o[j][i] += rest;
+            }
+    }
 
     // Join the waves of the same heads: each scales to the common maximum, then
     // they add up in LDS, one after the other.
@@ -247,8 +318,9 @@ __global__ void __launch_bounds__(64 * kWaves) kvx_attend_kernel(AttendParams p,
         }
         __syncthreads();
         float all = -INFINITY, sum = 0.f;
-        for (int k = wh; k < kWaves; k += p.waves_h) all = fmaxf(all, ml[k][c][0]);
-        for (int k = wh; k < kWaves; k += p.waves_h) sum += ml[k][c][1] * weight(ml[k][c][0], all);
+        const int w0 = wave - wt;
+        for (int k = w0; k < w0 + waves_t; ++k) all = fmaxf(all, ml[k][c][0]);
+        for (int k = w0; k < w0 + waves_t; ++k) sum += ml[k][c][1] * weight(ml[k][c][0], all);
         const float f = weight(m, all);
         m = all;
         l = sum;
@@ -257,17 +329,14 @@ __global__ void __launch_bounds__(64 * kWaves) kvx_attend_kernel(AttendParams p,
         for (int i = 0; i < 4; ++i) fr[i] = __shfl(f, 4 * quad + i);
 #pragma unroll
         for (int j = 0; j < NB * W; ++j) o[j] *= fr;
-        float *mine = joined + (int64_t)wh * 16 * (NB * 16 * W);
+        f32x4 *mine = reinterpret_cast<f32x4 *>(joined) + (int64_t)(wave / waves_t) * 64 * NB * W + lane;
         for (int turn = 0; turn < waves_t; ++turn) {
             if (wt == turn) {
 #pragma unroll
-                for (int j = 0; j < NB * W; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float *at = mine + (4 * quad + i) * (NB * 16 * W) + (j / W * 16 + c) * W + j % W;
-                        if (turn > 0) o[j][i] += *at;
-                        if (turn < waves_t - 1) *at = o[j][i];
-                    }
+                for (int j = 0; j < NB * W; ++j) {
+                    if (turn > 0) o[j] += mine[64 * j];
+                    if (turn < waves_t - 1) mine[64 * j] = o[j];
+                }
             }
             __syncthreads();
         }
@@ -275,16 +344,16 @@ __global__ void __launch_bounds__(64 * kWaves) kvx_attend_kernel(AttendParams p,
     }
 
     const int64_t head0 = (int64_t)r * p.pool.H * p.G + h * p.G + g0;      // of the wave's 16
-    const bool last = used_chunks(rec, p.chunk) == 1;
-    if (quad == 0 && g0 + c < p.G) {
-        if (last) {
+    // a part's heads: those of wave block wk, from wh * 16 on
+    const int64_t part0 = place < 0 ? 0 : (place * p.waves_k + wk) * p.part_heads + wh * 16;
+    if (quad == 0 && c < heads) {
+        if (place < 0) {
             const float x = l > 0.f || l != l ? m + __builtin_amdgcn_logf(l) : -INFINITY;
             if (p.lse) p.lse[head0 + c] = x * kLn2;
-            if (p.lse2) p.lse2[head0 + c] = x;
+            p.lse2[head0 + c] = x;
         } else {
-            float *at = p.part_ml + ((head0 + c) * p.chunks + chunk) * 2;
-            at[0] = m;
-            at[1] = l;
+            p.part_ml[(part0 + c) * 2] = m;
+            p.part_ml[(part0 + c) * 2 + 1] = l;
         }
     }
     f32x4 lr;
@@ -293,8 +362,8 @@ __global__ void __launch_bounds__(64 * kWaves) kvx_attend_kernel(AttendParams p,
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int g = g0 + 4 * quad + i;
-        if (g >= p.G) continue;
-        if (last) {
+        if (4 * quad + i >= heads) continue;
+        if (place < 0) {
             const float f = lr[i] == 0.f ? 0.f : v_scale / lr[i];
             char *dst = p.out.base + r * p.out.s_row + (int64_t)(h * p.G + g) * p.out.s_head;
 #pragma unroll
@@ -308,7 +377,7 @@ __global__ void __launch_bounds__(64 * kWaves) kvx_attend_kernel(AttendParams p,
                 __builtin_memcpy(__builtin_assume_aligned(dst + 2 * d, 2 * W), w, 2 * W);
             }
         } else {
-            float *dst = p.part_o + ((head0 + 4 * quad + i) * p.chunks + chunk) * p.Dv;
+            float *dst = p.part_o + (part0 + 4 * quad + i) * p.Dv;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
                 const int d = (nb * 16 + c) * W;
@@ -322,104 +391,229 @@ __global__ void __launch_bounds__(64 * kWaves) kvx_attend_kernel(AttendParams p,
     }
 }
 
-// Joins the chunks of one record and query head: a wavefront per 64 outputs at
-// a time, every lane its element over all chunks.
-template <bool F16>
-__global__ void __launch_bounds__(256) kvx_attend_join_kernel(AttendParams p, int64_t first) {
-    const int64_t head = first + blockIdx.x;
-    const int Hq = p.pool.H * p.G;
-    const int r = (int)(head / Hq), hq = (int)(head % Hq);
-    const kvx_attend_req rec = p.reqs[r];
-    if (!valid(rec, p)) return;
-    const int n = used_chunks(rec, p.chunk);
-    if (n == 1) return;
-    const float *ml = p.part_ml + head * p.chunks * 2;
+// A workgroup's share, unit by unit.
+template <bool F16, bool E4M3, int DC, int W, int NB, int TT, bool EXACT, bool ACC>
+__global__ void __launch_bounds__(64 * kWaves) kvx_attend_kernel(AttendParams p, int32_t r0, int32_t n) {
+    __shared__ int32_t before[kAttendGroup + 1];
+    __shared__ __align__(16) int64_t row_off[2 * kWaves][64];
+    __shared__ float ml[kWaves][16][2];
+    extern __shared__ __align__(16) float joined[];   // [4 / waves along positions][W NB][lane][4]
+
+    Walk walk(p, r0, n, before, blockIdx.x);
+    Part part;
+    while (walk.next(p, before, &part)) {
+        attend_part<F16, E4M3, DC, W, NB, TT, EXACT, ACC>(p, part, row_off, ml, joined);
+        __syncthreads();                         // the next unit uses the same LDS
+    }
+}
+
+// The parts of a unit: shares first .. last, all or none of a unit in one.
+struct Parts {
+    int64_t first, last, unit0;
+    Shares s;
+    __device__ __forceinline__ Parts(const AttendParams &p, int32_t r, int hb, int32_t n) : s(p, p.before[n]) {
+        const int32_t steps = p.before[r + 1] - p.before[r];
+        unit0 = (int64_t)p.before[r] * p.per + (int64_t)hb * steps;
+        first = quotient(unit0, s.each);
+        last = steps > 0 ? quotient(unit0 + steps - 1, s.each) : first;
+    }
+    // a part's index of head g of the unit's cache head wk
+    __device__ __forceinline__ int64_t head(const AttendParams &p, int64_t k, int wk, int g) const {
+        return (s.place(p, unit0, k) * p.waves_k + wk) * p.part_heads + g;
+    }
+};
+
+// log2 of a head's sum over its parts of 2^score, by a wavefront: maximum m and
+// sum l of the parts' own.
+__device__ __forceinline__ float joined_lse(const AttendParams &p, const Parts &u, int wk, int g) {
     float m = -INFINITY, l = 0.f;
-    for (int k = threadIdx.x % 64; k < n; k += 64) m = fmaxf(m, ml[2 * k]);
+#pragma unroll 4
+    for (int64_t k = u.first + threadIdx.x % 64; k <= u.last; k += 64) {
+        const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * u.head(p, k, wk, g));
+        const float top = fmaxf(m, ml.x);
+        l = l * weight(m, top) + ml.y * weight(ml.x, top);
+        m = top;
+    }
+    const float mine = m;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
-    for (int k = threadIdx.x % 64; k < n; k += 64) l += ml[2 * k + 1] * weight(ml[2 * k], m);
+    l *= weight(mine, m);
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
-    if (threadIdx.x == 0) {
-        const float x = l > 0.f || l != l ? m + __builtin_amdgcn_logf(l) : -INFINITY;
-        if (p.lse) p.lse[head] = x * kLn2;
-        if (p.lse2) p.lse2[head] = x;
-    }
-    const int h = hq / p.G;
-    const float v_scale = p.scales ? p.scales[(p.pool.C - 1) * p.pool.H + h] : 1.f;
-    const float f = l == 0.f ? 0.f : v_scale / l;
-    const float *part = p.part_o + head * p.chunks * p.Dv;
-    char *dst = p.out.base + r * p.out.s_row + hq * p.out.s_head;
-    for (int d = threadIdx.x; d < p.Dv; d += 256) {
-        float x = 0.f;
-        for (int k = 0; k < n; ++k) x += part[(int64_t)k * p.Dv + d] * weight(ml[2 * k], m);
-        reinterpret_cast<uint16_t *>(dst)[d] = (uint16_t)Half<F16>::pack(x * f, 0.f);
-    }
+    return l > 0.f || l != l ? m + __builtin_amdgcn_logf(l) : -INFINITY;
 }
 
-// acc += sum over the group of 2^(score - lse): a thread per position.
-__global__ void __launch_bounds__(256) kvx_attend_acc_kernel(AttendParams p, int32_t r0, int32_t piece0, int32_t blocks) {
-    uint32_t b = blockIdx.x;
-    const int piece = piece0 + (int)(b % (uint32_t)blocks);
-    b /= (uint32_t)blocks;
-    const int h = (int)(b % (uint32_t)p.pool.H), r = r0 + (int)(b / (uint32_t)p.pool.H);
-    const kvx_attend_req rec = p.reqs[r];
+
+// The second launch.  Its first `joins` workgroups join the parts of a record
+// and query head each (Dv / 4 threads side by side, the parts dealt to as many
+// such rows of threads as fit, added up in LDS); the others add the weights
+// 2^(score - lse) of 4 positions a thread of a record and cache head to their
+// accumulators.  They do not wait for the joins: each takes lse from the
+// parts' maxima and sums itself.
+template <bool F16>
+__global__ void __launch_bounds__(1024) kvx_attend_finish_kernel(AttendParams p, int32_t r0, int32_t n, int64_t first,
+                                                                int64_t joins, int32_t runs) {
+    // partial outputs, maxima and sums of the rows of threads; a group's lse
+    extern __shared__ __align__(16) float sums[];
+    const int64_t at = first + blockIdx.x;
+    const int Hq = p.pool.H * p.G, tid = threadIdx.x;
+    const int span = p.span;
+    if (at < joins) {
+        const int r = (int)(at / Hq), hq = (int)(at % Hq), h = hq / p.G, g = hq % p.G;
+        const Parts u(p, r, h / p.waves_k * p.head_blocks + g / span, n);
+        if (u.first == u.last) return;           // written by the first launch, or malformed
+        const int wk = h % p.waves_k, gp = g % span, parts = (int)(u.last - u.first) + 1;
+        const int cols = p.Dv / 4, rows = blockDim.x / cols, col = tid % cols, row = tid / cols;
+        float *row_m = sums + 4 * blockDim.x, *row_l = row_m + blockDim.x / 2;      // cols >= 2
+        float m = -INFINITY, l = 0.f;
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        if (row < rows) {
+            for (int k0 = row; k0 < parts; k0 += 8 * rows) {
+                f32x4 x[8];
+                float2 y[8];
+                // all on their way at once; past the end the last one, without weight
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int k = k0 + i * rows < parts ? k0 + i * rows : parts - 1;
+                    const int64_t at = u.head(p, u.first + k, wk, gp);
+                    y[i] = *reinterpret_cast<const float2 *>(p.part_ml + 2 * at);
+                    x[i] = *reinterpret_cast<const f32x4 *>(p.part_o + at * p.Dv + 4 * col);
+                }
+                float top = m;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, y[i].x);
+                const float f = weight(m, top);
+                m = top;
+                l *= f;
+                sum *= f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (k0 + i * rows >= parts) continue;
+                    const float w = weight(y[i].x, m);
+                    l += y[i].y * w;
+                    sum += x[i] * w;
+                }
+            }
+            *reinterpret_cast<f32x4 *>(sums + 4 * tid) = sum;
+            if (col == 0) {
+                row_m[row] = m;
+                row_l[row] = l;
+            }
+        }
+        __syncthreads();
+        if (row != 0) return;
+        for (int k = 1; k < rows; ++k) m = fmaxf(m, row_m[k]);
+        sum = f32x4{0.f, 0.f, 0.f, 0.f};
+        l = 0.f;
+        for (int k = 0; k < rows; ++k) {
+            const float w = weight(row_m[k], m);
+            l += row_l[k] * w;
+            sum += *reinterpret_cast<const f32x4 *>(sums + 4 * (k * cols + col)) * w;
+        }
+        if (tid == 0 && p.lse)
+            p.lse[(int64_t)(r0 + r) * Hq + hq] = (l > 0.f || l != l ? m + __builtin_amdgcn_logf(l) : -INFINITY) * kLn2;
+        const float v_scale = p.scales ? p.scales[(p.pool.C - 1) * p.pool.H + h] : 1.f;
+        sum *= l == 0.f ? 0.f : v_scale / l;
+        char *dst = p.out.base + (r0 + r) * p.out.s_row + hq * p.out.s_head;
+        *reinterpret_cast<u32x2 *>(dst + 8 * col) =
+            u32x2{Half<F16>::pack(sum[0], sum[1]), Half<F16>::pack(sum[2], sum[3])};
+        return;
+    }
+    const int64_t b = at - joins;
+    const int run = (int)(b % runs), h = (int)(b / runs % p.pool.H), r = (int)(b / runs / p.pool.H);
+    const kvx_attend_req rec = p.reqs[r0 + r];
     if (!valid(rec, p)) return;
     const int base = rec.start & -kTile;
-    const int t = base + piece * 256 + (int)threadIdx.x;
-    if (t < rec.start || t >= rec.end) return;
-    const int64_t head0 = ((int64_t)r * p.pool.H + h) * p.G;
-    float x = 0.f;
-    for (int g = 0; g < p.G; ++g) {
-        const float lse = p.lse2[head0 + g];
-        if (lse != -INFINITY) x += exp2_fast(p.scores[(head0 + g) * p.score_stride + t - base] - lse);
+    if (rec.end - base <= run * 4 * (int)blockDim.x) return;
+    const int64_t head0 = ((int64_t)(r0 + r) * p.pool.H + h) * p.G;
+    // lse of the group's heads (at most 1024)
+    for (int g = tid / 64; g < p.G; g += blockDim.x / 64) {
+        float x = 0.f;
+        bool split = false;
+        if (!p.whole) {
+            const Parts u(p, r, h / p.waves_k * p.head_blocks + g / span, n);
+            split = u.first != u.last;
+            if (split) x = joined_lse(p, u, h % p.waves_k, g % span);
+        }
+        if (!split) x = p.lse2[head0 + g];
+        if (tid % 64 == 0) sums[g] = x;
     }
-    p.acc[rec.acc_off + h * p.acc_stride + t] += x;
+    __syncthreads();
+    const int t = 4 * (run * (int)blockDim.x + tid);     // from base
+    if (t >= rec.end - base) return;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    const float *scores = p.scores + head0 * p.score_stride + t;
+    for (int g = 0; g < p.G; ++g) {
+        const f32x4 s = *reinterpret_cast<const f32x4 *>(scores + g * p.score_stride);
+        const float lse = sums[g];
+        if (lse == -INFINITY) continue;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] += exp2_fast(s[i] - lse);
+    }
+    float *acc = p.acc + rec.acc_off + h * p.acc_stride + base + t;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (base + t + i >= rec.start && t + i < rec.end - base) acc[i] += x[i];
 }
 
-template <bool F16, bool E4M3>
+// Tiles of 64 positions where rows are short (128 bytes and less): a wavefront
+// then has 16 KiB on their way as with rows of 256.
+int tile_of(int D) { return D <= 64 ? 2 : 1; }
+
+template <bool F16, bool E4M3, bool ACC>
 auto pick(int D, int Dv) {
-    if (D <= 64) return kvx_attend_kernel<F16, E4M3, 2, 4, 1>;
-    if (D <= 128) return kvx_attend_kernel<F16, E4M3, 4, 8, 1>;
-    if (D <= 192) return kvx_attend_kernel<F16, E4M3, 6, 4, 3>;
-    if (D <= 256) return kvx_attend_kernel<F16, E4M3, 8, 8, 2>;
-    return kvx_attend_kernel<F16, E4M3, 18, 8, 4>;
+    const bool exact = D == Dv;
+    if (D == 64 && exact) return kvx_attend_kernel<F16, E4M3, 2, 4, 1, 2, true, ACC>;
+    if (D <= 64) return kvx_attend_kernel<F16, E4M3, 2, 4, 1, 2, false, ACC>;
+    if (D == 128 && exact) return kvx_attend_kernel<F16, E4M3, 4, 8, 1, 1, true, ACC>;
+    if (D <= 128) return kvx_attend_kernel<F16, E4M3, 4, 8, 1, 1, false, ACC>;
+    if (D <= 192) return kvx_attend_kernel<F16, E4M3, 6, 4, 3, 1, false, ACC>;
+    if (D == 256 && exact) return kvx_attend_kernel<F16, E4M3, 8, 8, 2, 1, true, ACC>;
+    return kvx_attend_kernel<F16, E4M3, 8, 8, 2, 1, false, ACC>;
 }
 
-int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : D <= 192 ? 192 : D <= 256 ? 256 : 512; }
+template <bool ACC>
+auto pick(const AttendParams &p) {
+    return p.f16 ? (p.e4m3 ? pick<true, true, ACC>(p.pool.D, p.Dv) : pick<true, false, ACC>(p.pool.D, p.Dv))
+                 : (p.e4m3 ? pick<false, true, ACC>(p.pool.D, p.Dv) : pick<false, false, ACC>(p.pool.D, p.Dv));
+}
+
+int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : D <= 192 ? 192 : 256; }
+
+// Workgroups that the device holds at a time (its 256 compute units; a
+// workgroup's registers leave room for 2 or 1 on each).
+int resident(int D) { return D <= 128 ? 512 : 256; }
+
+// A unit of up to this many steps is not worth a second launch: 8 steps take
+// less time than the launch does.
+constexpr int kWholeSteps = 8;
+// Fewer steps than this are not worth a share.
+constexpr int kLeastShare = 4;
 
 }  // namespace
-
-// Workgroups aimed at: 4 or more for each of the 256 compute units at equal
-// lengths; half as many where a workgroup holds 64 heads of 512 values, whose
-// partial sums would weigh against the cache read.
-static int64_t target(const AttendParams &p) { return p.waves_h == kWaves ? 1024 : 2048; }
 
 void plan_attend(AttendParams &p) {
     const int tiles = (p.G + 15) / 16;
     p.waves_h = tiles >= 4 ? 4 : tiles >= 2 ? 2 : 1;
     p.head_blocks = (tiles + p.waves_h - 1) / p.waves_h;
-    const int step = kTile * (kWaves / p.waves_h);          // positions a workgroup takes at a time
-    const int64_t units = (int64_t)p.n_reqs * p.pool.H * p.head_blocks;
-    const int64_t span = (int64_t)p.max_tokens + kTile - 1;
-    int64_t chunk = (span * units + target(p) - 1) / target(p);
-    chunk = (chunk + step - 1) / step * step;
-    if (chunk > span) chunk = (span + step - 1) / step * step;
-    if (chunk < step) chunk = step;
-    p.chunk = (int32_t)chunk;
-    p.chunks = (int32_t)((span + chunk - 1) / chunk);
-    p.score_stride = (span + kTile + 31) / 32 * 32;
-}
-
-// Partial results of a call with as many or fewer records and positions: units
-// * chunks is at most target + units, and at most one chunk per step.
-static int64_t most_parts(const AttendParams &p) {
-    const int step = kTile * (kWaves / p.waves_h);
-    const int64_t units = (int64_t)p.n_reqs * p.pool.H * p.head_blocks;
-    const int64_t span = (int64_t)p.max_tokens + kTile - 1;
-    const int64_t a = target(p) + units, b = units * ((span + step - 1) / step);
-    return (p.G + p.head_blocks - 1) / p.head_blocks * (a < b ? a : b);
+    p.waves_k = 1;
+    p.v_blocks = 1;
+    if (p.pool.D > 256) {
+        plan_attend_wide(p);
+    } else {
+    while (p.waves_h * p.waves_k < kWaves && p.pool.H % (2 * p.waves_k) == 0 && p.token_major) p.waves_k *= 2;
+    p.span = p.waves_h * 16;
+    p.step = 32 * tile_of(p.pool.D) * (kWaves / (p.waves_h * p.waves_k));
+    p.shares = resident(p.pool.D);
+    }
+    p.part_heads = p.G < p.span ? p.G : p.span;
+    p.per = p.pool.H / p.waves_k * p.head_blocks;
+    const int64_t span = (int64_t)p.max_tokens + kTile - 1, steps = (span + p.step - 1) / p.step;
+    p.whole = steps <= kWholeSteps;
+    const int64_t n = p.n_reqs < kAttendGroup ? p.n_reqs : kAttendGroup;
+    const int64_t most = (n * p.per * steps + kLeastShare - 1) / kLeastShare;
+    if (p.shares > most) p.shares = (int32_t)most;
+    p.score_stride = (span + 127) / 64 * 64;         // whole tiles
 }
 
 int64_t attend_workspace(AttendParams &p, char *base) {
@@ -430,48 +624,41 @@ int64_t attend_workspace(AttendParams &p, char *base) {
         at += (floats * 4 + 15) / 16 * 16;
         return x;
     };
-    const int64_t parts = base ? heads * p.chunks : most_parts(p);
+    // two parts a share, its first and its last
+    const int64_t parts = 2 * (int64_t)p.shares * p.waves_k * p.part_heads;
+    p.before = reinterpret_cast<int32_t *>(take(kAttendGroup + 1));
     p.lse2 = take(heads);
     p.part_ml = take(parts * 2);
     p.part_o = take(parts * p.Dv);
     p.scores = p.acc ? take(heads * p.score_stride) : nullptr;
+    p.spare = p.acc ? take(64) : nullptr;
     return at;
 }
 
+int launch_attend_narrow(const AttendParams &p, int32_t r0, int32_t n, hipStream_t stream) {
+    const auto kernel = p.acc ? pick<true>(p) : pick<false>(p);
+    const int streams = p.waves_h * p.waves_k;
+    const size_t lds = streams == kWaves ? 0 : sizeof(float) * streams * 16 * padded(p.pool.D);
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.whole ? n * p.per : p.shares)), dim3(64 * kWaves), lds, stream, p, r0, n);
+    return hipGetLastError();
+}
+
 int launch_attend(const AttendParams &p, hipStream_t stream) {
-    if (p.n_reqs == 0) return hipSuccess;
-    const auto kernel = p.f16 ? (p.e4m3 ? pick<true, true>(p.pool.D, p.Dv) : pick<true, false>(p.pool.D, p.Dv))
-                              : (p.e4m3 ? pick<false, true>(p.pool.D, p.Dv) : pick<false, false>(p.pool.D, p.Dv));
-    const size_t lds = p.waves_h == kWaves ? 0 : sizeof(float) * p.waves_h * 16 * padded(p.pool.D);
-    const int64_t per = (int64_t)p.pool.H * p.head_blocks * p.chunks;
-    int64_t group = kMaxBlocks / per > 0 ? kMaxBlocks / per : 1;
-    hipError_t e;
-    for (int64_t r0 = 0; r0 < p.n_reqs; r0 += group) {
-        const int64_t n = p.n_reqs - r0 < group ? p.n_reqs - r0 : group;
-        hipLaunchKernelGGL(kernel, dim3((uint32_t)(n * per)), dim3(64 * kWaves), lds, stream, p, (int32_t)r0);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
-    if (p.chunks > 1) {
-        const int64_t heads = (int64_t)p.n_reqs * p.pool.H * p.G;
-        for (int64_t at = 0; at < heads; at += kMaxBlocks) {
-            const int64_t n = heads - at < kMaxBlocks ? heads - at : kMaxBlocks;
-            hipLaunchKernelGGL(p.f16 ? kvx_attend_join_kernel<true> : kvx_attend_join_kernel<false>, dim3((uint32_t)n),
-                               dim3(256), 0, stream, p, at);
+    // Threads of the second launch: many parts of few heads need many rows of them.
+    const int threads = p.shares / (p.n_reqs < kAttendGroup ? p.n_reqs : kAttendGroup) / p.per >= 32 ? 1024 : 256;
+    const int32_t runs = (p.max_tokens + kTile - 1 + 4 * threads - 1) / (4 * threads);
+    for (int32_t r0 = 0; r0 < p.n_reqs; r0 += kAttendGroup) {
+        const int32_t n = p.n_reqs - r0 < kAttendGroup ? p.n_reqs - r0 : kAttendGroup;
+        int e = p.pool.D > 256 ? launch_attend_wide(p, r0, n, stream) : launch_attend_narrow(p, r0, n, stream);
+        if (e != hipSuccess) return e;
+        const int64_t joins = p.whole ? 0 : (int64_t)n * p.pool.H * p.G;
+        const int64_t blocks = joins + (p.acc ? (int64_t)n * p.pool.H * runs : 0);
+        for (int64_t at = 0; at < blocks; at += kMaxBlocks) {
+            const int64_t some = blocks - at < kMaxBlocks ? blocks - at : kMaxBlocks;
+            hipLaunchKernelGGL(p.f16 ? kvx_attend_finish_kernel<true> : kvx_attend_finish_kernel<false>,
+                               dim3((uint32_t)some), dim3(threads), sizeof(float) * 5 * threads, stream, p, r0, n, at,
+                               joins, runs);
             if ((e = hipGetLastError()) != hipSuccess) return e;
-        }
-    }
-    if (p.acc) {
-        const int32_t pieces = (p.max_tokens + kTile - 1 + 255) / 256;
-        const int32_t blocks = (int32_t)(kMaxBlocks / p.pool.H < pieces ? kMaxBlocks / p.pool.H : pieces);
-        const int64_t per_r = (int64_t)blocks * p.pool.H;
-        group = kMaxBlocks / per_r;
-        for (int32_t piece0 = 0; piece0 < pieces; piece0 += blocks) {
-            for (int64_t r0 = 0; r0 < p.n_reqs; r0 += group) {
-                const int64_t n = p.n_reqs - r0 < group ? p.n_reqs - r0 : group;
-                hipLaunchKernelGGL(kvx_attend_acc_kernel, dim3((uint32_t)(n * per_r)), dim3(256), 0, stream, p,
-                                   (int32_t)r0, piece0, blocks);
-                if ((e = hipGetLastError()) != hipSuccess) return e;
-            }
         }
     }
     return hipSuccess;

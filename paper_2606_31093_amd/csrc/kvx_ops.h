@@ -65,16 +65,26 @@ struct AttendParams {
     int64_t acc_len, acc_stride;
     uint32_t *err;
     int32_t f16, e4m3;
-    // launch: chunk positions per workgroup, chunks per record and head block,
-    // waves along heads, head blocks (of waves_h * 16 query heads) per cache head
-    int32_t chunk, chunks, waves_h, head_blocks;
+    int32_t token_major;
+    // launch: a workgroup's waves along cache heads and along blocks of 16 of their
+    // query heads (the others along positions); head blocks (of `span` query heads)
+    // per cache head, per record (per); positions of a step; whether every
+    // unit has its own workgroup (whole), else the shares of the steps; query
+    // heads of a part and cache head
+    int32_t waves_k, waves_h, span, head_blocks, per, step, whole, shares, part_heads;
+    int32_t v_blocks;            // workgroups that divide a unit's values among them
     // workspace
+    int32_t *before;             // [record of the launch + 1]: steps before it
     float *lse2;                 // [record][q head]: m + log2 l, log2 units
-    float *part_ml;              // [record][q head][chunk][2]
-    float *part_o;               // [record][q head][chunk][Dv]
+    float *part_ml;              // [place][cache head][part head][2]
+    float *part_o;               // [place][cache head][part head][Dv]
     float *scores;               // [record][q head][score_stride], log2 units
+    float *spare;                // 64 floats
     int64_t score_stride;
 };
+
+// Records of one launch of kvx_attend.
+constexpr int kAttendGroup = 1024;
 
 // The division of a call's work, from the sizes alone.
 void plan_attend(AttendParams &p);

@@ -95,6 +95,8 @@ int view_layer(const kvx_pool *pool, int32_t layer, const int32_t *pt, int64_t p
     return KVX_OK;
 }
 
+bool token_major(const kvx_pool *pool) { return pool->layout == KVX_LPCTHD || pool->layout == KVX_PLCTHD; }
+
 int launched(int e) {
     return e == hipSuccess ? KVX_OK
                            : fail(KVX_ERR_HIP, "kernel launch failed: %s", hipGetErrorString((hipError_t)e));
@@ -203,9 +205,12 @@ int64_t kvx_attend_workspace(const kvx_pool *pool, int32_t n_reqs, int32_t q_hea
         return -1;
     }
     AttendParams P{};
+    P.pool.C = s.C;
     P.pool.H = s.H;
     P.pool.D = s.D;
     P.G = q_heads / s.H;
+    P.token_major = token_major(pool);
+    P.e4m3 = s.e == 1;
     P.Dv = v_dim;
     P.n_reqs = n_reqs;
     P.max_tokens = max_tokens;
@@ -238,9 +243,12 @@ int kvx_attend(const kvx_pool *pool, int32_t layer, const float *scales, const k
     if (acc && (st = check_array(acc, acc_len, acc_stride, "acc"))) return st;
     if (n_reqs == 0) return KVX_OK;
     AttendParams P{};
+    P.pool.C = s.C;
     P.pool.H = s.H;
     P.pool.D = s.D;
     P.G = q->num_heads / s.H;
+    P.token_major = token_major(pool);
+    P.e4m3 = s.e == 1;
     P.Dv = out->head_dim;
     P.n_reqs = n_reqs;
     P.max_tokens = max_tokens;
@@ -263,13 +271,14 @@ int kvx_attend(const kvx_pool *pool, int32_t layer, const float *scales, const k
     if ((st = view(static_cast<char *>(workspace), need, "workspace", true, known, &ws))) return st;
     if ((st = view(reqs, (int64_t)n_reqs * (int64_t)sizeof *reqs, "reqs", false, known, &P.reqs))) return st;
     if ((st = view(dev_err, 4, "dev_err", true, known, &P.err))) return st;
+    // the kernel reads an entry for every position, also where none is in range
+    if (!P.pool.pt) P.pool.pt = reinterpret_cast<const int32_t *>(P.reqs);
     P.acc_len = acc_len;
     P.acc_stride = acc_stride;
     if (acc && !P.acc) P.acc = acc;      // no elements: every record with positions is malformed
     (void)attend_workspace(P, ws);
     P.scale_log2 = scale * 1.4426950408889634f;
     P.f16 = q->dtype == KVX_F16;
-    P.e4m3 = s.e == 1;
     return launched(launch_attend(P, static_cast<hipStream_t>(stream)));
 }
 
