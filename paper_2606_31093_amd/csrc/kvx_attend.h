@@ -100,6 +100,17 @@ struct Part {
     int64_t place;
 };
 
+// The same record in scalar registers (loaded, it comes in vector registers).
+__device__ __forceinline__ kvx_attend_req scalar(const kvx_attend_req &q) {
+    uint32_t w[6];
+    __builtin_memcpy(w, &q, sizeof w);
+#pragma unroll
+    for (int i = 0; i < 6; ++i) w[i] = __builtin_amdgcn_readfirstlane(w[i]);
+    kvx_attend_req s;
+    __builtin_memcpy(&s, w, sizeof w);
+    return s;
+}
+
 // The parts of a workgroup's share, in order.  Uniform over the workgroup.
 struct Walk {
     int64_t at, stop;            // units (p.whole), or steps of all units in order
@@ -128,7 +139,7 @@ struct Walk {
         if (p.whole) {
             part->r = r0 + (int)(at / p.per);
             part->hb = (int)(at % p.per);
-            part->rec = p.reqs[part->r];
+            part->rec = scalar(p.reqs[part->r]);
             at = stop;
             here = steps_of(part->rec, p);
             if (here == 0) {
@@ -148,7 +159,7 @@ struct Walk {
             const int steps = __builtin_amdgcn_readfirstlane(before[r + 1]) - base;
             const int64_t in = at - (int64_t)base * p.per;
             part->r = r0 + r;
-            part->rec = p.reqs[part->r];
+            part->rec = scalar(p.reqs[part->r]);
             part->hb = (int)quotient(in, steps);
             step0 = (int)(in - (int64_t)part->hb * steps);
             here = stop - at < steps - step0 ? (int)(stop - at) : steps - step0;

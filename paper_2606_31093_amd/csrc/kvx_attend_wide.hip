@@ -133,18 +133,22 @@ __global__ void __launch_bounds__(64 * WAVES) kvx_attend_wide_kernel(AttendParam
             // computed again instead of kept in registers.
             int ln = lane;
             asm volatile("" : "+v"(ln));
-            const auto one = [&](int q) {
+            const auto from = [&](int q) {
                 const bool is_v = two && q >= row_chunks / 2;
                 const uint32_t u = (is_v ? q - row_chunks / 2 : q) * 64 + ln;
                 const uint32_t row = u / (uint32_t)row_chunks, x = (u - row * row_chunks) ^ (row & 7);
-                const char *from = kbase + off[row] + 16 * ((int)x < chunks ? x : 0) + (is_v ? p.pool.s_c : 0);
-                load_lds(from, tile + q * 1024);
+                return kbase + off[row] + 16 * ((int)x < chunks ? x : 0) + (is_v ? p.pool.s_c : 0);
             };
             if (LATENT) {
+                // addresses first: each load to LDS might write the offsets, for all the
+                // compiler knows, and would wait for the reads of the next one's
+                const char *at[LATENT_LOADS];
 #pragma unroll
-                for (int t = 0; t < LATENT_LOADS; ++t) one(wave * LATENT_LOADS + t);
+                for (int t = 0; t < LATENT_LOADS; ++t) at[t] = from(wave * LATENT_LOADS + t);
+#pragma unroll
+                for (int t = 0; t < LATENT_LOADS; ++t) load_lds(at[t], tile + (wave * LATENT_LOADS + t) * 1024);
             } else {
-                for (int t = 0; t < loads; ++t) one(wave * loads + t);
+                for (int t = 0; t < loads; ++t) load_lds(from(wave * loads + t), tile + (wave * loads + t) * 1024);
             }
         };
 
@@ -205,8 +209,10 @@ __global__ void __launch_bounds__(64 * WAVES) kvx_attend_wide_kernel(AttendParam
             if (mask != 0xffffffffu) {
                 // positions that take no part must not bring their NaN: zeros in their place
                 const u32x4 zero = {0, 0, 0, 0};
-                for (int base = 0; base < tile_bytes; base += 1024 * WAVES) {
-                    const int at = base + threadIdx.x * 16;
+                int th = threadIdx.x * 16;
+                asm volatile("" : "+v"(th));               // as above
+#pragma unroll 1
+                for (int at = th; at < tile_bytes; at += 1024 * WAVES) {
                     if (!((mask >> (at / pitch & 31)) & 1)) *reinterpret_cast<u32x4 *>(tile + at) = zero;
                 }
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -255,9 +261,10 @@ __global__ void __launch_bounds__(64 * WAVES) kvx_attend_wide_kernel(AttendParam
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[i] = s[i] * unit;
             if (mask != 0xffffffffu) {
+                const uint32_t mine = mask >> (4 * e);
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (!((mask >> (8 * (i / 4) + 4 * e + i % 4)) & 1)) x[i] = -INFINITY;
+                    if (!((mine >> (8 * (i / 4) + i % 4)) & 1)) x[i] = -INFINITY;
             }
             float top = x[0];
 #pragma unroll
