@@ -41,9 +41,9 @@ __device__ __forceinline__ int steps_of(const kvx_attend_req &q, const AttendPar
 }
 
 // before[r] = steps of the launch's records 0 .. r-1, one cache head block's;
-// the last entry is the total.  All threads, 64 to 256.
+// the last entry is the total.  All threads, 64 to 512.
 __device__ __forceinline__ void add_up(const AttendParams &p, int32_t r0, int32_t n, int32_t *before) {
-    __shared__ int32_t waves[4];
+    __shared__ int32_t waves[8];
     const int tid = threadIdx.x, lane = tid % 64;
     const int threads = blockDim.x, each = (n + threads - 1) / threads;      // records a thread
     int32_t sum = 0;
@@ -115,7 +115,7 @@ __device__ __forceinline__ kvx_attend_req scalar(const kvx_attend_req &q) {
 struct Walk {
     int64_t at, stop;            // units (p.whole), or steps of all units in order
     int32_t r0, n, share;
-    // `id`: the unit (p.whole) or the share.  All threads, 64 to 256.
+    // `id`: the unit (p.whole) or the share.  All threads, 64 to 512.
     __device__ __forceinline__ Walk(const AttendParams &p, int32_t r0_, int32_t n_, int32_t *before, int32_t id)
         : at(id), stop(at + 1), r0(r0_), n(n_), share(id) {
         if (p.whole) {
