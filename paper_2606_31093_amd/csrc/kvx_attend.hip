@@ -597,7 +597,6 @@ void plan_attend(AttendParams &p) {
     p.waves_h = tiles >= 4 ? 4 : tiles >= 2 ? 2 : 1;
     p.head_blocks = (tiles + p.waves_h - 1) / p.waves_h;
     p.waves_k = 1;
-    p.v_blocks = 1;
     if (p.pool.D > 256) {
         plan_attend_wide(p);
     } else {

@@ -9,17 +9,17 @@
 // way), while the one before it is in use.  With c = lane % 16, e = lane / 16
 // the products are those of the narrow kernel, of 16 x 16:
 // - scores: A = 16 rows of K, B = the queries (registers, all their elements);
-//   lane (c, e) gets the scores of head c at positions 4 e + i, i < 4;
-// - those of 32 positions are the A operand of the second product, if its k
-//   index 8 e + i stands for position 16 (i / 4) + 4 e + i % 4;
-// - B = V: lane (c, e) reads 8 elements from (16 nb + c) * 8 on of those 8
-//   positions and transposes its 8 x 8 block with byte permutes.
+//   row r of product b < 2 is position 8 (r / 4) + 4 b + r % 4, so that lane (c, e)
+//   gets the scores of head c at positions 8 e + 4 b + i, i < 4;
+// - they are the A operand of the second product, whose k index is the position;
+// - B = V, from LDS by the loads that transpose: 16 lanes give the addresses of
+//   4 rows x 16 elements of 16 bits (8 x 16 of 8), lane c gets column c.
 //
 // LDS.  A row is cut into chunks of 16 bytes and padded to an odd multiple of 8 of
-// them; chunk x of row r lies at place x ^ (r / 2 % 8), so that one chunk of 16
-// rows (scores) and 16 chunks of a row (values) each lie in all 64 banks.
-// The loads write LDS in order of lanes; the permutation is in the addresses
-// they read.
+// them; chunk x of row r lies at place x ^ turn(r).  One chunk of the rows of a
+// product (scores), two of 4 and one of 8 successive rows (values) then lie in
+// different banks.  The loads write LDS in order of lanes; the permutation is in
+// the addresses they read.
 
 #include "kvx_attend.h"
 
@@ -27,8 +27,29 @@ namespace kvx {
 namespace {
 
 constexpr int kSteps = 18;               // 32 elements each: rows of up to 576
+constexpr int kTiles = 32;               // 16 values each: up to 512
+// Turns that reads of K and of V are ahead of their products, and one.  A query, its
+// outputs and these fill the 256 registers of one of two wavefronts on a SIMD: a
+// turn more of K took a wait for all loads per tile (170 us became 182).
+constexpr int kKDepth = 2, kVDepth = 4;
 
-constexpr int kBlocks = 2;                // values of a workgroup, 128 each
+// A row's permutation of its chunks, in each 8 of them.
+template <bool E4M3>
+__device__ __forceinline__ int turn(int r) {
+    return (r & 2) | ((r >> 1 ^ r >> 2) & 4) | (((E4M3 ? r >> 2 : 0) ^ r >> 4) & 1);
+}
+
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(2))) int s32x2;
+
+// The transposing loads: column c of the 4 (8) rows that a lane's group of 16 gives
+// the addresses of, 8 bytes a lane.
+__device__ __forceinline__ u32x2 columns16(const char *at) {
+    return bits<u32x2>(__builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at));
+}
+__device__ __forceinline__ u32x2 columns8(const char *at) {
+    return bits<u32x2>(__builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) s32x2 *)at));
+}
 
 // Bytes of a row in LDS.
 __host__ __device__ inline int pitch_of(int elems, bool e4m3) { return ((elems * (e4m3 ? 1 : 2) + 127) / 128 | 1) * 128; }
@@ -41,6 +62,14 @@ constexpr int tile_of(int waves) { return waves == 8 ? 64 : 32; }
 __device__ __forceinline__ void load_lds(const char *from, char *to) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
                                      (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
+
+// The lane, computed where it is used: the registers are full, and what is known
+// not to change would be kept in memory.  Reading it back waits for all loads.
+__device__ __forceinline__ int lane_again() {
+    int zero = 0;
+    asm volatile("" : "+s"(zero));
+    return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, zero));
 }
 
 // This wavefront's memory operations are done, and the workgroup's other
@@ -74,24 +103,7 @@ __global__ void __launch_bounds__(64 * WAVES, LATENT ? 2 : 1) kvx_attend_wide_ke
     constexpr int LATENT_LOADS = (E4M3 ? 640 : 1152) * TILE / 1024 / WAVES;
     const int loads = LATENT ? LATENT_LOADS : tile_bytes / 1024 / WAVES;      // a wavefront's, of a tile
 
-    // Two workgroups share a unit's values where they are more than 256: one takes
-    // the first 256, one the others.  They lie 8 apart, on one XCD, and the second
-    // finds the rows in its cache.
-    const int vb = p.v_blocks == 2 ? (int)(blockIdx.x / 8 % 2) : 0, v0 = 256 * vb;
-    const int id = p.v_blocks == 2 ? (int)(blockIdx.x / 16 * 8 + blockIdx.x % 8) : (int)blockIdx.x;
-    if (vb) p.err = nullptr;                             // the first one reports
-    // Addresses in LDS from a tile's begin.  Scores: chunk 4 j + e of row c, for
-    // j % 2 = i; values: this lane's first chunk of rows 4 e + 2 i and 4 e + 2 i + 1
-    // (the second a pitch behind).
-    int k_at[2], v_at[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        k_at[i] = c * pitch + ((4 * i + e) ^ (c >> 1)) * 16;
-        const int s = (2 * e + i) & 7;
-        v_at[i] = v_rows + (4 * e + 2 * i) * pitch + v0 * ES + (E4M3 ? ((c >> 1) ^ s) * 16 + (c & 1) * 8 : (c ^ s) * 16);
-    }
-
-    Walk walk(p, r0, n, before, id);
+    Walk walk(p, r0, n, before, blockIdx.x);
     Part part;
     while (walk.next(p, before, &part)) {
         const kvx_attend_req rec = part.rec;
@@ -103,33 +115,29 @@ __global__ void __launch_bounds__(64 * WAVES, LATENT ? 2 : 1) kvx_attend_wide_ke
         // A lane resolves position t0 + lane: its page id, and later the row offset.
         uint32_t bad = 0;
         const auto entry = [&](uint32_t t) { return (uint64_t)rec.pt_off + fd_div(p.pool.fd_T, t); };
-        const auto look = [&](uint32_t t0) {
-            const uint32_t t = t0 + lane;
+        const auto look = [&](uint32_t t0, int ln) {
+            const uint32_t t = t0 + ln;
             const uint64_t idx = entry(t < end ? t : end - 1);
             return p.pool.pt[idx < (uint64_t)p.pool.pt_len ? idx : 0];
         };
-        const auto resolve = [&](uint32_t t0, int32_t page, int64_t *to) {
-            const uint32_t t = t0 + lane;
-            const bool in = lane < TILE && t >= first && t < end;
+        const auto resolve = [&](uint32_t t0, int32_t page, int64_t *to, int ln) {
+            const uint32_t t = t0 + ln;
+            const bool in = ln < TILE && t >= first && t < end;
             const uint32_t at = t < end ? t : end - 1;
             const bool known = entry(at) < (uint64_t)p.pool.pt_len;
             const bool ok = in && known && (uint32_t)page < (uint32_t)p.pool.N;
             if (in && !ok) bad |= known ? KVX_DERR_SRC_PAGE : KVX_DERR_PT_RANGE;
             const int64_t off = page * p.pool.s_p + (int64_t)(at - fd_div(p.pool.fd_T, at) * p.pool.fd_T.d) * p.pool.s_t;
-            if (TILE == 64 || lane < TILE) to[lane] = ok ? off : 0;
+            if (TILE == 64 || ln < TILE) to[ln] = ok ? off : 0;
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             return (uint64_t)__ballot(ok);
         };
         // This wavefront's loads of a tile: 1 KiB of it each, row by row.
-        const auto load_tile = [&](const int64_t *off, char *tile) {
-            // Not known to be the same in every turn, so that what follows from it is
-            // computed again instead of kept in registers.
-            int ln = lane;
-            asm volatile("" : "+v"(ln));
+        const auto load_tile = [&](const int64_t *off, char *tile, int ln) {
             const auto from = [&](int q) {
                 const bool is_v = two && q >= TILE * row_chunks / 64;
                 const uint32_t u = (is_v ? q - TILE * row_chunks / 64 : q) * 64 + ln;
-                const uint32_t row = u / (uint32_t)row_chunks, x = (u - row * row_chunks) ^ (row / 2 & 7);
+                const uint32_t row = u / (uint32_t)row_chunks, x = (u - row * row_chunks) ^ turn<E4M3>(row);
                 return kbase + off[row] + 16 * ((int)x < chunks ? x : 0) + (is_v ? p.pool.s_c : 0);
             };
             if (LATENT) {
@@ -169,167 +177,161 @@ __global__ void __launch_bounds__(64 * WAVES, LATENT ? 2 : 1) kvx_attend_wide_ke
         const float v_scale = p.scales ? p.scales[(p.pool.C - 1) * p.pool.H + h] : 1.f;
         const float unit = p.scale_log2 * k_scale;
 
-        f32x4 o[kBlocks][8];
+        f32x4 o[kTiles];
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[b][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < kTiles; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
         float m = -INFINITY, l = 0.f;
         float *scores = nullptr;
         if (ACC)
             scores = (c < heads ? p.scores + ((int64_t)part.r * p.pool.H * p.G + h * p.G + g0 + c) * p.score_stride -
                                       (rec.start & -kTile)
-                                : p.spare) + 4 * e;
+                                : p.spare) + 8 * e;
 
-        uint64_t mask = resolve(begin, look(begin), row_off[wave][0]);
-        load_tile(row_off[wave][0], tiles);
-        int32_t page = look(begin + TILE);
+        uint64_t mask = resolve(begin, look(begin, lane), row_off[wave][0], lane);
+        load_tile(row_off[wave][0], tiles, lane);
+        int32_t page = look(begin + TILE, lane);
         int buf = 0;
         for (uint32_t t0 = begin; t0 < end; t0 += TILE) {
             // this tile is here, and nobody reads the one before it any more
             arrive<(WAVES > 1)>();
             char *tile = tiles + buf * tile_bytes;
+            const int ln = lane_again(), lc = ln & 15, le = ln >> 4;
             buf ^= 1;
-            const uint64_t next_mask = resolve(t0 + TILE, page, row_off[wave][buf]);
-            page = look(t0 + 2 * TILE);
-            load_tile(row_off[wave][buf], tiles + buf * tile_bytes);
+            const uint64_t next_mask = resolve(t0 + TILE, page, row_off[wave][buf], ln);
+            page = look(t0 + 2 * TILE, ln);
+            load_tile(row_off[wave][buf], tiles + buf * tile_bytes, ln);
             constexpr uint64_t ALL = TILE == 64 ? ~0ull : 0xffffffffull;
             if (mask != ALL) {
                 // positions that take no part must not bring their NaN: zeros in their place
-                int th = threadIdx.x * 16;
-                asm volatile("" : "+v"(th));               // as above
+                uint32_t zero = 0;
+                asm volatile("" : "+v"(zero));             // as above
 #pragma unroll 1
-                for (int at = th; at < tile_bytes; at += 1024 * WAVES) {
-                    if (!((mask >> (at / pitch & (TILE - 1))) & 1)) *reinterpret_cast<u32x4 *>(tile + at) = u32x4{0, 0, 0, 0};
+                for (int at = (wave * 64 + ln) * 16; at < tile_bytes; at += 1024 * WAVES) {
+                    if (!((mask >> (at / pitch & (TILE - 1))) & 1))
+                        *reinterpret_cast<u32x4 *>(tile + at) = u32x4{zero, zero, zero, zero};
                 }
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 if (WAVES > 1) __builtin_amdgcn_s_barrier();
                 asm volatile("" ::: "memory");
             }
 
-            // x[b][i]: the score of position 16 b + 4 e + i
-            f32x4 x[2 * HALVES];
-#pragma unroll
+            // Addresses in LDS from a tile's begin: a lane's first chunk of its row of product
+            // 0, and of its first row of values.
+            const int k_row = 8 * (lc / 4) + lc % 4, v_row = 8 * le + (E4M3 ? lc / 2 : lc / 4);
+            const int k_at = k_row * pitch + (le ^ turn<E4M3>(k_row)) * 16;
+            const int v_at = v_rows + v_row * pitch + ((E4M3 ? 0 : lc % 4 / 2) ^ turn<E4M3>(v_row)) * 16 + lc % 2 * 8;
+            // not unrolled: twice the code took registers that there are not
+#pragma unroll 1
             for (int half = 0; half < HALVES; ++half) {
                 f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-                // A pair of steps is read ahead of the one in use; left alone the
+                // Product b's rows are 4 on; turn() takes that into account for 8 bits.
+                // Rows are read kKDepth - 1 turns ahead of the products; left alone the
                 // compiler would read all first, for which there are no registers.
-                u32x4 k[2][2][2];
-                const auto read_k = [&](int j0, u32x4 (*to)[2]) {
+                constexpr int WIDE = E4M3 ? 2 : 1, TURNS = kSteps / WIDE;         // steps a turn
+                u32x4 k[kKDepth][2];
+                const auto read_k = [&](int u) {
 #pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        const char *row = tile + (32 * half + 16 * b) * pitch;
-                        if (E4M3) {
-                            to[0][b] = *reinterpret_cast<const u32x4 *>(row + k_at[j0 / 2 % 2] + j0 / 4 * 128);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 2; ++i)
-                                to[i][b] = *reinterpret_cast<const u32x4 *>(row + k_at[i] + j0 / 2 * 128);
-                        }
-                    }
+                    for (int b = 0; b < 2; ++b)
+                        k[u % kKDepth][b] = *reinterpret_cast<const u32x4 *>(
+                            tile + (k_at ^ (u % 2 * 64 + (E4M3 ? 16 * b : 0))) + (32 * half + 4 * b) * pitch + u / 2 * 128);
                 };
-                read_k(0, k[0]);
 #pragma unroll
-                for (int j0 = 0; j0 < kSteps; j0 += 2) {
-                    if (!LATENT && 32 * j0 >= D) continue;
-                    if (j0 + 2 < kSteps && (LATENT || 32 * j0 + 64 < D)) read_k(j0 + 2, k[j0 / 2 % 2 ^ 1]);
+                for (int u = 0; u < kKDepth - 1; ++u) read_k(u);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int j = j0 + i;
+                for (int u = 0; u < TURNS; ++u) {
+                    if (!LATENT && 32 * WIDE * u >= D) continue;
+                    if (u + kKDepth - 1 < TURNS && (LATENT || 32 * WIDE * (u + kKDepth - 1) < D)) read_k(u + kKDepth - 1);
+#pragma unroll
+                    for (int i = 0; i < WIDE; ++i) {
 #pragma unroll
                         for (int b = 0; b < 2; ++b) {
-                            u32x4 a = k[j0 / 2 % 2][E4M3 ? 0 : i][b];
+                            u32x4 a = k[u % kKDepth][b];
                             if (E4M3) {
                                 const uint32_t w[2] = {a[2 * i], a[2 * i + 1]};
                                 a = widen<F16, true>(w);
                             }
-                            if (!LATENT && (E4M3 ? (j / 2 * 4 + e) * 16 : j * 32 + e * 8) >= D) a = u32x4{0, 0, 0, 0};
-                            s[b] = V::mfma(a, qv[j], s[b]);
+                            if (!LATENT && (E4M3 ? (4 * u + le) * 16 : u * 32 + le * 8) >= D) a = u32x4{0, 0, 0, 0};
+                            s[b] = V::mfma(a, qv[WIDE * u + i], s[b]);
                         }
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
+                // x[b][i]: the score of position 32 half + 8 e + 4 b + i
+                f32x4 x[2];
 #pragma unroll
-                for (int b = 0; b < 2; ++b) x[2 * half + b] = s[b] * unit;
-            }
-            if (mask != ALL) {
-                const uint64_t mine = mask >> (4 * e);
+                for (int b = 0; b < 2; ++b) x[b] = s[b] * unit;
+                if (mask != ALL) {
+                    const uint32_t mine = (uint32_t)(mask >> (32 * half)) >> (8 * le);
 #pragma unroll
-                for (int b = 0; b < 2 * HALVES; ++b)
+                    for (int i = 0; i < 8; ++i)
+                        if (!((mine >> i) & 1)) x[i / 4][i % 4] = -INFINITY;
+                }
+                if (ACC) {
+                    float *to = scores + (lc < heads ? t0 + 32 * half : 0);
+                    *reinterpret_cast<f32x4 *>(to) = x[0];
+                    *reinterpret_cast<f32x4 *>(to + (lc < heads ? 4 : 0)) = x[1];
+                }
+                float top = x[0][0];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (!((mine >> (16 * b + i)) & 1)) x[b][i] = -INFINITY;
-            }
-            mask = next_mask;
-            if (ACC && vb == 0) {
-                float *to = scores + (c < heads ? t0 : 0);
+                for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i / 4][i % 4]);
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                if (__builtin_amdgcn_ballot_w64(top - kLift<F16> > m + kSlack) != 0) {
+                    const float raised = fmaxf(m, top - kLift<F16>);
+                    const float f = weight(m, raised);
+                    m = raised;
+                    l *= f;
+                    f32x4 fr;
 #pragma unroll
-                for (int b = 0; b < 2 * HALVES; ++b) *reinterpret_cast<f32x4 *>(to + (c < heads ? 16 * b : 0)) = x[b];
-            }
-            float top = x[0][0];
+                    for (int i = 0; i < 4; ++i) fr[i] = __shfl(f, 4 * le + i);
 #pragma unroll
-            for (int i = 1; i < 8 * HALVES; ++i) top = fmaxf(top, x[i / 4][i % 4]);
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            if (__builtin_amdgcn_ballot_w64(top - kLift<F16> > m + kSlack) != 0) {
-                const float raised = fmaxf(m, top - kLift<F16>);
-                const float f = weight(m, raised);
-                m = raised;
-                l *= f;
-                f32x4 fr;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) fr[i] = __shfl(f, 4 * e + i);
-#pragma unroll
-                for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) o[b][j] *= fr;
-            }
-            const float from = m == -INFINITY ? 0.f : m;       // then every x is -inf
-            u32x4 a[HALVES];
-#pragma unroll
-            for (int half = 0; half < HALVES; ++half) {
+                    for (int j = 0; j < kTiles; ++j) o[j] *= fr;
+                }
+                const float from = m == -INFINITY ? 0.f : m;       // then every x is -inf
                 float w[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    w[i] = exp2_fast(x[2 * half + i / 4][i % 4] - from);
+                    w[i] = exp2_fast(x[i / 4][i % 4] - from);
                     l += w[i];
                 }
-                a[half] = u32x4{V::pack(w[0], w[1]), V::pack(w[2], w[3]), V::pack(w[4], w[5]), V::pack(w[6], w[7])};
-                if (twice && c >= 8) {
+                u32x4 a = {V::pack(w[0], w[1]), V::pack(w[2], w[3]), V::pack(w[4], w[5]), V::pack(w[6], w[7])};
+                if (twice && lc >= 8) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) a[half][i] = V::pack(w[2 * i] - V::lo(a[half][i]), w[2 * i + 1] - V::hi(a[half][i]));
+                    for (int i = 0; i < 4; ++i) a[i] = V::pack(w[2 * i] - V::lo(a[i]), w[2 * i + 1] - V::hi(a[i]));
                 }
-            }
-#pragma unroll
-            for (int half = 0; half < HALVES; ++half) {
-#pragma unroll
-                for (int nb = 0; nb < kBlocks; ++nb) {
-                    uint32_t v[8][4];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const char *at = tile + v_at[i / 2 % 2] + (32 * half + 16 * (i / 4) + i % 2) * pitch + nb * 128 * ES;
-                        u32x4 y;
-                        if (E4M3) {
-                            const u32x2 z = *reinterpret_cast<const u32x2 *>(at);
-                            const uint32_t zw[2] = {z[0], z[1]};
-                            y = widen<F16, true>(zw);
-                        } else {
-                            y = *reinterpret_cast<const u32x4 *>(at);
-                        }
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) v[i][k] = !LATENT && v0 + nb * 128 + c * 8 >= Dv ? 0 : y[k];
+                // Values are read kVDepth - 1 turns ahead.  Successive turns' chunks are 8 apart,
+                // in the same place of theirs.
+                constexpr int STRIDE = E4M3 ? 8 : 4;               // tiles of 128 bytes
+                u32x4 v[kVDepth];
+                const auto tile_of_turn = [&](int u) { return u % (kTiles / STRIDE) * STRIDE + u / (kTiles / STRIDE); };
+                const auto read_v = [&](int u) {
+                    const int j = tile_of_turn(u), far = 32 * half * pitch + j / STRIDE * 128;
+                    if (!LATENT && 16 * j >= Dv) return;
+                    if (E4M3) {
+                        const u32x2 y = columns8(tile + (v_at ^ j % STRIDE * 16) + far);
+                        v[u % kVDepth] = u32x4{y[0], y[1], 0, 0};
+                    } else {
+                        const u32x2 y = columns16(tile + (v_at ^ j % STRIDE * 32) + far);
+                        const u32x2 z = columns16(tile + (v_at ^ j % STRIDE * 32) + far + 4 * pitch);
+                        v[u % kVDepth] = u32x4{y[0], y[1], z[0], z[1]};
                     }
+                };
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const uint32_t pick = j % 2 ? 0x07060302u : 0x05040100u;
-                        u32x4 bv;
+                for (int u = 0; u < kVDepth - 1; ++u) read_v(u);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) bv[k] = __builtin_amdgcn_perm(v[2 * k + 1][j / 2], v[2 * k][j / 2], pick);
-                        o[nb][j] = V::mfma(a[half], bv, o[nb][j]);
+                for (int u = 0; u < kTiles; ++u) {
+                    if (u + kVDepth - 1 < kTiles) read_v(u + kVDepth - 1);
+                    if (!LATENT && 16 * tile_of_turn(u) >= Dv) continue;
+                    u32x4 bv = v[u % kVDepth];
+                    if (E4M3) {
+                        const uint32_t w[2] = {bv[0], bv[1]};
+                        bv = widen<F16, true>(w);
                     }
+                    o[tile_of_turn(u)] = V::mfma(a, bv, o[tile_of_turn(u)]);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
+            mask = next_mask;
         }
         if (bad && p.err) atomicOr(p.err, bad);
         l += __shfl_xor(l, 16);
@@ -337,19 +339,17 @@ __global__ void __launch_bounds__(64 * WAVES, LATENT ? 2 : 1) kvx_attend_wide_ke
         if (twice) {
             // row 4 e + i, its rest 8 rows on: of lane + 32; see the narrow kernel
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b)
+            for (int j = 0; j < kTiles; ++j)
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float rest = __shfl_xor(o[b][j][i], 32);
-                        if (__builtin_fabsf(o[b][j][i]) < INFINITY) o[b][j][i] += rest;
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    const float rest = __shfl_xor(o[j][i], 32);
+                    if (__builtin_fabsf(o[j][i]) < INFINITY) o[j][i] += rest;
+                }
         }
 
         const int64_t head0 = (int64_t)part.r * p.pool.H * p.G + h * p.G + g0;
         const int64_t part0 = part.place < 0 ? 0 : part.place * p.part_heads + wave * 16;
-        if (vb == 0 && e == 0 && c < heads) {
+        if (e == 0 && c < heads) {
             if (part.place < 0) {
                 const float x = l > 0.f || l != l ? m + __builtin_amdgcn_logf(l) : -INFINITY;
                 if (p.lse) p.lse[head0 + c] = x * kLn2;
@@ -368,18 +368,11 @@ __global__ void __launch_bounds__(64 * WAVES, LATENT ? 2 : 1) kvx_attend_wide_ke
             char *dst = p.out.base + part.r * p.out.s_row + (int64_t)(h * p.G + g0 + row) * p.out.s_head;
             float *po = p.part_o + (part0 + row) * Dv;
 #pragma unroll
-            for (int nb = 0; nb < kBlocks; ++nb) {
-                const int d = v0 + nb * 128 + c * 8;
+            for (int j = 0; j < kTiles; ++j) {
+                const int d = j * 16 + c;
                 if (!LATENT && d >= Dv) continue;
-                const f32x4 *y = o[nb];
-                if (part.place < 0) {
-                    *reinterpret_cast<u32x4 *>(dst + 2 * d) =
-                        u32x4{V::pack(y[0][i] * f, y[1][i] * f), V::pack(y[2][i] * f, y[3][i] * f),
-                              V::pack(y[4][i] * f, y[5][i] * f), V::pack(y[6][i] * f, y[7][i] * f)};
-                } else {
-                    *reinterpret_cast<f32x4 *>(po + d) = f32x4{y[0][i], y[1][i], y[2][i], y[3][i]};
-                    *reinterpret_cast<f32x4 *>(po + d + 4) = f32x4{y[4][i], y[5][i], y[6][i], y[7][i]};
-                }
+                if (part.place < 0) reinterpret_cast<uint16_t *>(dst)[d] = V::pack(o[j][i] * f, 0.f);
+                else po[d] = o[j][i];
             }
         }
         // the loads behind the last tile, before LDS is used again
@@ -419,16 +412,15 @@ void plan_attend_wide(AttendParams &p) {
     p.span = 16 * p.waves_h;
     p.head_blocks = (tiles + p.waves_h - 1) / p.waves_h;
     p.step = tile_of(p.waves_h);
-    p.v_blocks = p.Dv > 256 ? 2 : 1;
     // as many as a compute unit's LDS and registers hold
     const int fit = 150 * 1024 / lds_of(p), waves = 8 / p.waves_h;
-    p.shares = 256 * (!latent(p) ? 1 : fit < waves ? fit : waves) / p.v_blocks;
+    p.shares = 256 * (!latent(p) ? 1 : fit < waves ? fit : waves);
 }
 
 int launch_attend_wide(const AttendParams &p, int32_t r0, int32_t n, hipStream_t stream) {
     const auto kernel = p.acc ? pick<true>(p) : pick<false>(p);
     const int64_t blocks = p.whole ? (int64_t)n * p.per : p.shares;
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.v_blocks == 2 ? (blocks + 7) / 8 * 16 : blocks)), dim3(64 * p.waves_h), lds_of(p), stream, p, r0, n);
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(64 * p.waves_h), lds_of(p), stream, p, r0, n);
     return hipGetLastError();
 }
 

@@ -72,7 +72,6 @@ struct AttendParams {
     // unit has its own workgroup (whole), else the shares of the steps; query
     // heads of a part and cache head
     int32_t waves_k, waves_h, span, head_blocks, per, step, whole, shares, part_heads;
-    int32_t v_blocks;            // workgroups that divide a unit's values among them
     // workspace
     int32_t *before;             // [record of the launch + 1]: steps before it
     float *lse2;                 // [record][q head]: m + log2 l, log2 units
