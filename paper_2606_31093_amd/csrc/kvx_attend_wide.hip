@@ -28,10 +28,12 @@ namespace {
 
 constexpr int kSteps = 18;               // 32 elements each: rows of up to 576
 constexpr int kTiles = 32;               // 16 values each: up to 512
-// Turns that reads of K and of V are ahead of their products, and one.  A query, its
-// outputs and these fill the 256 registers of one of two wavefronts on a SIMD: a
-// turn more of K took a wait for all loads per tile (170 us became 182).
-constexpr int kKDepth = 2, kVDepth = 4;
+// Turns that reads of K and of V are ahead of their products, and one.  With four
+// wavefronts and more two lie on a SIMD: a query, its outputs and these fill the
+// 256 registers of each, and a turn more of K took a wait for all loads per tile (170 us
+// became 182).  Fewer have twice the registers.
+constexpr int k_depth(int waves) { return waves >= 4 ? 2 : 6; }
+constexpr int v_depth(int waves) { return waves >= 4 ? 4 : 8; }
 
 // A row's permutation of its chunks, in each 8 of them.
 template <bool E4M3>
@@ -87,9 +89,10 @@ __device__ __forceinline__ void arrive() {
 // their first 512; else any head_dim up to 576, values up to 512, in rows of
 // their own if num_kv is 2.
 template <bool F16, bool E4M3, int WAVES, bool LATENT, bool ACC>
-__global__ void __launch_bounds__(64 * WAVES, LATENT ? 2 : 1) kvx_attend_wide_kernel(AttendParams p, int32_t r0, int32_t n) {
+__global__ void __launch_bounds__(64 * WAVES, LATENT && WAVES >= 4 ? 2 : 1) kvx_attend_wide_kernel(AttendParams p, int32_t r0, int32_t n) {
     typedef Half<F16> V;
     constexpr int ES = E4M3 ? 1 : 2, TILE = tile_of(WAVES), HALVES = TILE / 32;
+    constexpr int kKDepth = LATENT ? k_depth(WAVES) : 2, kVDepth = LATENT ? v_depth(WAVES) : 4;
     __shared__ int32_t before[kAttendGroup + 1];
     __shared__ __align__(16) int64_t row_off[WAVES][2][TILE];
     extern __shared__ __align__(256) char tiles[];       // [2][rows of K, rows of V if num_kv is 2]
