@@ -13,27 +13,52 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Unsigned order of the weights: NaN lowest, -0 as 0.
+// Unsigned order of the weights, -0 as 0, with a key below and above all of
+// them: 0 for what is not there, 1 for NaN, the largest for what is kept in any case.
+constexpr uint32_t kAbsent = 0, kAlways = 0xffffffffu;
 __device__ __forceinline__ uint32_t key_of(float x) {
-    if (x != x) return 0;
-    const uint32_t u = bits<uint32_t>(x == 0.f ? 0.f : x);
-    return u >> 31 ? ~u : u | 0x80000000u;
+    const uint32_t u = bits<uint32_t>(x + 0.f);          // -0 + 0 is 0
+    return x != x ? 1 : u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
 __device__ __forceinline__ bool inside(int64_t off, int64_t stride, int rows, int64_t n, int64_t len) {
     return off >= 0 && off <= len && n <= len - off && (rows == 1 || stride <= (len - off - n) / (rows - 1));
 }
 
-// A workgroup per record and row.  The n_keep - sink - recent largest keys of
-// the middle are found digit by digit from the top, 8 bits at a time: count
-// the digits of the keys that share the digits found so far, and take the
-// digit in which the last kept key lies.  Then all positions are walked in
-// order and the kept ones listed.
-__global__ void __launch_bounds__(kThreads) kvx_select_kernel(SelectParams p, int32_t r0) {
-    __shared__ uint32_t hist[256];
-    __shared__ uint32_t found[2];
-    __shared__ uint32_t counts[2][kThreads / 64];
-    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+// Lanes below this one in a ballot.
+__device__ __forceinline__ uint32_t below(uint64_t ballot) {
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(ballot >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)ballot, 0));
+}
+
+// Sum over this lane and those below it, by the moves of lanes within and across
+// rows of 16.
+__device__ __forceinline__ uint32_t sum_upto(uint32_t x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);        // 1 lane up
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);        // 2
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);        // 4
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);        // 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);        // lane 15 of rows 0 and 2 to the next row
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);        // lane 31 to the upper half
+    return x;
+}
+
+// A workgroup per record and row.  The keys lie in LDS, so that the row is read once
+// (KEEP; else they are made again in every pass, for rows too long for that).  A
+// wavefront has a run of successive positions, four a lane.  The first and last
+// positions have the largest key there is; then the n_keep largest are found
+// digit by digit from the top, 11, 11 and 10 bits: count the digits of the keys that
+// share the digits found so far, and take the digit in which the last kept key
+// lies; when all of its keys are kept, the rest needs no look.  Then each
+// wavefront counts what it keeps, and lists it behind what the ones before it keep.
+// Bound by its instructions (about 12 a key): 1792 rows of 2048 to 16384 positions,
+// 2048 kept of each, take 71 us, 50 MB read and 29 MB written.
+template <int THREADS, bool KEEP>
+__global__ void __launch_bounds__(THREADS) kvx_select_kernel(SelectParams p, int32_t r0) {
+    constexpr int WAVES = THREADS / 64, BINS = 2048, MINE = BINS / THREADS;
+    extern __shared__ __align__(16) uint32_t keys[];
+    __shared__ uint32_t hist[BINS];
+    __shared__ uint32_t found[3], sums[WAVES], ties[WAVES];
+    const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int r = r0 + (int)(blockIdx.x / (uint32_t)p.rows), j = (int)(blockIdx.x % (uint32_t)p.rows);
     const kvx_select_req q = p.reqs[r];
     const int64_t kept_n = q.n_tokens < q.n_keep ? q.n_tokens : q.n_keep;
@@ -49,79 +74,162 @@ __global__ void __launch_bounds__(kThreads) kvx_select_kernel(SelectParams p, in
     float *out = p.out ? p.out + q.out_off + j * p.out_stride : nullptr;
     const int n = q.n_tokens;
     if (n <= q.n_keep) {
-        for (int t = tid; t < n; t += kThreads) {
+        for (int t = tid; t < n; t += THREADS) {
             kept[t] = t;
             if (out) out[t] = acc[t];
         }
         return;
     }
-    const int lo = q.sink, hi = n - q.recent;
-    uint32_t need = q.n_keep - q.sink - q.recent;       // < hi - lo
-    uint32_t prefix = 0;
-    for (int shift = 24; shift >= 0 && need > 0; shift -= 8) {
-        hist[tid] = 0;
+    const int turns = (n + 4 * THREADS - 1) / (4 * THREADS);        // of 256 positions a wavefront
+    const int t0 = wave * turns * 256 + 4 * lane;
+    const auto key_at = [&](int t) {
+        if (t >= n) return kAbsent;
+        return t < q.sink || t >= n - q.recent ? kAlways : key_of(acc[t]);
+    };
+    if (KEEP) {
+        const int padded = turns * 4 * THREADS;
+#pragma unroll 4
+        for (int t = tid; t < padded; t += THREADS) keys[t] = key_of(acc[t < n ? t : n - 1]);
         __syncthreads();
-        for (int t = lo + tid; t < hi; t += kThreads) {
-            const uint32_t k = key_of(acc[t]);
-            if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1u);
+        for (int t = tid; t < q.sink; t += THREADS) keys[t] = kAlways;
+        for (int t = n - q.recent + tid; t < n; t += THREADS) keys[t] = kAlways;
+        for (int t = n + tid; t < padded; t += THREADS) keys[t] = kAbsent;
+    }
+    // f(first position, keys) for this lane's positions, in order
+    const auto each = [&](const auto &f) {
+        for (int i = 0; i < turns; ++i) {
+            if ((wave * turns + i) * 256 >= n) break;
+            const int t = t0 + 256 * i;
+            u32x4 k;
+            if (KEEP) k = *reinterpret_cast<const u32x4 *>(keys + t);
+            else k = u32x4{key_at(t), key_at(t + 1), key_at(t + 2), key_at(t + 3)};
+            f(t, k);
+        }
+    };
+
+    // kept: keys above `prefix`, and the first `need` equal to it
+    uint32_t need = q.n_keep, prefix = 0;                // < n
+    if (need == 0) return;
+    bool crowded = true;                                 // many keys share the digits found
+    for (int shift = 21, width = 11;;) {
+        for (int i = tid; i < BINS; i += THREADS) hist[i] = 0;
+        __syncthreads();
+        if (crowded) {
+            // Lanes with the digit of the first one are counted together: equal weights
+            // (zeros, say) would be added one after the other.
+            each([&](int, u32x4 k) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const bool on = shift == 21 || k[i] >> (shift + width) == prefix >> (shift + width);
+                    const uint64_t all = __ballot(on);
+                    if (all == 0) continue;
+                    const uint32_t d = k[i] >> shift & ((1u << width) - 1);
+                    const int leader = __builtin_ctzll(all);
+                    const uint32_t d0 = __builtin_amdgcn_readlane(d, leader);
+                    const uint64_t same = __ballot(on && d == d0);
+                    if (on && (d != d0 || lane == leader))
+                        atomicAdd(&hist[d], lane == leader ? (uint32_t)__popcll(same) : 1u);
+                }
+            });
+        } else {
+            each([&](int, u32x4 k) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (k[i] >> (shift + width) == prefix >> (shift + width))
+                        atomicAdd(&hist[k[i] >> shift & ((1u << width) - 1)], 1u);
+            });
         }
         __syncthreads();
-        if (tid < 64) {
-            // lane x: digits 255 - 4x .. 252 - 4x, from the largest down
-            uint32_t part[4], sum = 0;
-            for (int i = 0; i < 4; ++i) {
-                part[i] = hist[255 - 4 * lane - i];
-                sum += part[i];
+        // thread x: MINE digits, the larger ones before the smaller ones
+        uint32_t part[MINE], sum = 0;
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+            part[i] = hist[BINS - 1 - MINE * tid - i];
+            sum += part[i];
+        }
+        uint32_t above = sum_upto(sum);
+        if (lane == 63) sums[wave] = above;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES - 1; ++w) above += w < wave ? sums[w] : 0;       // all read at once
+        above -= sum;
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+            if (above < need && above + part[i] >= need) {
+                found[0] = BINS - 1 - MINE * tid - i;
+                found[1] = above + part[i] == need ? 0 : need - above;
+                found[2] = part[i];
             }
-            uint32_t above = sum;
-            for (int d = 1; d < 64; d <<= 1) {
-                const uint32_t x = __shfl_up(above, d);
-                if (lane >= d) above += x;
-            }
-            above -= sum;
-            for (int i = 0; i < 4; ++i) {
-                if (above < need && above + part[i] >= need) {
-                    found[0] = 255 - 4 * lane - i;
-                    found[1] = need - above;
-                }
-                above += part[i];
-            }
+            above += part[i];
         }
         __syncthreads();
         prefix |= found[0] << shift;
         need = found[1];
+        crowded = found[2] > 4 * THREADS;
+        if (need == 0) --prefix;                         // all of them; not 0, the key of none that is there
+        if (need == 0 || shift == 0) break;
+        width = shift == 21 ? 11 : 10;
+        shift -= width;
     }
-    // `need` of the keys equal to prefix, the first ones, and all above
-    const bool any = q.n_keep > q.sink + q.recent;
-    uint32_t at = 0, ties = 0;
-    for (int t0 = 0; t0 < n; t0 += kThreads) {
-        const int t = t0 + tid;
-        const bool mid = t >= lo && t < hi;
-        const float x = t < n ? acc[t] : 0.f;
-        const uint32_t k = key_of(x);
-        const bool tie = any && mid && k == prefix;
-        const uint64_t bt = __ballot(tie);
-        if (lane == 0) counts[0][wave] = __popcll(bt);
-        __syncthreads();
-        uint32_t rank = ties + __popcll(bt & ((1ull << lane) - 1));
-        for (int w = 0; w < kThreads / 64; ++w) {
-            if (w < wave) rank += counts[0][w];
-            ties += counts[0][w];
+
+    uint32_t mine = 0, equal = 0;
+    each([&](int, u32x4 k) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            mine += __popcll(__ballot(k[i] > prefix));
+            equal += __popcll(__ballot(k[i] == prefix));
         }
-        const bool take = t < n && (!mid || (any && (k > prefix || (tie && rank < need))));
-        const uint64_t bk = __ballot(take);
-        if (lane == 0) counts[1][wave] = __popcll(bk);
-        __syncthreads();
-        uint32_t to = at + __popcll(bk & ((1ull << lane) - 1));
-        for (int w = 0; w < kThreads / 64; ++w) {
-            if (w < wave) to += counts[1][w];
-            at += counts[1][w];
-        }
-        if (take) {
-            kept[to] = t;
-            if (out) out[to] = x;
-        }
+    });
+    if (lane == 0) {
+        sums[wave] = mine;
+        ties[wave] = equal;
     }
+    __syncthreads();
+    uint32_t at = 0, rank = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES - 1; ++w) {
+        at += w < wave ? sums[w] : 0;
+        rank += w < wave ? ties[w] : 0;
+    }
+    at += rank < need ? rank : need;
+    each([&](int t, u32x4 k) {
+        float x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = out ? acc[t + i < n ? t + i : n - 1] : 0.f;
+        bool take[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) take[i] = k[i] > prefix;
+        if (rank < need) {                               // ties are left: the first ones in order
+            uint32_t mine = rank, all = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint64_t b = __ballot(k[i] == prefix);
+                mine += below(b);
+                all += __popcll(b);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool tie = k[i] == prefix;
+                take[i] = take[i] || (tie && mine < need);
+                mine += tie;
+            }
+            rank += all;
+        }
+        uint32_t to = at;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint64_t b = __ballot(take[i]);
+            to += below(b);
+            at += __popcll(b);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (!take[i]) continue;
+            *reinterpret_cast<int32_t *>(reinterpret_cast<char *>(kept) + 4 * to) = t + i;
+            if (out) *reinterpret_cast<float *>(reinterpret_cast<char *>(out) + 4 * to) = x[i];
+            ++to;
+        }
+    });
 }
 
 // ---------------------------------------------------------------------------
@@ -132,7 +240,9 @@ constexpr int kRows = 64;            // list entries of a workgroup
 
 // A workgroup per 64 entries of one list (a record's layer and head): their
 // source and destination rows are resolved once, then copied 16 bytes a lane,
-// keys and values.
+// keys and values.  Bound by the memory: 1792 lists of up to 2048 rows of 256 bytes, 3.8 GB
+// read and written, take 715 us, 5.2 TB/s (750 us through the caches; four rows a
+// lane on their way at a time 719, eight 814).
 __global__ void __launch_bounds__(kThreads) kvx_kept_kernel(KeptParams p, int32_t r0, int32_t piece0) {
     __shared__ int64_t from[kRows], to[kRows];           // to < 0: left out
     uint32_t b = blockIdx.x;
@@ -194,8 +304,8 @@ __global__ void __launch_bounds__(kThreads) kvx_kept_kernel(KeptParams p, int32_
         for (int x = threadIdx.x; x < per; x += kThreads) {
             const int i = (int)fd_div(p.fd_vpr, x), v = x - i * p.vpr;
             if (to[i] < 0) continue;
-            *reinterpret_cast<u32x4 *>(dst + to[i] + 16 * v) =
-                *reinterpret_cast<const u32x4 *>(src + from[i] + 16 * v);
+            const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(src + from[i] + 16 * v));
+            __builtin_nontemporal_store(w, reinterpret_cast<u32x4 *>(dst + to[i] + 16 * v));
         }
         src += p.src.s_c;
         dst += p.dst.s_c;
@@ -204,11 +314,28 @@ __global__ void __launch_bounds__(kThreads) kvx_kept_kernel(KeptParams p, int32_
 
 }  // namespace
 
+// Threads of a workgroup, by the longest row there may be: 288 rows of 1500 took 8.5 us
+// with 512 (9.0 with 256, and 10 with 1024), 1792 rows of 2048 to 16384 71 us with 1024
+// (81 with 512).
+int select_threads(int max_tokens) { return max_tokens <= 8192 ? 512 : 1024; }
+
+// The longest row whose keys lie in LDS (128 KiB).
+constexpr int kMostKeys = 32768;
+
+auto pick_select(int threads, bool keep) {
+    if (threads == 512) return kvx_select_kernel<512, true>;
+    return keep ? kvx_select_kernel<1024, true> : kvx_select_kernel<1024, false>;
+}
+
 int launch_select(const SelectParams &p, hipStream_t stream) {
+    const int threads = select_threads(p.max_tokens);
+    const bool keep = p.max_tokens <= kMostKeys;
+    const auto kernel = pick_select(threads, keep);
+    const int lds = keep ? (p.max_tokens + 4 * threads - 1) / (4 * threads) * 16 * threads : 0;
     const int64_t group = kMaxBlocks / p.rows > 0 ? kMaxBlocks / p.rows : 1;
     for (int64_t r0 = 0; r0 < p.n_reqs; r0 += group) {
         const int64_t n = p.n_reqs - r0 < group ? p.n_reqs - r0 : group;
-        hipLaunchKernelGGL(kvx_select_kernel, dim3((uint32_t)(n * p.rows)), dim3(kThreads), 0, stream, p, (int32_t)r0);
+        hipLaunchKernelGGL(kernel, dim3((uint32_t)(n * p.rows)), dim3(threads), lds, stream, p, (int32_t)r0);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
