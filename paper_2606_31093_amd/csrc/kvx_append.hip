@@ -7,6 +7,12 @@
 // workgroup computes them once into LDS: the angle's whole turns are removed in
 // 64 bits (position * freq reaches 2^31 turns of which only the fraction
 // counts), cosine and sine are then taken in 32.
+//
+// Four prompts of 1024 to 8192 tokens into an e4m3 cache (28 query heads of 128 on
+// 4, 245 MB) take 64 us, MLA's 824 MB (16 query heads, rows of 576) 175 us, 4.7
+// TB/s; 64 new tokens 9.7 us, of which the data is under one.  Wavefronts hide
+// the loads' latency: with the rows of two items a thread asked for ahead of the
+// angles, or of four, fewer fit and the same cases took 84 and 261 us, or 95 and 292.
 
 #include "kvx_ops.h"
 #include "kvx_values.h"
