@@ -689,8 +689,9 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, factor: float = 1.0, s
       leaves the first frequency and divides the last by factor;
     - "ramp": pairs that turn more than ``fast`` times within the ``trained``
       length stay, those that turn less than ``slow`` times are divided by
-      factor, linearly in the pair's index between; the amplitude is
-      0.1 ln(factor) + 1."""
+      factor, linearly in the pair's index between (from the last index, or 0,
+      to the first whose pair turns at least `fast` and at most `slow` times);
+      the amplitude is 0.1 ln(factor) + 1."""
     if rot_dim < 2 or rot_dim % 2 or base <= 1 or factor < 1:
         raise ValueError("rot_dim must be even and >= 2, base above 1 and factor >= 1")
     j = np.arange(0, rot_dim, 2, dtype=np.float64)
@@ -708,8 +709,9 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, factor: float = 1.0, s
 
     def pair(turns):                   # the (real) pair index that turns so often within `trained`
         return rot_dim * math.log(trained / (2 * math.pi * turns)) / (2 * math.log(base))
-    lo, hi = max(0.0, math.floor(pair(fast))), min(rot_dim / 2 - 1.0, math.ceil(pair(slow)))
-    keep = 1 - np.clip((j / 2 - lo) / max(hi - lo, 1e-3), 0, 1)
+    # The ends are those of the turns, wherever the last pair is: it may turn more often than `slow`.
+    lo, hi = max(0, math.floor(pair(fast))), math.ceil(pair(slow))
+    keep = np.clip((hi - j / 2) / (hi - lo), 0, 1) if hi > lo else np.zeros_like(j)     # hi <= 0: none turns `slow` times
     return (freq * keep + freq / factor * (1 - keep)).astype(np.float32), 0.1 * math.log(factor) + 1
 
 

@@ -207,3 +207,32 @@ def test_rope_frequencies():
                dict(rot_dim=64, scaling="ramp"), dict(rot_dim=2, scaling="base"), dict(rot_dim=64, base=1.0)):
         with pytest.raises(ValueError):
             kvx.rope_frequencies(**kw)
+
+
+@pytest.mark.parametrize("rot_dim,base,trained,factor,fast,slow", [
+    (64, 1e4, 131072, 4.0, 32.0, 1.0),          # the slowest pair turns more than `slow` times
+    (64, 1e4, 65536, 4.0, 32.0, 1.0),
+    (128, 1e4, 131072, 8.0, 32.0, 1.0),
+    (128, 1e6, 4096, 8.0, 32.0, 1.0),           # both ends inside
+    (64, 100.0, 131072, 2.0, 32.0, 1.0),        # the ramp's end beyond every dimension
+    (64, 100.0, 1 << 24, 2.0, 32.0, 1.0),       # every pair turns more than `fast` times: none changes
+    (64, 1e4, 100, 4.0, 32.0, 1.0),             # none does: the ramp begins at the first pair
+    (64, 1e4, 6, 4.0, 32.0, 1.0),               # no pair turns `slow` times: all are divided
+    (2, 1e4, 1000, 4.0, 32.0, 1.0),
+])
+def test_rope_ramp_pair_by_pair(rot_dim, base, trained, factor, fast, slow):
+    """Pair j turns trained * base ** (-2j / rot_dim) / (2 pi) times.  The ramp falls from the last whole
+    pair index that turns `fast` times or more (or 0) to the first that turns `slow` times or fewer."""
+    def index(turns):
+        return rot_dim / 2 * math.log(trained / (2 * math.pi * turns), base)
+    lo, hi = max(0, math.floor(index(fast))), math.ceil(index(slow))
+    f, _ = kvx.rope_frequencies(rot_dim, base=base, factor=factor, scaling="ramp", trained=trained, fast=fast, slow=slow)
+    for j in range(rot_dim // 2):
+        plain = base ** (-2 * j / rot_dim)
+        turns = trained * plain / (2 * math.pi)
+        keep = 1.0 if j <= lo < hi else 0.0 if j >= hi else (hi - j) / (hi - lo)
+        if turns > fast:
+            assert keep == 1.0
+        if turns < slow and lo < hi and j > lo:
+            assert keep == 0.0
+        assert abs(float(f[j]) / plain - (keep + (1 - keep) / factor)) < 1e-6, (j, turns)
