@@ -543,8 +543,9 @@ int kvx_append(const kvx_pool *pool, int32_t layer, const float *scales,
 
 /* One query of a request (24 bytes): it attends over positions [start, end)
  * of its pages.  Malformed (its outputs are then not written): start < 0,
- * end < start, end - start > max_tokens, or, with accumulators, positions that
- * reach outside them. */
+ * end < start, end - start > max_tokens, or, with accumulators, a range that
+ * reaches outside them or, with num_heads above 1, is longer than acc_stride
+ * (heads would share accumulators). */
 typedef struct kvx_attend_req {
     int64_t pt_off;
     int64_t acc_off;             /* accumulator of cache head 0's position 0 */
@@ -587,7 +588,8 @@ int64_t kvx_attend_workspace(const kvx_pool *pool, int32_t n_reqs, int32_t q_hea
  * `sink`, the last `recent`, and of those between them the n_keep - sink -
  * recent of the largest accumulated weight.  All are kept if n_tokens <=
  * n_keep.  Malformed: a negative field, sink + recent > n_keep, n_tokens >
- * max_tokens, or a range outside its array. */
+ * max_tokens, a range outside its array, or, with rows above 1, more positions
+ * kept than kept_stride or acc_out_stride holds (rows would share entries). */
 typedef struct kvx_select_req {
     int64_t acc_off;             /* in acc: position 0 of row 0 */
     int64_t kept_off;            /* in kept: entry 0 of row 0 */

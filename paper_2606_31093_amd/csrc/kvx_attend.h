@@ -27,6 +27,8 @@ __device__ __forceinline__ float weight(float x, float m) { return m == -INFINIT
 __device__ __forceinline__ bool valid(const kvx_attend_req &q, const AttendParams &p) {
     if (q.start < 0 || q.end < q.start || q.end - q.start > p.max_tokens) return false;
     if (!p.acc) return true;
+    // one accumulator for each head and position: heads that shared one would add to it at the same time
+    if (p.pool.H > 1 && p.acc_stride < q.end - q.start) return false;
     // accumulators [acc_off + start, acc_off + (H - 1) * stride + end) lie inside
     return q.acc_off >= 0 && q.acc_off <= p.acc_len && q.end <= p.acc_len - q.acc_off &&
            (p.pool.H == 1 || p.acc_stride <= (p.acc_len - q.acc_off - q.end) / (p.pool.H - 1));

@@ -65,7 +65,8 @@ __global__ void __launch_bounds__(THREADS) kvx_select_kernel(SelectParams p, int
     if (q.n_tokens < 0 || q.n_keep < 0 || q.sink < 0 || q.recent < 0 || q.n_tokens > p.max_tokens ||
         (int64_t)q.sink + q.recent > q.n_keep || !inside(q.acc_off, p.acc_stride, p.rows, q.n_tokens, p.acc_len) ||
         !inside(q.kept_off, p.kept_stride, p.rows, kept_n, p.kept_len) ||
-        (p.out && !inside(q.out_off, p.out_stride, p.rows, kept_n, p.out_len))) {
+        (p.out && !inside(q.out_off, p.out_stride, p.rows, kept_n, p.out_len)) ||
+        (p.rows > 1 && (p.kept_stride < kept_n || (p.out && p.out_stride < kept_n)))) {      // rows would meet
         if (j == 0 && tid == 0 && p.err) atomicOr(p.err, KVX_DERR_BAD_REQ);
         return;
     }

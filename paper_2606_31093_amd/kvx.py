@@ -803,13 +803,23 @@ def attend_workspace(spec, n_reqs: int, q_heads: int, max_tokens: int, v_dim=Non
                        dtype=torch.uint8, device=device)
 
 
+def _stride(stride, name: str, of, rows: int) -> int:
+    """The stride of an optional array's rows, which only a single row or no array does without."""
+    if stride is None:
+        if of is not None and rows > 1:
+            raise ValueError(f"{name} is needed for {rows} rows")
+        return 0
+    return int(stride)
+
+
 def kvx_attend(q, out, pool, spec, layer, pt, reqs, max_tokens, workspace, scale=None, scales=None, lse=None,
-               acc=None, acc_stride=0, dev_err=None, stream=None) -> None:
+               acc=None, acc_stride=None, dev_err=None, stream=None) -> None:
     """Attention of one query per record over a layer's pages (see kvx_attend
     in include/kvx.h).  ``q`` [records, q heads, head_dim] and ``out``
     [records, q heads, v_dim]; ``scale`` defaults to head_dim ** -0.5;
     ``workspace`` from ``attend_workspace``; ``lse`` and ``acc`` optional float32
-    tensors."""
+    tensors, ``acc_stride`` the accumulators from one cache head to the next."""
+    acc_stride = _stride(acc_stride, "acc_stride", acc, spec.H)
     P = _pool_arg(spec, pool, "pool")
     table, n_pt = _table(pt, "pt")
     rec, n = _reqs_arg(reqs, ATTEND_REQ_DTYPE)
@@ -821,21 +831,22 @@ def kvx_attend(q, out, pool, spec, layer, pt, reqs, max_tokens, workspace, scale
         raise ValueError("workspace must be contiguous")
     _check(lib().kvx_attend(P, int(layer), _scales(scales, spec), _rows_arg(q, "q"), _rows_arg(out, "out"), lse_ptr,
                             float(spec.D ** -0.5 if scale is None else scale), table, n_pt, rec, n, int(max_tokens),
-                            acc_ptr, n_acc, int(acc_stride), workspace.data_ptr(), workspace.nbytes,
+                            acc_ptr, n_acc, acc_stride, workspace.data_ptr(), workspace.nbytes,
                             _err_word(dev_err), _stream(stream)))
 
 
-def kvx_select_kept(acc, acc_stride, rows, reqs, max_tokens, kept, kept_stride, acc_out=None, acc_out_stride=0,
+def kvx_select_kept(acc, acc_stride, rows, reqs, max_tokens, kept, kept_stride, acc_out=None, acc_out_stride=None,
                     dev_err=None, stream=None) -> None:
     """The positions that each of ``rows`` lists of every record keeps, by
     accumulated weight (see kvx_select_kept in include/kvx.h): ``acc`` and
     ``acc_out`` float32, ``kept`` an int32 tensor."""
+    acc_out_stride = _stride(acc_out_stride, "acc_out_stride", acc_out, rows)
     a, n_a = _floats(acc, "acc")
     o, n_o = _floats(acc_out, "acc_out")
     kp, n_k = _table(kept, "kept")
     rec, n = _reqs_arg(reqs, SELECT_REQ_DTYPE)
     _check(lib().kvx_select_kept(a, n_a, int(acc_stride), int(rows), rec, n, int(max_tokens), kp, n_k,
-                                 int(kept_stride), o, n_o, int(acc_out_stride), _err_word(dev_err), _stream(stream)))
+                                 int(kept_stride), o, n_o, acc_out_stride, _err_word(dev_err), _stream(stream)))
 
 
 def kvx_transfer_kept(src, src_spec, dst, dst_spec, src_pt, dst_pt, reqs, max_tokens, kept, kept_stride, sl=None,

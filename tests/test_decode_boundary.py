@@ -236,3 +236,14 @@ def test_rope_ramp_pair_by_pair(rot_dim, base, trained, factor, fast, slow):
         if turns < slow and lo < hi and j > lo:
             assert keep == 0.0
         assert abs(float(f[j]) / plain - (keep + (1 - keep) / factor)) < 1e-6, (j, turns)
+
+
+def test_binding_needs_strides():
+    """Without a stride several heads' accumulators, or rows' weights, would be the same ones."""
+    import torch
+    x, f = torch.zeros(1, 8, 64, dtype=torch.bfloat16), torch.zeros(100)
+    reqs = torch.zeros(24, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="acc_stride"):
+        kvx.kvx_attend(x, x, f, KV, 0, None, reqs, 1, f, acc=f)
+    with pytest.raises(ValueError, match="acc_out_stride"):
+        kvx.kvx_select_kept(f, 10, 2, reqs, 1, f, 10, f)

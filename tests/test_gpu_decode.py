@@ -631,3 +631,40 @@ def test_example_decodes_with_a_bounded_cache():
     total = s.acc.double().sum(dim=3)
     assert ((total - 90 * 4).abs() < 90 * 4 * 2.0 ** -16).all()        # 4 query heads a cache head, no eviction yet
     assert all(torch.isfinite(o).all() for o in outs)
+
+
+@pytest.mark.parametrize("D,G,end,stride,H,ok", [
+    (64, 4, 60, 0, 2, False), (64, 4, 60, 56, 2, False), (64, 4, 60, 57, 2, True), (64, 4, 60, 0, 1, True),
+    (64, 4, 3, 0, 2, True), (64, 1, 900, 896, 2, False), (64, 1, 900, 897, 2, True), (576, 4, 60, 56, 2, False)])
+def test_attend_heads_share_no_accumulators(D, G, end, stride, H, ok):
+    """Records from position 3 on whose heads' accumulators would meet are malformed."""
+    spec = PoolSpec(1, 1, H, D, T=16, N=60, e=2)
+    v, n = min(D, 512), H * 1000
+    pool = torch.zeros(spec.nbytes, dtype=torch.uint8, device="cuda")
+    q = torch.ones(1, H * G, D, dtype=torch.bfloat16, device="cuda")
+    out, acc, err = torch.full((1, H * G, v), 7.0, dtype=q.dtype, device="cuda"), torch.zeros(n, device="cuda"), error_word()
+    kvx.kvx_attend(q, out, pool, spec, 0, tensor(np.arange(60, dtype=np.int32)), kvx.device_attend_reqs([[0, 0, 3, end]]), 900,
+                   kvx.attend_workspace(spec, 1, H * G, 900, v, accumulate=True), acc=acc, acc_stride=stride, dev_err=err)
+    assert int(err.item()) == (0 if ok else kvx.DERR_BAD_REQ)
+    assert bool((out == (0.0 if ok else 7.0)).all())
+    want = torch.zeros(n, dtype=torch.float64)
+    for h in range(H if ok else 0):
+        want[h * stride + 3:h * stride + end] += G / max(1, end - 3)
+    # equal scores: each weight is G / positions, within the roundings of an exp2, a log2 and G sums
+    assert ((acc.double().cpu() - want).abs() <= want * 2.0 ** -18).all()
+
+
+@pytest.mark.parametrize("kept_stride,out_stride,rows,with_out,ok", [
+    (20, 20, 2, True, True), (19, 20, 2, True, False), (20, 19, 2, True, False), (0, 20, 2, True, False),
+    (20, 0, 2, True, False), (20, 0, 2, False, True), (0, 0, 1, True, True)])
+def test_select_rows_share_no_entries(kept_stride, out_stride, rows, with_out, ok):
+    acc = torch.rand(2 * 64, device="cuda")
+    kept = torch.full((64,), -1, dtype=torch.int32, device="cuda")
+    out, err = torch.full((64,), -1.0, device="cuda"), error_word()
+    kvx.kvx_select_kept(acc, 64, rows, kvx.device_select_reqs([[0, 0, 0, 50, 20, 2, 3], [0, 5, 5, 0, 20, 2, 3]]), 50, kept,
+                        kept_stride, out if with_out else None, out_stride, err)
+    assert int(err.item()) == (0 if ok else kvx.DERR_BAD_REQ)
+    for j in range(rows):
+        want = ref.select(acc[64 * j:64 * j + 50].cpu().numpy(), 20, 2, 3) if ok else [-1] * 20
+        assert kept[j * kept_stride:j * kept_stride + 20].tolist() == want
+    assert with_out or (out == -1).all()
