@@ -30,20 +30,24 @@ struct Dest {
     float scale;
 };
 
+// Eight elements: w as they are stored in the row, x their values.  Bit i of `turned`:
+// elements 2i and 2i + 1 have rotated, and only those are rounded again: the others keep
+// their bits, also those of a NaN.
 template <bool F16>
-__device__ __forceinline__ void store8(const Dest &to, int d, u32x4 w, const float *x, bool changed) {
+__device__ __forceinline__ void store8(const Dest &to, int d, u32x4 w, const float *x, uint32_t turned) {
     if (!to.row) return;
     if (to.e4m3) {
         float y[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = (changed ? x[i] : i % 2 ? Half<F16>::hi(w[i / 2]) : Half<F16>::lo(w[i / 2])) / to.scale;
+        for (int i = 0; i < 8; ++i) y[i] = x[i] / to.scale;
         const u32x2 o = {pack_e4m3(y[0], y[1], y[2], y[3]), pack_e4m3(y[4], y[5], y[6], y[7])};
         *reinterpret_cast<u32x2 *>(to.row + d) = o;
         return;
     }
-    if (changed) {
+    if (turned) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = Half<F16>::pack(x[2 * i], x[2 * i + 1]);
+        for (int i = 0; i < 4; ++i)
+            if (turned >> i & 1) w[i] = Half<F16>::pack(x[2 * i], x[2 * i + 1]);
     }
     *reinterpret_cast<u32x4 *>(to.row + 2 * d) = w;
 }
@@ -160,8 +164,8 @@ __global__ void __launch_bounds__(kThreads) kvx_append_kernel(AppendParams p, in
                         a[e] = x;
                         b[e] = y;
                     }
-                    store8<F16>(to, 8 * item, wa, a, true);
-                    store8<F16>(to, 8 * (item + hv), wb, b, true);
+                    store8<F16>(to, 8 * item, wa, a, 0xf);
+                    store8<F16>(to, 8 * (item + hv), wb, b, 0xf);
                     continue;
                 }
                 if ((int)item >= ov + hv) item += hv;      // behind the second half
@@ -171,8 +175,8 @@ __global__ void __launch_bounds__(kThreads) kvx_append_kernel(AppendParams p, in
             unpack8<F16>(w, x);
             const int d = 8 * item;
             // interleaved pairs of this eight that rotate: elements [o, o + 2 half)
-            const bool changed = half && p.interleaved && d + 8 > o && d < o + 2 * half;
-            if (changed) {
+            uint32_t turned = 0;
+            if (half && p.interleaved && d + 8 > o && d < o + 2 * half) {
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
                     if (d + e < o || d + e >= o + 2 * half) continue;
@@ -180,9 +184,10 @@ __global__ void __launch_bounds__(kThreads) kvx_append_kernel(AppendParams p, in
                     const float a = x[e], b = x[e + 1];
                     x[e] = a * z.x - b * z.y;
                     x[e + 1] = b * z.x + a * z.y;
+                    turned |= 1u << e / 2;
                 }
             }
-            store8<F16>(to, d, w, x, changed);
+            store8<F16>(to, d, w, x, turned);
         } else {
             // a rotated pair, or one element that stays
             const uint16_t *x = reinterpret_cast<const uint16_t *>(src);

@@ -668,3 +668,28 @@ def test_select_rows_share_no_entries(kept_stride, out_stride, rows, with_out, o
         want = ref.select(acc[64 * j:64 * j + 50].cpu().numpy(), 20, 2, 3) if ok else [-1] * 20
         assert kept[j * kept_stride:j * kept_stride + 20].tolist() == want
     assert with_out or (out == -1).all()
+
+
+@pytest.mark.parametrize("rot,off", [(6, 2), (8, 4), (2, 0), (14, 0), (12, 10)])
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_append_copies_what_does_not_rotate(kind, rot, off):
+    """Interleaved pairs that end inside an eight: the eight's other elements keep
+    their bits, signalling NaN, infinities, subnormals and negative zero among them."""
+    D = 32
+    odd = {"bf16": [0x7f81, 0xffa3, 0x7fc1, 0xff80, 0x0001, 0x8000, 0x807f, 0x7f7f],
+           "f16": [0x7c01, 0xfd55, 0x7e03, 0xfc00, 0x0001, 0x8000, 0x83ff, 0x7bff]}[kind]
+    bits = np.array(odd * (3 * D // 8), np.uint16).reshape(1, 3, D)
+    stay = np.ones(D, bool)
+    stay[off:off + rot] = False
+    bits[..., ~stay] = 0x3c00
+    x = rows_tensor(bits, kind)
+    spec = PoolSpec(1, 1, 1, D, T=4, N=1, e=2)
+    pool, q_out, err = torch.zeros(spec.nbytes, dtype=torch.uint8, device="cuda"), torch.zeros_like(x[:, :2]), error_word()
+    kvx.kvx_append(pool, spec, 0, x[:, 2:], None, tensor(np.zeros(1, np.int32)), kvx.device_append_reqs([[0, 0, 1, 9, 1]]), 1,
+                   q=x[:, :2], q_out=q_out, rope=kvx.Rope(tensor(np.full(rot // 2, 0.3, np.float32)), off, True), dev_err=err)
+    assert int(err.item()) == 0
+    got = q_out.view(torch.int16).cpu().numpy().view(np.uint16)
+    assert (got[..., stay] == bits[:, :2][..., stay]).all()
+    key = ref.canonical(pool.cpu().numpy(), spec)[0, 0, 0, 1, 0]
+    assert (key[stay] == bits[0, 2, stay]).all()
+    assert (got[..., ~stay] != bits[:, :2][..., ~stay]).all()
