@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(kThreads) kvx_append_kernel(AppendParams p, in
 }  // namespace
 
 int launch_append(const AppendParams &p0, hipStream_t stream) {
-    if (p0.n_reqs == 0 || p0.max_tokens == 0) return hipSuccess;
+    if (p0.n_reqs == 0) return hipSuccess;
     AppendParams p = p0;
     const int D = p.pool.D;
     // Eights where pairs never straddle one: halves that begin and end between
@@ -223,9 +223,10 @@ int launch_append(const AppendParams &p0, hipStream_t stream) {
     int64_t tokens = (4 * kThreads + per_token - 1) / per_token;
     if (p.half && tokens > kMaxHalf / p.half) tokens = kMaxHalf / p.half;
     if (tokens > 64) tokens = 64;
-    if (tokens > p.max_tokens) tokens = p.max_tokens;
+    if (tokens > p.max_tokens) tokens = p.max_tokens > 0 ? p.max_tokens : 1;
     p.tokens = (int32_t)tokens;
-    p.blocks = (int32_t)((p.max_tokens + tokens - 1) / tokens);
+    // with max_tokens 0 one too: it looks whether the record is malformed
+    p.blocks = p.max_tokens > 0 ? (int32_t)((p.max_tokens + tokens - 1) / tokens) : 1;
     p.fd_token = make_fastdiv(per_token);
     p.fd_items = make_fastdiv(p.items);
     p.fd_items_v = make_fastdiv(p.items_v);

@@ -344,9 +344,10 @@ int launch_select(const SelectParams &p, hipStream_t stream) {
 }
 
 int launch_kept(const KeptParams &p0, hipStream_t stream) {
-    if (p0.n_reqs == 0 || p0.max_tokens == 0) return hipSuccess;
+    if (p0.n_reqs == 0) return hipSuccess;
     KeptParams p = p0;
-    const int32_t pieces = (p.max_tokens + kRows - 1) / kRows;
+    // with max_tokens 0 one too: it looks whether the record is malformed
+    const int32_t pieces = p.max_tokens > 0 ? (p.max_tokens + kRows - 1) / kRows : 1;
     const int64_t lists = (int64_t)p.L * p.H;             // at most 2^20
     p.blocks = (int32_t)(kMaxBlocks / lists < pieces ? kMaxBlocks / lists : pieces);
     const int64_t per = p.blocks * lists, group = kMaxBlocks / per;

@@ -693,3 +693,21 @@ def test_append_copies_what_does_not_rotate(kind, rot, off):
     key = ref.canonical(pool.cpu().numpy(), spec)[0, 0, 0, 1, 0]
     assert (key[stay] == bits[0, 2, stay]).all()
     assert (got[..., ~stay] != bits[:, :2][..., ~stay]).all()
+
+
+def test_max_tokens_zero_finds_malformed_records():
+    """Records of any positions are malformed where max_tokens says there are none; empty ones are fine."""
+    spec = PoolSpec(1, 1, 1, 16, T=4, N=4, e=2)
+    pt = tensor(np.arange(4, dtype=np.int32))
+    k = torch.ones(8, 1, 16, dtype=torch.bfloat16, device="cuda")
+    kept = tensor(np.arange(8, dtype=np.int32))
+    for n, want in ((0, 0), (1, kvx.DERR_BAD_REQ), (-1, kvx.DERR_BAD_REQ)):
+        pool, dst = (torch.zeros(spec.nbytes, dtype=torch.uint8, device="cuda") for _ in range(2))
+        err = error_word()
+        kvx.kvx_append(pool, spec, 0, k, None, pt, kvx.device_append_reqs([[0, 0, 0, 0, 0], [0, 0, 0, 0, n]]), 0, dev_err=err)
+        assert int(err.item()) == want and (pool == 0).all()
+        pool.fill_(1)
+        err.zero_()
+        kvx.kvx_transfer_kept(pool, spec, dst, spec, pt, pt, kvx.device_reqs([[0, 0, 0, 0, 0, 0], [0, 0, 0, 0, 0, n]]), 0, kept,
+                              8, None, err)
+        assert int(err.item()) == want and (dst == 0).all()
