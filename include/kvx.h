@@ -484,7 +484,9 @@ int kvx_page_hashes(const void *payload, int64_t payload_positions, int32_t rec_
 /* Rows [num_rows][num_heads][head_dim] of 16-bit values: element (r, h, d) is
  * at base + r * row_stride + h * head_stride + d (elements).  base 16-byte
  * aligned, strides >= 0 and multiples of 8, head_dim a multiple of 8
- * (KVX_ERR_ALIGN).  Rows of a wider projection have its width as stride. */
+ * (KVX_ERR_ALIGN).  Rows of a wider projection have its width as stride.
+ * Inputs may have rows or heads in common (stride 0); outputs (q_out, out)
+ * whose rows share elements are refused with KVX_ERR_RANGE. */
 typedef struct kvx_rows {
     void *base;
     int64_t num_rows;

@@ -60,6 +60,23 @@ int check_rows(const kvx_rows *x, const char *name) {
     return KVX_OK;
 }
 
+// The first n rows of an output, which wavefronts write in any order, share no element:
+// |i * row_stride - j * head_stride| >= head_dim for all i < n and j < num_heads but 0, 0.
+int check_apart(const kvx_rows *x, int64_t n, const char *name) {
+    const int64_t a = x->row_stride, b = x->head_stride, D = x->head_dim, m = x->num_heads;
+    bool apart = (n <= 1 || a >= D) && (m <= 1 || b >= D);
+    if (apart && n > 1 && m > 1 && a < (m - 1) * b + D && b < (n - 1) * a + D) {
+        // neither do rows hold all heads nor heads all rows: the rows next to each head
+        for (int64_t j = 1; j < m && apart; ++j) {
+            const int64_t i = j * b / a;
+            apart = (i >= n || j * b - i * a >= D) && (i + 1 >= n || (i + 1) * a - j * b >= D);
+        }
+    }
+    return apart ? KVX_OK
+                 : fail(KVX_ERR_RANGE, "%s: rows of %lld elements share elements (row_stride %lld, head_stride %lld)", name,
+                        (long long)D, (long long)a, (long long)b);
+}
+
 int view_rows(const kvx_rows *x, const char *name, bool device_only, Known &known, Rows &out) {
     const int64_t bytes = rows_bytes(x);
     void *d = nullptr;
@@ -155,6 +172,7 @@ int kvx_append(const kvx_pool *pool, int32_t layer, const float *scales, const k
         if (q_out->num_heads != q->num_heads || q_out->head_dim != q->head_dim || q_out->dtype != q->dtype ||
             q_out->num_rows != q->num_rows)
             return fail(KVX_ERR_SHAPE, "q_out differs from q in heads, head_dim, dtype or rows");
+        if ((st = check_apart(q_out, q_out->num_rows, "q_out"))) return st;
     }
     if (((int64_t)(q ? q->num_heads : 0) + 2 * s.H) * s.D > (1 << 26))
         return fail(KVX_ERR_SHAPE, "a token's rows hold more than 2^26 elements");
@@ -237,6 +255,7 @@ int kvx_attend(const kvx_pool *pool, int32_t layer, const float *scales, const k
     if (q->num_rows < n_reqs || out->num_rows < n_reqs)
         return fail(KVX_ERR_RANGE, "q and out hold %lld and %lld rows for %d records", (long long)q->num_rows,
                     (long long)out->num_rows, n_reqs);
+    if ((st = check_apart(out, n_reqs, "out"))) return st;
     if ((st = check_records(reqs, n_reqs, max_tokens, dev_err))) return st;
     if ((st = check_table(pt, pt_len, "pt"))) return st;
     if ((reinterpret_cast<uintptr_t>(lse) & 3u) != 0) return fail(KVX_ERR_ALIGN, "lse is not 4-byte aligned");

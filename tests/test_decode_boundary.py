@@ -247,3 +247,21 @@ def test_binding_needs_strides():
         kvx.kvx_attend(x, x, f, KV, 0, None, reqs, 1, f, acc=f)
     with pytest.raises(ValueError, match="acc_out_stride"):
         kvx.kvx_select_kept(f, 10, 2, reqs, 1, f, 10, f)
+
+
+@pytest.mark.parametrize("n,heads,s_row,s_head,ok", [
+    (3, 8, 512, 64, True), (3, 8, 64, 192, True), (3, 8, 0, 64, False), (3, 8, 512, 0, False), (1, 8, 0, 64, True),
+    (1, 8, 0, 56, False), (3, 8, 504, 64, False), (3, 8, 56, 512, False), (3, 8, 64, 64, False), (3, 8, 64, 184, False),
+    (2, 2, 192, 128, True), (3, 3, 192, 128, True), (3, 4, 192, 128, False), (2, 4, 192, 128, True), (3, 2, 184, 128, False),
+])
+def test_output_rows_share_nothing(lib, n, heads, s_row, s_head, ok):
+    """Outputs whose rows meet would be written by several wavefronts; the rule against every pair of rows."""
+    at = [i * s_row + j * s_head for i in range(n) for j in range(heads)]
+    assert ok == all(abs(a - b) >= 64 for x, a in enumerate(at) for b in at[:x])
+    o = rows(heads, 64, n, s_row=s_row, s_head=s_head)
+    status = 0 if ok else -5
+    assert append(spec=PoolSpec(2, 2, 1, 64, T=16, N=8, e=2), q=rows(heads, 64, n), q_out=o, k=rows(1, 64, n),
+                  v=rows(1, 64, n)) == status
+    # without a workspace, so that what passes this check is refused by a later one
+    got = attend(spec=PoolSpec(2, 2, 1, 64, T=16, N=8, e=2), q=rows(heads, 64, n), out=o, n=n, ws=None)
+    assert got == (-1 if ok else -5)
