@@ -237,9 +237,9 @@ __global__ void __launch_bounds__(THREADS) kvx_select_kernel(SelectParams p, int
 // move
 // ---------------------------------------------------------------------------
 
-constexpr int kRows = 64;            // list entries of a workgroup
+constexpr int kRows = 64;            // list entries of a workgroup at most
 
-// A workgroup per 64 entries of one list (a record's layer and head): their
+// A workgroup per p.rows entries of one list (a record's layer and head): their
 // source and destination rows are resolved once, then copied 16 bytes a lane,
 // keys and values.  Bound by the memory: 1792 lists of up to 2048 rows of 256 bytes, 3.8 GB
 // read and written, take 715 us, 5.2 TB/s (750 us through the caches; four rows a
@@ -260,9 +260,9 @@ __global__ void __launch_bounds__(kThreads) kvx_kept_kernel(KeptParams p, int32_
         if (piece == 0 && h == 0 && l == 0 && threadIdx.x == 0 && p.err) atomicOr(p.err, KVX_DERR_BAD_REQ);
         return;
     }
-    const int first = piece * kRows;
+    const int first = piece * p.rows;
     if (first >= n) return;
-    const int rows = (int)(n - first < kRows ? n - first : kRows);
+    const int rows = (int)(n - first < p.rows ? n - first : p.rows);
     if ((int)threadIdx.x < rows) {
         const int i = first + threadIdx.x;
         const int64_t k = p.kept[q.buf_off + ((int64_t)l * p.H + h) * p.kept_stride + i];
@@ -346,8 +346,11 @@ int launch_select(const SelectParams &p, hipStream_t stream) {
 int launch_kept(const KeptParams &p0, hipStream_t stream) {
     if (p0.n_reqs == 0) return hipSuccess;
     KeptParams p = p0;
+    // the vectors of a workgroup's entries are counted in 31 bits: fewer entries where rows have 512 MiB and more
+    const int32_t fit = (INT32_MAX - kThreads) / p.vpr;
+    p.rows = fit < kRows ? fit : kRows;
     // with max_tokens 0 one too: it looks whether the record is malformed
-    const int32_t pieces = p.max_tokens > 0 ? (p.max_tokens + kRows - 1) / kRows : 1;
+    const int32_t pieces = p.max_tokens > 0 ? (p.max_tokens + p.rows - 1) / p.rows : 1;
     const int64_t lists = (int64_t)p.L * p.H;             // at most 2^20
     p.blocks = (int32_t)(kMaxBlocks / lists < pieces ? kMaxBlocks / lists : pieces);
     const int64_t per = p.blocks * lists, group = kMaxBlocks / per;

@@ -112,6 +112,7 @@ struct KeptParams {
     const int32_t *kept;
     int64_t kept_len, kept_stride;
     uint32_t *err;
+    int32_t rows;                // list entries of a workgroup
     int32_t blocks;              // workgroups per record, layer and head
     FastDiv fd_Ts, fd_Td, fd_vpr;
 };

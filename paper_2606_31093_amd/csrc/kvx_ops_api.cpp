@@ -371,7 +371,7 @@ int kvx_transfer_kept(const kvx_pool *src, const kvx_pool *dst, const kvx_slice 
     P.L = sl.num_layers;
     P.C = sl.num_kv;
     P.H = sl.num_heads;
-    P.vpr = ss.D * ss.e / 16;
+    P.vpr = (int32_t)((int64_t)ss.D * ss.e / 16);      // rows of up to 2 GiB
     P.kept_len = kept_len;
     P.kept_stride = kept_stride;
     P.err = v.err;

@@ -711,3 +711,21 @@ def test_max_tokens_zero_finds_malformed_records():
         kvx.kvx_transfer_kept(pool, spec, dst, spec, pt, pt, kvx.device_reqs([[0, 0, 0, 0, 0, 0], [0, 0, 0, 0, 0, n]]), 0, kept,
                               8, None, err)
         assert int(err.item()) == want and (dst == 0).all()
+
+
+def test_transfer_kept_rows_of_2_gib():
+    """The largest rows a pool may have, 16 of them in a list: 2^31 vectors of 16 bytes."""
+    spec = PoolSpec(1, 1, 1, 1 << 28, T=1, N=17, e=8)
+    src = torch.empty(spec.N, 1 << 28, dtype=torch.int64, device="cuda")
+    for i in range(spec.N):
+        torch.arange(i << 40, (i << 40) + (1 << 28), dtype=torch.int64, out=src[i])
+    dst = torch.full_like(src, -1)
+    rng = np.random.default_rng(1)
+    spt, dpt, kept = (rng.permutation(17)[:k].astype(np.int32) for k in (17, 16, 16))
+    err = error_word()
+    kvx.kvx_transfer_kept(src.view(torch.uint8).view(-1), spec, dst.view(torch.uint8).view(-1), spec, tensor(spt), tensor(dpt),
+                          kvx.device_reqs([[0, 0, 0, 0, 0, 16]]), 16, tensor(kept), 16, None, err)
+    assert int(err.item()) == 0
+    for i in range(16):
+        assert torch.equal(dst[int(dpt[i])], src[int(spt[kept[i]])]), i
+    assert (dst[next(p for p in range(17) if p not in dpt)] == -1).all()
