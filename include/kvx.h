@@ -571,8 +571,8 @@ typedef struct kvx_attend_req {
  * lse: n_reqs * q heads floats or NULL.
  * acc: acc_len floats or NULL; records must not share accumulators.
  * workspace: kvx_attend_workspace() bytes for the same arguments, or more,
- * 16-byte aligned, zero before its first use; each call leaves it ready for
- * the next one.  Calls that may run at the same time need one each. */
+ * 16-byte aligned; what it holds before a call does not matter.  Calls that
+ * may run at the same time need one each. */
 int kvx_attend(const kvx_pool *pool, int32_t layer, const float *scales,
                const kvx_rows *q, const kvx_rows *out, float *lse, float scale,
                const int32_t *pt, int64_t pt_len,

@@ -797,9 +797,9 @@ def attend_workspace_bytes(spec, n_reqs: int, q_heads: int, max_tokens: int, v_d
 def attend_workspace(spec, n_reqs: int, q_heads: int, max_tokens: int, v_dim=None, accumulate: bool = False,
                      device="cuda"):
     """A workspace for kvx_attend calls of up to ``n_reqs`` records and
-    ``max_tokens`` positions, as a zeroed device tensor."""
+    ``max_tokens`` positions: device memory, whatever it holds."""
     import torch
-    return torch.zeros(attend_workspace_bytes(spec, n_reqs, q_heads, max_tokens, v_dim, accumulate),
+    return torch.empty(attend_workspace_bytes(spec, n_reqs, q_heads, max_tokens, v_dim, accumulate),
                        dtype=torch.uint8, device=device)
 
 

@@ -729,3 +729,28 @@ def test_transfer_kept_rows_of_2_gib():
     for i in range(16):
         assert torch.equal(dst[int(dpt[i])], src[int(spt[kept[i]])]), i
     assert (dst[next(p for p in range(17) if p not in dpt)] == -1).all()
+
+
+@pytest.mark.parametrize("C,H,D,G,v", [(2, 2, 64, 8, 64), (1, 1, 576, 16, 512), (1, 1, 576, 128, 512)])
+@pytest.mark.parametrize("most", [100, 3000])
+def test_attend_workspace_may_hold_anything(most, C, H, D, G, v):
+    """Bytes that read as NaN, and as large offsets: the results are those of a zeroed workspace."""
+    spec = PoolSpec(1, C, H, D, T=16, N=400, e=2)
+    rng = np.random.default_rng(4)
+    pool, pt = tensor(make_pool(rng, spec, "bf16")), tensor(rng.permutation(400).astype(np.int32))
+    n, Hq = 5, H * G
+    q = rows_tensor(ref.bits(rng.standard_normal((n, Hq, D)).astype(np.float32), "bf16"), "bf16")
+    # one in full, an empty one, a malformed one, and two that share pages with the first
+    reqs = kvx.device_attend_reqs([[0, 0, 0, most], [0, 1 << 14, 7, 7], [0, 0, 5, 4], [9, 2 << 14, 3, most // 2],
+                                   [1, 3 << 14, 33, 34]])
+    res = []
+    for fill in (0, 0xff, 0x7f):
+        ws = kvx.attend_workspace(spec, n, Hq, most, v, accumulate=True)
+        ws.fill_(fill)
+        out, lse = torch.zeros(n, Hq, v, dtype=q.dtype, device="cuda"), torch.zeros(n, Hq, device="cuda")
+        acc, err = torch.zeros(1 << 16, device="cuda"), error_word()
+        kvx.kvx_attend(q, out, pool, spec, 0, pt, reqs, most, ws, lse=lse, acc=acc, acc_stride=1 << 12, dev_err=err)
+        assert int(err.item()) == kvx.DERR_BAD_REQ
+        res.append([x.cpu() for x in (out, lse, acc)])
+    assert all(torch.equal(a, b) for other in res[1:] for a, b in zip(res[0], other))
+    assert res[0][0][0].any() and torch.isfinite(res[0][2]).all()
