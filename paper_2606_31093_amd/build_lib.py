@@ -19,13 +19,15 @@ LIBRARY = os.path.join(PKG, "libkvx.so")
 # transfers of any size take the sweep launch (its launch choice starts as
 # KVX_CHOOSE_SWEEP), with at most 2048 copying workgroups, so that larger cases
 # take several launches, unplanned runs of any size are copied in order, and
-# unplanned rows of any size by teams of wavefronts.
+# unplanned rows of any size by teams of wavefronts.  The calls that compute with
+# a cache start a new launch after 1024 workgroups, kvx_attend after 16 records.
 # These are compile-time options: the product library has
 # no switch for them.
 TEST_LIBRARY = os.path.join(PKG, "libkvx_test.so")
 TEST_DEFINES = ("KVX_HASH_IDLE_POLLS=1", "KVX_SWEEP_MIN_BYTES=0", "KVX_SWEEP_MAX_BLOCKS=2048",
                 "KVX_LAUNCH_CHOICE_DEFAULT=1", "KVX_ORDER_PAGES=0", "KVX_ORDER_PIECES=0",
-                "KVX_ORDER_QUARTERS=0", "KVX_ORDER_TURNS=0", "KVX_TEAM_KIB=0", "KVX_TEAM_UNIT=0")
+                "KVX_ORDER_QUARTERS=0", "KVX_ORDER_TURNS=0", "KVX_TEAM_KIB=0", "KVX_TEAM_UNIT=0",
+                "KVX_OPS_MAX_BLOCKS=1024", "KVX_ATTEND_GROUP=16")
 SOURCES = [os.path.join(CSRC, f) for f in ("kvx_kernels.hip", "kvx_hash.hip", "kvx_append.hip", "kvx_attend.hip", "kvx_attend_wide.hip",
                                            "kvx_kept.hip", "kvx_api.cpp", "kvx_ops_api.cpp")]
 HEADERS = [os.path.join(INCLUDE, "kvx.h")] + [os.path.join(CSRC, f) for f in (

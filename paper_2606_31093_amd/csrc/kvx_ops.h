@@ -13,7 +13,10 @@ namespace kvx {
 
 // Most workgroups of one launch of these kernels: the work-items (up to 1024 a
 // workgroup) stay below 2^32.  More take several launches.
-constexpr int64_t kMaxBlocks = 1 << 21;
+#ifndef KVX_OPS_MAX_BLOCKS
+#define KVX_OPS_MAX_BLOCKS (1 << 21)
+#endif
+constexpr int64_t kMaxBlocks = KVX_OPS_MAX_BLOCKS;
 
 // One layer of a pool: row (c, page, slot, h) is at base + c * s_c + page *
 // s_p + slot * s_t + h * s_h (bytes).
@@ -83,7 +86,10 @@ struct AttendParams {
 };
 
 // Records of one launch of kvx_attend.
-constexpr int kAttendGroup = 1024;
+#ifndef KVX_ATTEND_GROUP
+#define KVX_ATTEND_GROUP 1024
+#endif
+constexpr int kAttendGroup = KVX_ATTEND_GROUP;
 
 // The division of a call's work, from the sizes alone.
 void plan_attend(AttendParams &p);

@@ -1,0 +1,168 @@
+"""Forms of the decode step's calls that sizes choose and test_gpu_decode.py does
+not reach: every kernel of kvx_attend with its split and join, several blocks of
+query heads, several launches (the test build starts a new one after 16 records
+or 1024 workgroups), pools in pinned host memory, and the second column that
+carries what rounding weights to bfloat16 leaves.  Bounds as there."""
+import numpy as np
+import pytest
+import torch
+
+import np_decode as ref
+import test_gpu_decode as base
+from paper_2606_31093_amd import build_lib, kvx
+from paper_2606_31093_amd.workloads import LAYOUTS, PoolSpec
+from test_gpu_decode import error_word, rows_tensor, rows_values, tensor
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [("bf16", "bf16"), ("f16", "f16"), ("bf16", "e4m3"), ("f16", "e4m3")]
+
+
+@pytest.fixture
+def several_launches(monkeypatch):
+    kvx.lib()    # the product library first: raises if it is missing
+    monkeypatch.setattr(kvx, "_LIB", kvx.load(build_lib.TEST_LIBRARY))
+
+
+@pytest.mark.parametrize("kind,cache", TYPES)
+@pytest.mark.parametrize("C,H,D,G,v", [
+    (1, 1, 576, 48, 512), (1, 1, 576, 64, 512),       # latents: four wavefronts
+    (1, 1, 576, 160, 512),                            # latents: two blocks of heads
+    (1, 1, 320, 40, 256), (2, 1, 512, 20, 0),         # wide rows of another shape: four wavefronts
+    (1, 2, 576, 5, 480), (2, 1, 272, 130, 0),         # and values that end inside, three blocks of heads
+    (2, 1, 128, 80, 0), (2, 1, 64, 130, 0)])          # narrow rows: two and three blocks
+def test_attend_blocks_of_heads(C, H, D, G, v, kind, cache):
+    spec = PoolSpec(2, C, H, D, T=16, N=60, e=1 if cache == "e4m3" else 2, layout=LAYOUTS[(D // 16 + G) % 4])
+    base.attend_case(D + G, spec, kind, cache, base.LENGTHS, G, v or None, acc=True, spoil=True)
+
+
+@pytest.mark.parametrize("kind,cache", TYPES)
+@pytest.mark.parametrize("layout", ["LPCTHD", "PLCHTD"])
+@pytest.mark.parametrize("C,H,D,G,v", [
+    (2, 2, 64, 4, 0), (2, 2, 80, 3, 0), (2, 4, 128, 7, 0), (2, 1, 128, 20, 0), (2, 1, 192, 3, 0), (2, 1, 256, 16, 0),
+    (1, 2, 128, 4, 96), (2, 1, 96, 70, 0), (1, 1, 576, 16, 512), (1, 1, 576, 30, 512), (1, 1, 576, 64, 512),
+    (1, 1, 576, 130, 512), (1, 1, 448, 6, 384), (2, 1, 320, 24, 0)])
+def test_attend_split_and_joined(C, H, D, G, v, layout, kind, cache):
+    """One long request and ragged ones, so that units are split among workgroups and joined."""
+    spec = PoolSpec(1, C, H, D, T=16, N=420, e=1 if cache == "e4m3" else 2, layout=layout)
+    base.attend_case(D + G, spec, kind, cache, [(0, 3001), (77, 2000), (0, 1), (5, 5), (900, 1300)], G, v or None, acc=True,
+                     spoil=True)
+
+
+@pytest.mark.parametrize("C,H,D,G,v", [(2, 2, 64, 4, 0), (1, 1, 576, 20, 512)])
+def test_attend_more_records_than_a_launch(C, H, D, G, v):
+    """1100 short records, with long ones on both sides of the 1024th."""
+    spec = PoolSpec(1, C, H, D, T=16, N=1600, e=2)
+    ranges = [(0, 1 + r % 5) for r in range(1100)]
+    ranges[3], ranges[1023], ranges[1024], ranges[1090] = (0, 1500), (3, 1700), (0, 1100), (31, 900)
+    base.attend_case(1, spec, "bf16", "bf16", ranges, G, v or None, acc=True)
+
+
+@pytest.mark.parametrize("C,H,D,G,v,most", [(2, 2, 64, 4, 0, 70), (2, 2, 64, 40, 0, 700), (1, 1, 576, 128, 512, 600),
+                                            (2, 1, 128, 4, 0, 3000)])
+def test_attend_in_several_launches(several_launches, C, H, D, G, v, most):
+    spec = PoolSpec(1, C, H, D, T=16, N=800, e=2)
+    rng = np.random.default_rng(most)
+    ranges = [(0, int(x)) for x in rng.integers(0, 150, 40)]
+    ranges[7], ranges[16], ranges[39] = (3, most), (0, most), (most - 1, most)
+    base.attend_case(2, spec, "bf16", "bf16", ranges, G, v or None, acc=True, spoil=True)
+
+
+def test_append_in_several_launches(several_launches):
+    spec = PoolSpec(1, 2, 2, 64, T=16, N=300, e=2)
+    lens = [200, 0, 1, 17] * 15
+    base.append_case(5, spec, "bf16", "bf16", lens, [r % 3 for r in range(60)], list(range(60)), 30, 64, 0, False, 1.0)
+
+
+def test_select_in_several_launches(several_launches):
+    n = 300
+    base.select_case(6, [20 + r % 50 for r in range(n)], [10 + r % 20 for r in range(n)], [1] * n, [2] * n, 5,
+                     base.WEIGHTS["heavy"])
+
+
+def test_transfer_kept_in_several_launches(several_launches):
+    S = PoolSpec(8, 1, 8, 16, T=16, N=80, e=1)           # 64 lists: 16 pieces of a record in a launch
+    base.kept_case(7, S, S, [1150], [1100], [0], [0])
+    S = PoolSpec(2, 2, 3, 16, T=16, N=700, e=2)          # 6 lists, 2 pieces, 120 records
+    base.kept_case(8, S, S, [60 + r % 9 for r in range(119)] + [200], [30 + r % 30 for r in range(119)] + [100], [0] * 120,
+                   [0] * 120)
+
+
+def split_case(D, G, C):
+    """Half of 256 positions of weight 1, the others of a weight that bfloat16 rounds down by nearly half a step, and
+    values that nearly cancel: what the rounding leaves decides the result."""
+    spec = PoolSpec(1, C, 1, D, T=16, N=16, e=2)
+    p = 0.5 + 0.9 * 2.0 ** -9
+    scale = float(np.float32(-np.log(p)))
+    light = np.arange(256) % 2 == 1
+    pool = np.zeros(spec.elems * 2, np.uint8)
+    c = ref.canonical(pool, spec)[0].transpose(0, 2, 1, 3, 4).reshape(256, C, D)       # a copy: positions, kv, elements
+    c[:, 0, D - 1] = np.where(light, 0xbf80, 0)                                       # a key of -1 or 0 in the last element
+    v_dim = D if C == 2 else 512
+    c[:, C - 1, :v_dim if C == 1 else D] = np.where(light, 0xbfff, 0x3f80)[:, None]   # -1.9921875 or 1
+    ref.canonical(pool, spec)[0] = c.reshape(16, 16, C, 1, D).transpose(0, 2, 1, 3, 4)
+    q = np.zeros((1, G, D), np.uint16)
+    q[..., D - 1] = 0x3f80
+    return spec, pool, q, scale, p, v_dim
+
+
+@pytest.mark.parametrize("D,G,C", [(64, 8, 2), (128, 1, 2), (256, 4, 2), (576, 8, 1), (320, 3, 2)])
+def test_attend_weights_in_two_columns(D, G, C):
+    """With 8 query heads or fewer on a cache head, weights are held to twice bfloat16's 8 bits: out is off by
+    u |out| + (u u + 2 ds + 2^-20) sum w |v|."""
+    spec, pool, qb, scale, p, v_dim = split_case(D, G, C)
+    pt, rows = np.arange(16, dtype=np.int32), [[0, 0, 0, 256]]
+    want, _, _, mag, dots = ref.attend(ref.values(qb, "bf16"), ref.values(ref.canonical(pool, spec), "bf16"), spec, 0, pt, rows,
+                                       scale, v_dim)
+    u = base.U["bf16"]
+    tol = u * np.abs(want) + (u * u + 2 * (D + 8) * 2.0 ** -24 * dots[0] + 2.0 ** -20) * mag
+    # the same with weights rounded once would be outside
+    once = (1 - 0.5 * 1.9921875) / (1 + p)
+    assert (np.abs(once - want) > 8 * tol).all()
+    q = rows_tensor(qb, "bf16")
+    out = torch.zeros(1, G, v_dim, dtype=q.dtype, device="cuda")
+    for most in (256, 1 << 20):          # a workgroup for the unit, and shares of its steps
+        out.fill_(7.0)
+        kvx.kvx_attend(q, out, tensor(pool), spec, 0, tensor(pt), kvx.device_attend_reqs(rows), most,
+                       kvx.attend_workspace(spec, 1, G, most, v_dim), scale=scale)
+        assert (np.abs(rows_values(out, "bf16") - want) <= tol).all()
+
+
+def test_pinned_host_memory():
+    """Kept rows from and to pools in pinned host memory, lists and records there too; attention reads such a pool;
+    append writes device memory only."""
+    S = PoolSpec(2, 2, 2, 64, T=16, N=8, e=2)
+    rng = np.random.default_rng(9)
+    src = torch.from_numpy(rng.integers(0, 256, S.nbytes).astype(np.uint8))
+    pt, kept = np.arange(8, dtype=np.int32)[::-1].copy(), np.sort(rng.choice(100, (4, 40), replace=True), axis=1).astype(np.int32)
+    reqs, err = kvx.device_reqs([[0, 0, 0, 0, 0, 40]], "cpu"), error_word()
+
+    def pinned(x):
+        t = torch.empty(x.shape, dtype=x.dtype, pin_memory=True)
+        t.copy_(x)
+        return t
+    lists, table, recs = pinned(torch.from_numpy(kept)), pinned(torch.from_numpy(pt)), pinned(reqs)
+    got = []
+    for s, d in ((src.cuda(), torch.zeros(S.nbytes, dtype=torch.uint8, device="cuda")),
+                 (src.cuda(), pinned(torch.zeros(S.nbytes, dtype=torch.uint8))),
+                 (pinned(src), torch.zeros(S.nbytes, dtype=torch.uint8, device="cuda"))):
+        kvx.kvx_transfer_kept(s, S, d, S, table, table, recs, 40, lists, 40, None, err)
+        torch.cuda.synchronize()
+        got.append(d.cpu().numpy())
+    want = np.zeros(S.nbytes, np.uint8)
+    a, b = ref.canonical(src.numpy(), S), ref.canonical(want, S)
+    for l in range(2):
+        for h in range(2):
+            for i, k in enumerate(kept[2 * l + h]):
+                b[l, pt[i // 16], :, i % 16, h] = a[l, pt[k // 16], :, k % 16, h]
+    assert int(err.item()) == 0 and all(np.array_equal(x, want) for x in got)
+
+    q = torch.randn(1, 4, 64, device="cuda").to(torch.bfloat16)
+    host = pinned(torch.randn(S.elems).to(torch.bfloat16).view(torch.uint8))
+    out = [torch.zeros_like(q) for _ in range(2)]
+    for o, pool in zip(out, (host, host.cuda())):
+        kvx.kvx_attend(q, o, pool, S, 1, table, kvx.device_attend_reqs([[0, 0, 0, 100]]), 100, kvx.attend_workspace(S, 1, 4, 100))
+    assert torch.equal(out[0], out[1]) and out[0].any()
+    k = torch.zeros(1, 2, 64, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(kvx.KvxError, match="pool base"):
+        kvx.kvx_append(host, S, 0, k, k, table, kvx.device_append_reqs([[0, 0, 0, 0, 1]]), 1)
