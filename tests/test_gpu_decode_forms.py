@@ -166,3 +166,50 @@ def test_pinned_host_memory():
     k = torch.zeros(1, 2, 64, dtype=torch.bfloat16, device="cuda")
     with pytest.raises(kvx.KvxError, match="pool base"):
         kvx.kvx_append(host, S, 0, k, k, table, kvx.device_append_reqs([[0, 0, 0, 0, 1]]), 1)
+
+
+def test_example_attends_over_what_it_keeps(monkeypatch):
+    """The example, past an eviction: the lists are those of the accumulated weights, fresh pages hold their rows, the
+    weights left are theirs, and the last step's outputs are attention over those rows and the newer ones."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import decode_step
+    calls, moves = {}, []
+
+    class Watched(decode_step.Sequences):
+        def evict(self, sink=4, recent=32):
+            full = [r for r in range(self.n) if self.length[r] == self.limit]
+            pool, acc, pages = self.pool.cpu().numpy().copy(), self.acc.cpu().numpy().copy(), [list(p) for p in self.pages]
+            freed = super().evict(sink, recent)
+            for r in full:
+                old, new = ref.canonical(pool, self.spec), ref.canonical(self.pool.cpu().numpy(), self.spec)
+                left = self.acc[r].cpu().numpy()
+                assert not set(pages[r]) & set(self.pages[r])
+                for layer in range(self.spec.L):
+                    for h in range(self.spec.H):
+                        kept = ref.select(acc[r, layer, h], self.budget, sink, recent)
+                        assert np.array_equal(left[layer, h, :self.budget], acc[r, layer, h, kept])
+                        assert (left[layer, h, self.budget:] == 0).all()
+                        for i, t in enumerate(kept):
+                            a, b = pages[r][t // 64], self.pages[r][i // 64]
+                            assert np.array_equal(new[layer, b, :, i % 64, h], old[layer, a, :, t % 64, h])
+                moves.append(r)
+            return freed
+
+    real = kvx.kvx_attend
+
+    def attend(q, out, pool, spec, layer, *rest, **kw):
+        real(q, out, pool, spec, layer, *rest, **kw)
+        calls[layer] = (q.clone(), out)
+    monkeypatch.setattr(decode_step, "Sequences", Watched)
+    monkeypatch.setattr(kvx, "kvx_attend", attend)
+    s, outs = decode_step.run(steps=105, n=2, budget=64, limit=100, verbose=False)
+    assert moves == [0, 1] and s.length == [69, 69] and sorted(calls) == [0, 1, 2]
+    values = ref.values(ref.canonical(s.pool.cpu().numpy(), s.spec), "bf16")
+    rows, u = [[r * s.slots_per, 0, 0, 69] for r in range(2)], base.U["bf16"]
+    for layer, (q, out) in calls.items():
+        want, _, _, mag, dots = ref.attend(rows_values(q, "bf16"), values, s.spec, layer, s.pt.cpu().numpy(), rows, 128 ** -0.5,
+                                           128)
+        tol = u * np.abs(want) + (u + 2 * ((128 + 8) * 2.0 ** -24 * dots)[:, None, None] + 2.0 ** -20) * mag
+        assert (np.abs(rows_values(out, "bf16") - want) <= tol).all()
