@@ -564,8 +564,10 @@ typedef struct kvx_attend_req {
  *   acc[acc_off + h * acc_stride + t] += sum over the G heads of p(t) / l.
  * Positions that cannot be resolved take no part.  A query without positions
  * (or with every score -inf) gives zeros, lse -inf and adds nothing.
- * p is rounded to the rows' type for its product with V; sums, maxima, l and
- * the accumulated weights are not.
+ * For its product with V, p is held in two values of the rows' type, to 1/16 of
+ * the type's rounding or better; with more than 64 query heads a cache head
+ * and head_dim above 256 in one.  Sums, maxima, l and the accumulated weights
+ * are held in 32 bits.
  * q heads: a multiple of num_heads, at most 1024.  head_dim <= 576,
  * v_dim <= 512, v_dim <= head_dim, and v_dim == head_dim when num_kv is 2.
  * lse: n_reqs * q heads floats or NULL.

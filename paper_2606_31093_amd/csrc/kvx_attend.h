@@ -176,6 +176,24 @@ struct Walk {
     }
 };
 
+// Eight weights in two parts of the rows' type, for a product each, so that their
+// rounding is kRest of one to the type: rounded once, weights cost an output as
+// much as its own rounding does.  `a` is less than w by about kRest of it: the rest
+// is then not zero where w is not, and an infinite value times it is not NaN.  (In
+// half, whose smallest value is 2^-24, that holds from 2^-21 on, 2^-28 of the
+// largest weight.)
+template <bool F16>
+constexpr float kRest = F16 ? 1.0f / 16 : 1.0f / 256;
+template <bool F16>
+__device__ __forceinline__ void split(const float *w, u32x4 &a, u32x4 &rest) {
+    typedef Half<F16> V;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        a[i] = V::pack(w[2 * i] * (1 - kRest<F16>), w[2 * i + 1] * (1 - kRest<F16>));
+        rest[i] = V::pack(w[2 * i] - V::lo(a[i]), w[2 * i + 1] - V::hi(a[i]));
+    }
+}
+
 template <bool F16, bool E4M3>
 __device__ __forceinline__ u32x4 widen(const uint32_t *w) {
     if (E4M3)

@@ -24,6 +24,8 @@
 // - those 8 weights are exactly one lane's part of the A operand of the second
 //   product if its k index 8q + i stands for position 4q + i (i < 4) or
 //   16 + 4q + i - 4.  Any order of k serves when B has the same one;
+//   The weights are two parts in the rows' type, a product each; the second product
+//   took no time with up to 16 query heads a cache head, and 1 to 3% with 32 and 64;
 // - B = V: lane (c, q) loads W consecutive elements from c * W on of those 8
 //   positions (16 lanes read a row as one run) and transposes its own 8 x W
 //   block with byte permutes; product j then makes the outputs c * W + j.
@@ -145,17 +147,12 @@ __device__ __forceinline__ void attend_part(const AttendParams &p, const Part pa
     // Step j of the first product contracts 8 elements from dim(j) on: any order
     // serves that gives a lane 16 consecutive bytes of its row.
     const auto dim = [&](int j) { return E4M3 ? j / 2 * 64 + quad * 16 + j % 2 * 8 : j * 32 + quad * 8; };
-    // Heads of this wave.  Where they are 8 or fewer, bfloat16 weights take two
-    // columns: head c in column c, and in column c + 8 what its rounding to 8 bits
-    // left, whose product is added at the end.  (Half keeps 11 bits.)
-    const int heads = p.G - g0 < 16 ? p.G - g0 : 16;
-    const bool twice = !F16 && heads <= 8;
+    const int heads = p.G - g0 < 16 ? p.G - g0 : 16;     // of this wave
     // queries
     u32x4 qv[DC];
     {
-        const int g = twice ? c & 7 : c;
-        const bool on = g < heads;
-        const char *src = p.q.base + r * p.q.s_row + (int64_t)(h * p.G + (on ? g0 + g : 0)) * p.q.s_head;
+        const bool on = c < heads;
+        const char *src = p.q.base + r * p.q.s_row + (int64_t)(h * p.G + (on ? g0 + c : 0)) * p.q.s_head;
 #pragma unroll
         for (int j = 0; j < DC; ++j) {
             const int d = dim(j);
@@ -255,12 +252,8 @@ __device__ __forceinline__ void attend_part(const AttendParams &p, const Part pa
                     w[i] = exp2_fast(x[8 * u + i] - from);
                     l += w[i];
                 }
-                u32x4 a = {V::pack(w[0], w[1]), V::pack(w[2], w[3]), V::pack(w[4], w[5]), V::pack(w[6], w[7])};
-                if (twice && c >= 8) {
-                    // what the rounding of head c - 8 left
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) a[i] = V::pack(w[2 * i] - V::lo(a[i]), w[2 * i + 1] - V::hi(a[i]));
-                }
+                u32x4 a, rest;
+                split<F16>(w, a, rest);
 
                 // values: 8 positions x W elements a lane, transposed
 #pragma unroll
@@ -286,6 +279,7 @@ __device__ __forceinline__ void attend_part(const AttendParams &p, const Part pa
                         for (int i = 0; i < 4; ++i)
                             bv[i] = __builtin_amdgcn_perm(v[2 * i + 1][j / 2], v[2 * i][j / 2], pick);
                         o[nb * W + j] = V::mfma(a, bv, o[nb * W + j]);
+                        o[nb * W + j] = V::mfma(rest, bv, o[nb * W + j]);
                     }
                 }
             }
@@ -304,16 +298,6 @@ __device__ __forceinline__ void attend_part(const AttendParams &p, const Part pa
     if (bad && p.err) atomicOr(p.err, bad);
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    if (twice) {
-#pragma unroll
-        for (int j = 0; j < NB * W; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                // an infinite value times a rest of 0 is NaN, and no part of the sum
-                const float rest = __shfl_xor(o[j][i], 32);
-                if (__builtin_fabsf(o[j][i]) < INFINITY) o[j][i] += rest;
-            }
-    }
 
     // Join the waves of the same heads: each scales to the common maximum, then
     // they add up in LDS, one after the other.

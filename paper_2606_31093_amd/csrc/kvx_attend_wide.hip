@@ -21,6 +21,12 @@
 // different banks.  The loads write LDS in order of lanes; the permutation is in
 // the addresses they read.
 //
+// Weights are in two parts, as in the narrow kernel, but for eight wavefronts: there
+// they are rounded once to the rows' type.  With 128 heads the second product took 185 us
+// instead of 167, for an error against 64 bits of 0.0017 instead of 0.0019 of the
+// outputs, 0.0017 of it their own rounding to bfloat16.  With 64 heads it took none (142 for
+// 150), with 16 and 32 1 to 3%, in half 11% with 16.
+//
 // 16 requests of 4096 to 32768 positions, 128 heads on rows of 576 (409 MB, 98
 // GFLOP): 174 us, 561 TFLOP/s, bound by the reads of LDS that feed the products.
 
@@ -95,6 +101,7 @@ template <bool F16, bool E4M3, int WAVES, bool LATENT, bool ACC>
 __global__ void __launch_bounds__(64 * WAVES, LATENT && WAVES >= 4 ? 2 : 1) kvx_attend_wide_kernel(AttendParams p, int32_t r0, int32_t n) {
     typedef Half<F16> V;
     constexpr int ES = E4M3 ? 1 : 2, TILE = tile_of(WAVES), HALVES = TILE / 32;
+    constexpr bool PARTS = WAVES < 8;                    // weights in two parts
     constexpr int kKDepth = LATENT ? k_depth(WAVES) : 2, kVDepth = LATENT ? v_depth(WAVES) : 4;
     __shared__ int32_t before[kAttendGroup + 1];
     __shared__ __align__(16) int64_t row_off[WAVES][2][TILE];
@@ -163,15 +170,11 @@ __global__ void __launch_bounds__(64 * WAVES, LATENT && WAVES >= 4 ? 2 : 1) kvx_
             }
         };
 
-        // Heads of this wave.  Where they are 8 or fewer, bfloat16 weights take two
-        // columns: head c in column c, and in column c + 8 what its rounding left.
-        const int heads = p.G - g0 < 16 ? (p.G > g0 ? p.G - g0 : 0) : 16;
-        const bool twice = !F16 && heads <= 8;
+        const int heads = p.G - g0 < 16 ? (p.G > g0 ? p.G - g0 : 0) : 16;     // of this wave
         u32x4 qv[kSteps];
         {
-            const int g = twice ? c & 7 : c;
-            const bool on = g < heads;
-            const char *src = p.q.base + part.r * p.q.s_row + (int64_t)(h * p.G + (on ? g0 + g : 0)) * p.q.s_head;
+            const bool on = c < heads;
+            const char *src = p.q.base + part.r * p.q.s_row + (int64_t)(h * p.G + (on ? g0 + c : 0)) * p.q.s_head;
 #pragma unroll
             for (int j = 0; j < kSteps; ++j) {
                 const int d = E4M3 ? (j / 2 * 4 + e) * 16 + j % 2 * 8 : j * 32 + e * 8;
@@ -300,11 +303,8 @@ __global__ void __launch_bounds__(64 * WAVES, LATENT && WAVES >= 4 ? 2 : 1) kvx_
                     w[i] = exp2_fast(x[i / 4][i % 4] - from);
                     l += w[i];
                 }
-                u32x4 a = {V::pack(w[0], w[1]), V::pack(w[2], w[3]), V::pack(w[4], w[5]), V::pack(w[6], w[7])};
-                if (twice && lc >= 8) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) a[i] = V::pack(w[2 * i] - V::lo(a[i]), w[2 * i + 1] - V::hi(a[i]));
-                }
+                u32x4 a = {V::pack(w[0], w[1]), V::pack(w[2], w[3]), V::pack(w[4], w[5]), V::pack(w[6], w[7])}, rest;
+                if (PARTS) split<F16>(w, a, rest);
                 // Values are read kVDepth - 1 turns ahead.  Successive turns' chunks are 8 apart,
                 // in the same place of theirs.
                 constexpr int STRIDE = E4M3 ? 8 : 4;               // tiles of 128 bytes
@@ -334,6 +334,7 @@ __global__ void __launch_bounds__(64 * WAVES, LATENT && WAVES >= 4 ? 2 : 1) kvx_
                         bv = widen<F16, true>(w);
                     }
                     o[tile_of_turn(u)] = V::mfma(a, bv, o[tile_of_turn(u)]);
+                    if (PARTS) o[tile_of_turn(u)] = V::mfma(rest, bv, o[tile_of_turn(u)]);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -342,16 +343,6 @@ __global__ void __launch_bounds__(64 * WAVES, LATENT && WAVES >= 4 ? 2 : 1) kvx_
         if (bad && p.err) atomicOr(p.err, bad);
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);
-        if (twice) {
-            // row 4 e + i, its rest 8 rows on: of lane + 32; see the narrow kernel
-#pragma unroll
-            for (int j = 0; j < kTiles; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float rest = __shfl_xor(o[j][i], 32);
-                    if (__builtin_fabsf(o[j][i]) < INFINITY) o[j][i] += rest;
-                }
-        }
 
         const int64_t head0 = (int64_t)part.r * p.pool.H * p.G + h * p.G + g0;
         const int64_t part0 = part.place < 0 ? 0 : part.place * p.part_heads + wave * 16;

@@ -1,8 +1,9 @@
 """Forms of the decode step's calls that sizes choose and test_gpu_decode.py does
 not reach: every kernel of kvx_attend with its split and join, several blocks of
 query heads, several launches (the test build starts a new one after 16 records
-or 1024 workgroups), pools in pinned host memory, and the second column that
-carries what rounding weights to bfloat16 leaves.  Bounds as there."""
+or 1024 workgroups), pools in pinned host memory, and the two parts that hold
+the weights for their product with the values.  Bounds as there, and tighter
+where a test says so."""
 import numpy as np
 import pytest
 import torch
@@ -107,9 +108,9 @@ def split_case(D, G, C):
 
 
 @pytest.mark.parametrize("D,G,C", [(64, 8, 2), (128, 1, 2), (256, 4, 2), (576, 8, 1), (320, 3, 2)])
-def test_attend_weights_in_two_columns(D, G, C):
-    """With 8 query heads or fewer on a cache head, weights are held to twice bfloat16's 8 bits: out is off by
-    u |out| + (u u + 2 ds + 2^-20) sum w |v|."""
+def test_attend_weights_to_twice_bfloat16(D, G, C):
+    """Weights are held to twice bfloat16's 8 bits: out is off by u |out| + (u u + 2 ds + 2^-20) sum w |v|.
+    (Few heads, where other columns of the products are free.)"""
     spec, pool, qb, scale, p, v_dim = split_case(D, G, C)
     pt, rows = np.arange(16, dtype=np.int32), [[0, 0, 0, 256]]
     want, _, _, mag, dots = ref.attend(ref.values(qb, "bf16"), ref.values(ref.canonical(pool, spec), "bf16"), spec, 0, pt, rows,
@@ -213,3 +214,76 @@ def test_example_attends_over_what_it_keeps(monkeypatch):
                                            128)
         tol = u * np.abs(want) + (u + 2 * ((128 + 8) * 2.0 ** -24 * dots)[:, None, None] + 2.0 ** -20) * mag
         assert (np.abs(rows_values(out, "bf16") - want) <= tol).all()
+
+
+FORMS = [(64, 3, 2), (128, 16, 2), (192, 9, 2), (256, 20, 2), (128, 70, 2), (320, 12, 2), (512, 40, 2), (576, 8, 1), (576, 16, 1),
+         (576, 30, 1), (576, 64, 1)]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("D,G,C", FORMS)
+def test_attend_weights_in_two_parts(D, G, C, kind):
+    """Any number of query heads up to 64 on rows of more than 256 elements: the weights' rounding is that of their second
+    part, 1/256 and 2^-8 of a weight in bfloat16, 1/16 and 2^-11 in half (a rounding of the first part is in the second)."""
+    spec, pool, qb, scale, p, v_dim = split_case(D, G, C)
+    u = base.U[kind]
+    if kind == "f16":
+        p = 0.5 + 0.9 * 2.0 ** -12
+        scale = float(np.float32(-np.log(p)))
+        swap = {0xbf80: 0xbc00, 0x3f80: 0x3c00, 0xbfff: 0xbfff, 0: 0}        # -1, 1, the largest value below 2 (negative), 0
+        words = pool.view(np.uint16)
+        words[:] = np.vectorize(swap.get)(words)
+        qb = np.vectorize(swap.get)(qb).astype(np.uint16)
+    pt, rows = np.arange(16, dtype=np.int32), [[0, 0, 0, 256]]
+    want, _, _, mag, dots = ref.attend(ref.values(qb, kind), ref.values(ref.canonical(pool, spec), kind), spec, 0, pt, rows,
+                                       scale, v_dim)
+    part = 2.0 ** -7 if kind == "bf16" else 1 / 16 + 2.0 ** -11
+    # a score is one product (the others are zeros): 2^-23 of it
+    tol = u * np.abs(want) + (part * u + 2.0 ** -22 * dots[0] + 2.0 ** -20) * mag + (2.0 ** -24 if kind == "f16" else 0)
+    last = 1.9921875 if kind == "bf16" else 2 - 2.0 ** -10
+    assert (np.abs((1 - 0.5 * last) / (1 + p) - want) > 4 * tol).all()       # weights rounded once would be outside
+    q = rows_tensor(qb, kind)
+    out = torch.zeros(1, G, v_dim, dtype=q.dtype, device="cuda")
+    for most in (256, 1 << 20):
+        out.fill_(7.0)
+        kvx.kvx_attend(q, out, tensor(pool), spec, 0, tensor(pt), kvx.device_attend_reqs(rows), most,
+                       kvx.attend_workspace(spec, 1, G, most, v_dim), scale=scale)
+        assert (np.abs(rows_values(out, kind) - want) <= tol).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("D,G,C", FORMS + [(576, 128, 1)])
+def test_attend_infinite_values(D, G, C, kind):
+    """An infinite value reaches its element as such, also at weights that the rows' type holds exactly (1, 1/2, 2^-9), which
+    leave no rest.  With one kv component it is a key's element too, which times the query's 0 makes the score NaN."""
+    spec = PoolSpec(1, C, 1, D, T=16, N=16, e=2)
+    one, inf = (0x3f80, 0x7f80) if kind == "bf16" else (0x3c00, 0x7c00)
+    pool = np.zeros(spec.elems * 2, np.uint8)
+    c = ref.canonical(pool, spec)                                 # l, page, kv, slot, h, d
+    v_dim = D if C == 2 else 512
+    c[0, :, C - 1, :, 0, :v_dim if C == 1 else D] = one
+    if C == 2:
+        c[0, :, 0] = 0
+    # keys: score -k in log2 units by the last element's value times the scale
+    key = {"bf16": [0, 0xbf80, 0xc110], "f16": [0, 0xbc00, 0xc880]}[kind]       # 0, -1, -9
+    where = {0: (0, 3), 1: (7, 100), 2: (9, 201)}                 # which key: element, position
+    c[0, :, 0, :, 0, D - 1] = key[2]
+    for k, (d, t) in where.items():
+        c[0, t // 16, 0, t % 16, 0, D - 1] = key[k]
+        c[0, t // 16, C - 1, t % 16, 0, d] = inf
+    qb = np.zeros((1, G, D), np.uint16)
+    qb[..., D - 1] = one
+    q = rows_tensor(qb, kind)
+    out = torch.zeros(1, G, v_dim, dtype=q.dtype, device="cuda")
+    for most in (256, 1 << 20):
+        out.fill_(7.0)
+        kvx.kvx_attend(q, out, tensor(pool), spec, 0, tensor(np.arange(16, dtype=np.int32)),
+                       kvx.device_attend_reqs([[0, 0, 0, 256]]), most, kvx.attend_workspace(spec, 1, G, most, v_dim),
+                       scale=float(np.log(2)))
+        got = rows_values(out, kind)[0]
+        if C == 1:
+            assert np.isnan(got).all()
+            continue
+        assert np.isposinf(got[:, [0, 7, 9]]).all()
+        rest = np.delete(got, [0, 7, 9], axis=1)
+        assert (np.abs(rest - 1) <= base.U[kind] + 2.0 ** -16).all()
