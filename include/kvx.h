@@ -464,13 +464,17 @@ int kvx_page_hashes(const void *payload, int64_t payload_positions, int32_t rec_
  * of elem_bytes 2).  Other widths are refused with KVX_ERR_SHAPE.
  * Ownership, synchrony and errors are as above: nothing is allocated, all
  * inputs must be device memory or mapped pinned host memory and all outputs,
- * accumulators and workspaces device memory.  A page of the pool that cannot
+ * accumulators and workspaces device memory (but kvx_transfer_kept's pools,
+ * either of which may be pinned host memory).  A page of the pool that cannot
  * be resolved raises KVX_DERR_SRC_PAGE (read) or KVX_DERR_DST_PAGE (written),
  * a table index out of range KVX_DERR_PT_RANGE, a malformed record
  * KVX_DERR_BAD_REQ; only the elements involved are left out.
  * max_tokens (each call), 0 .. KVX_MAX_TOKENS: no record holds more positions
  * than this; read on the host to shape the launch.  A record that holds more
- * is malformed.
+ * is malformed.  kvx_append and kvx_transfer_kept launch for max_tokens of
+ * every record, and kvx_attend's workspace holds them where it accumulates:
+ * there a call for the few long records and one for the many short ones is
+ * better than one for all.
  * Sums, maxima and angles are held in 32 bits or more.
  * ------------------------------------------------------------------------- */
 

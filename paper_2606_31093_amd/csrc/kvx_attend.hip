@@ -6,7 +6,7 @@
 // units of log2, so that a weight is one exp2.
 //
 // Division of the work.  A unit is a record and some of its cache heads (or a
-// part of their query heads); it takes a step for every 32 to 128 positions.
+// part of their query heads); it takes a step for every 32 to 256 positions.
 // Only the device knows the lengths, so the workgroups, as many as the device
 // holds at a time, add them up and take equal shares of all steps in order.  A
 // unit that lies in one share is finished there; the parts of the others are
@@ -34,9 +34,10 @@
 //
 // Bound by the cache's bytes, and where they are few by the second launch:
 // bfloat16, 8 cache heads of 128, 32 query heads: one request of 32768
-// positions (134 MB) takes 37 us, 29 of them the first launch; 32 requests of
-// 1024 to 8192 with accumulated weights (663 MB) 153 us; e4m3, 4 cache heads,
-// 28 query heads, 16 requests of 2048 to 16384 (177 MB) 48 us.
+// positions (134 MB) takes 36 us, 29 of them the first launch; 32 requests of
+// 1024 to 8192 with accumulated weights (663 MB) 152 us, 136 of them the first
+// launch; e4m3, 4 cache heads, 28 query heads, 16 requests of 2048 to 16384
+// (177 MB) 47 us, 42 of them the first launch.
 
 #include "kvx_attend.h"
 
@@ -547,7 +548,10 @@ __global__ void __launch_bounds__(1024) kvx_attend_finish_kernel(AttendParams p,
 }
 
 // Tiles of 64 positions where rows are short (128 bytes and less): a wavefront
-// then has 16 KiB on their way as with rows of 256.
+// then has 16 KiB on their way as with rows of 256, and units of up to 512 positions and
+// more are whole (below).  8 cache heads of 64, 32 query heads: 64 requests of 300 took 15.5
+// us, with tiles of 32 27.9 (e4m3: 11.3, 24.6); 32 of 4096 55.3 and 54.5 (37.8, 37.4); one
+// of 16384 24.2 and 20.5 (20.3, 19.3).
 int tile_of(int D) { return D <= 64 ? 2 : 1; }
 
 template <bool F16, bool E4M3, bool ACC>
@@ -574,10 +578,14 @@ int padded(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : D <= 192 ? 192 : 256;
 // workgroup's registers leave room for 2 or 1 on each).
 int resident(int D) { return D <= 128 ? 512 : 256; }
 
-// A unit of up to this many steps is not worth a second launch: 8 steps take
-// less time than the launch does.
+// A unit of up to this many steps is not worth a second launch.  8 cache heads of 128, 32
+// query heads, 1 and 64 requests of 200 positions (8 steps): 13 and 18 us whole, 20 and 29
+// split; of 300 (11): 17 and 25, 20 and 37; of 450 (16): 22 and 34, 20 and 40; of 700 (23):
+// 30 and 48, 20 and 50.  Latents, 128 heads, one of 500 (9 steps): 50 whole, 33 split.
 constexpr int kWholeSteps = 8;
-// Fewer steps than this are not worth a share.
+// Fewer steps than this are not worth a share.  The same heads, 1, 8 and 64 requests of 4000,
+// 4000 and 1000 positions: 21.7, 35.4 and 56.7 us; with shares of 1 step and more 17.7, 38.2 and
+// 56.5, of 16 and more 40.0, 46.0 and 53.7.
 constexpr int kLeastShare = 4;
 
 }  // namespace

@@ -2,11 +2,14 @@
 // whose rows have more than 256 elements (gfx950): MLA latents, with up to
 // 128 query heads on one cache head.
 //
-// With 128 heads every byte of the cache takes part in 240 operations: the
-// matrix units are as busy as the memory.  A wavefront takes 16 heads, so that
+// With 128 heads every byte of the cache takes part in 240 operations: at the
+// rates of a large product and a large copy the matrix units would be as busy as
+// the memory.  A wavefront takes 16 heads, so that
 // a workgroup of eight reads a tile of positions once for 128; the tile lies
 // in LDS, where the loads put it themselves (no register holds a row on its
-// way), while the one before it is in use.  With c = lane % 16, e = lane / 16
+// way).  They are asked for when the tile before is taken up, and have arrived
+// before its first values are read: the compiler waits for all loads there, as
+// the reads of LDS that transpose might meet what the loads write.  With c = lane % 16, e = lane / 16
 // the products are those of the narrow kernel, of 16 x 16:
 // - scores: A = 16 rows of K, B = the queries (registers, all their elements);
 //   row r of product b < 2 is position 8 (r / 4) + 4 b + r % 4, so that lane (c, e)
@@ -28,7 +31,12 @@
 // 150), with 16 and 32 1 to 3%, in half 11% with 16.
 //
 // 16 requests of 4096 to 32768 positions, 128 heads on rows of 576 (409 MB, 98
-// GFLOP): 174 us, 561 TFLOP/s, bound by the reads of LDS that feed the products.
+// GFLOP): 170 us, 573 TFLOP/s.  Bound by waits:
+// the matrix units are busy for a quarter of the first launch, a wavefront waits for 43%
+// of its cycles (for the next tile's loads, and for rows of K, which are read one
+// product ahead).  Registers for more reads ahead there are none: the kernels of four and
+// eight wavefronts, and of one with 16-bit rows, spill 29 to 52 a lane, none of them
+// among the products.
 
 #include "kvx_attend.h"
 
@@ -37,7 +45,8 @@ namespace {
 
 constexpr int kSteps = 18;               // 32 elements each: rows of up to 576
 constexpr int kTiles = 32;               // 16 values each: up to 512
-// Turns that reads of K and of V are ahead of their products, and one.  With four
+// Turns that reads of K and of V are ahead of their products, and one (a read of K is
+// asked for behind the product before, so that of depth 2 is one product ahead).  With four
 // wavefronts and more two lie on a SIMD: a query, its outputs and these fill the
 // 256 registers of each, and a turn more of K took a wait for all loads per tile (170 us
 // became 182).  Fewer have twice the registers.
@@ -409,7 +418,11 @@ void plan_attend_wide(AttendParams &p) {
     p.span = 16 * p.waves_h;
     p.head_blocks = (tiles + p.waves_h - 1) / p.waves_h;
     p.step = tile_of(p.waves_h);
-    // as many as a compute unit's LDS and registers hold
+    // For latents as many as a compute unit's LDS and registers hold, else one: for workgroups of
+    // one wavefront more would serve (rows of 320, 4 heads, 110 MB: 164 us, 95 with all that fit;
+    // of 448, 16 heads, 155 MB: 194, 127), for those of four not (rows of 320, 40 heads: 136, 162).
+    // Latents by the kernel for any rows take 405 us instead of 130 with 16 heads, 560 instead
+    // of 167 with 128.
     const int fit = 150 * 1024 / lds_of(p), waves = 8 / p.waves_h;
     p.shares = 256 * (!latent(p) ? 1 : fit < waves ? fit : waves);
 }

@@ -42,16 +42,18 @@ __device__ __forceinline__ uint32_t sum_upto(uint32_t x) {
     return x;
 }
 
-// A workgroup per record and row.  The keys lie in LDS, so that the row is read once
-// (KEEP; else they are made again in every pass, for rows too long for that).  A
+// A workgroup per record and row.  The keys lie in LDS, so that the choice reads the row
+// once (KEEP; else they are made again in every pass, for rows too long for that).  A
 // wavefront has a run of successive positions, four a lane.  The first and last
 // positions have the largest key there is; then the n_keep largest are found
 // digit by digit from the top, 11, 11 and 10 bits: count the digits of the keys that
 // share the digits found so far, and take the digit in which the last kept key
 // lies; when all of its keys are kept, the rest needs no look.  Then each
-// wavefront counts what it keeps, and lists it behind what the ones before it keep.
-// Bound by its instructions (about 12 a key): 1792 rows of 2048 to 16384 positions,
-// 2048 kept of each, take 71 us, 50 MB read and 29 MB written.
+// wavefront counts what it keeps, and lists it behind what the ones before it keep;
+// for acc_out it reads the row's weights a second time there, those not kept too.
+// Bound by its instructions and the waits between its up to six passes: 1792 rows of 2048
+// to 16384 positions (77 MB of weights, 29 MB of lists), 2048 kept of each, take 72 us;
+// 77 vector instructions a key are half of that, and 125 MB are read from memory.
 template <int THREADS, bool KEEP>
 __global__ void __launch_bounds__(THREADS) kvx_select_kernel(SelectParams p, int32_t r0) {
     constexpr int WAVES = THREADS / 64, BINS = 2048, MINE = BINS / THREADS;
@@ -243,7 +245,8 @@ constexpr int kRows = 64;            // list entries of a workgroup at most
 // source and destination rows are resolved once, then copied 16 bytes a lane,
 // keys and values.  Bound by the memory: 1792 lists of up to 2048 rows of 256 bytes, 3.8 GB
 // read and written, take 715 us, 5.2 TB/s (750 us through the caches; four rows a
-// lane on their way at a time 719, eight 814).
+// lane on their way at a time 719, eight 814).  Copies in the order of pages reach
+// 6.1 to 6.4 TB/s.
 __global__ void __launch_bounds__(kThreads) kvx_kept_kernel(KeptParams p, int32_t r0, int32_t piece0) {
     __shared__ int64_t from[kRows], to[kRows];           // to < 0: left out
     uint32_t b = blockIdx.x;
@@ -317,10 +320,12 @@ __global__ void __launch_bounds__(kThreads) kvx_kept_kernel(KeptParams p, int32_
 
 // Threads of a workgroup, by the longest row there may be: 288 rows of 1500 took 8.5 us
 // with 512 (9.0 with 256, and 10 with 1024), 1792 rows of 2048 to 16384 71 us with 1024
-// (81 with 512).
+// (81 with 512).  1792 and 288 rows of 8192 took 46.8 and 16.1 us with 512, 51.5 and 16.3
+// with 1024; of 12000 80.7 and 21.7 with 512, 67.2 and 21.0 with 1024.
 int select_threads(int max_tokens) { return max_tokens <= 8192 ? 512 : 1024; }
 
-// The longest row whose keys lie in LDS (128 KiB).
+// The longest row whose keys lie in LDS (128 KiB): 1792 and 288 rows of 32768 took 234 and
+// 60 us, and without it 370 and 97.  1792 of 40000 take 428 us, of 131072 1308.
 constexpr int kMostKeys = 32768;
 
 auto pick_select(int threads, bool keep) {
@@ -346,7 +351,9 @@ int launch_select(const SelectParams &p, hipStream_t stream) {
 int launch_kept(const KeptParams &p0, hipStream_t stream) {
     if (p0.n_reqs == 0) return hipSuccess;
     KeptParams p = p0;
-    // the vectors of a workgroup's entries are counted in 31 bits: fewer entries where rows have 512 MiB and more
+    // The longest list shapes the launch: one of 8192 entries among 256 of one (4 layers of 8
+    // heads) takes 1035 us, alone it takes 50.  The vectors of a workgroup's entries are counted
+    // in 31 bits: fewer entries where rows have 512 MiB and more.
     const int32_t fit = (INT32_MAX - kThreads) / p.vpr;
     p.rows = fit < kRows ? fit : kRows;
     // with max_tokens 0 one too: it looks whether the record is malformed
