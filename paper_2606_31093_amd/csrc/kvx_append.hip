@@ -30,11 +30,9 @@ struct Dest {
     float scale;
 };
 
-// Eight elements: w as they are stored in the row, x their values.  Bit i of `turned`:
-// elements 2i and 2i + 1 have rotated, and only those are rounded again: the others keep
-// their bits, also those of a NaN.
+// Eight elements: w as they lie in the row, x their values, which have changed or not.
 template <bool F16>
-__device__ __forceinline__ void store8(const Dest &to, int d, u32x4 w, const float *x, uint32_t turned) {
+__device__ __forceinline__ void store8(const Dest &to, int d, u32x4 w, const float *x, bool changed) {
     if (!to.row) return;
     if (to.e4m3) {
         float y[8];
@@ -44,10 +42,9 @@ __device__ __forceinline__ void store8(const Dest &to, int d, u32x4 w, const flo
         *reinterpret_cast<u32x2 *>(to.row + d) = o;
         return;
     }
-    if (turned) {
+    if (changed) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (turned >> i & 1) w[i] = Half<F16>::pack(x[2 * i], x[2 * i + 1]);
+        for (int i = 0; i < 4; ++i) w[i] = Half<F16>::pack(x[2 * i], x[2 * i + 1]);
     }
     *reinterpret_cast<u32x4 *>(to.row + 2 * d) = w;
 }
@@ -164,19 +161,19 @@ __global__ void __launch_bounds__(kThreads) kvx_append_kernel(AppendParams p, in
                         a[e] = x;
                         b[e] = y;
                     }
-                    store8<F16>(to, 8 * item, wa, a, 0xf);
-                    store8<F16>(to, 8 * (item + hv), wb, b, 0xf);
+                    store8<F16>(to, 8 * item, wa, a, true);
+                    store8<F16>(to, 8 * (item + hv), wb, b, true);
                     continue;
                 }
                 if ((int)item >= ov + hv) item += hv;      // behind the second half
             }
-            const u32x4 w = *reinterpret_cast<const u32x4 *>(src + 16 * item);
+            u32x4 w = *reinterpret_cast<const u32x4 *>(src + 16 * item);
             float x[8];
             unpack8<F16>(w, x);
             const int d = 8 * item;
             // interleaved pairs of this eight that rotate: elements [o, o + 2 half)
-            uint32_t turned = 0;
-            if (half && p.interleaved && d + 8 > o && d < o + 2 * half) {
+            bool changed = half && p.interleaved && d + 8 > o && d < o + 2 * half;
+            if (changed) {
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
                     if (d + e < o || d + e >= o + 2 * half) continue;
@@ -184,10 +181,16 @@ __global__ void __launch_bounds__(kThreads) kvx_append_kernel(AppendParams p, in
                     const float a = x[e], b = x[e + 1];
                     x[e] = a * z.x - b * z.y;
                     x[e + 1] = b * z.x + a * z.y;
-                    turned |= 1u << e / 2;
+                }
+                if (p.partly) {
+                    // the eight's other elements keep their bits, also those of a NaN
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2)
+                        if (d + e >= o && d + e < o + 2 * half) w[e / 2] = Half<F16>::pack(x[e], x[e + 1]);
+                    changed = false;
                 }
             }
-            store8<F16>(to, d, w, x, turned);
+            store8<F16>(to, d, w, x, changed);
         } else {
             // a rotated pair, or one element that stays
             const uint16_t *x = reinterpret_cast<const uint16_t *>(src);
@@ -218,6 +221,7 @@ int launch_append(const AppendParams &p0, hipStream_t stream) {
     // tokens, 32 query heads of 80 on 8 (216 MB), take 35 to 38 us in eights and 149 to 154
     // element by element, 40 to 46 and 158 to 165 into an e4m3 cache.
     p.vec = p.half == 0 || (p.interleaved ? p.rot_off % 2 == 0 : p.rot_off % 8 == 0 && p.half % 8 == 0);
+    p.partly = p.interleaved && (p.rot_off % 8 || 2 * p.half % 8);
     p.items = p.vec ? D / 8 - (p.interleaved ? 0 : p.half / 8) : D - p.half;
     p.items_v = p.vec ? D / 8 : D;
     const int per_token = (p.q.heads + p.k.heads) * p.items + p.v.heads * p.items_v;

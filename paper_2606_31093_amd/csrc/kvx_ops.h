@@ -51,6 +51,7 @@ struct AppendParams {
     // launch
     int32_t tokens, blocks;      // tokens per workgroup, workgroups per record
     int32_t vec;                 // 8 elements at a time, else a pair
+    int32_t partly;              // interleaved pairs end inside an eight
     int32_t items, items_v;      // of a q or k head, of a v head
     FastDiv fd_items, fd_items_v, fd_token, fd_half;
 };
