@@ -31,7 +31,7 @@
 // 150), with 16 and 32 1 to 3%, in half 11% with 16.
 //
 // 16 requests of 4096 to 32768 positions, 128 heads on rows of 576 (409 MB, 98
-// GFLOP): 170 us, 573 TFLOP/s.  Bound by waits:
+// GFLOP): 171 us, 571 TFLOP/s.  Bound by waits:
 // the matrix units are busy for a quarter of the first launch, a wavefront waits for 43%
 // of its cycles (for the next tile's loads, and for rows of K, which are read one
 // product ahead).  Registers for more reads ahead there are none: the kernels of four and

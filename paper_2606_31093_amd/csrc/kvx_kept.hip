@@ -53,7 +53,7 @@ __device__ __forceinline__ uint32_t sum_upto(uint32_t x) {
 // for acc_out it reads the row's weights a second time there, those not kept too.
 // Bound by its instructions and the waits between its up to six passes: 1792 rows of 2048
 // to 16384 positions (77 MB of weights, 29 MB of lists), 2048 kept of each, take 72 us;
-// 77 vector instructions a key are half of that, and 125 MB are read from memory.
+// 77 vector instructions a key are half of that, and 114 to 125 MB are read from memory.
 template <int THREADS, bool KEEP>
 __global__ void __launch_bounds__(THREADS) kvx_select_kernel(SelectParams p, int32_t r0) {
     constexpr int WAVES = THREADS / 64, BINS = 2048, MINE = BINS / THREADS;
