@@ -636,6 +636,149 @@ int kvx_transfer_kept(const kvx_pool *src, const kvx_pool *dst, const kvx_slice 
                       const int32_t *kept, int64_t kept_len, int64_t kept_stride,
                       uint32_t *dev_err, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Several tokens of a request: the calls above for chunks of prompts and for
+ * drafted tokens that are verified together.
+ *   kvx_append_normed  puts new tokens into their slots as kvx_append does, with
+ *                      queries and keys normed, and positions of their own;
+ *   kvx_attend_prompt  attends with the last queries of a request's positions;
+ *   kvx_attend_tree    attends with drafted tokens that form a tree;
+ *   kvx_keep_path      moves the accepted drafts' rows to the front.
+ * All rules of the calls above hold.  max_queries, 0 .. KVX_MAX_TOKENS: no
+ * record holds more queries than this; it shapes launch and workspace as
+ * max_tokens does, and a record that holds more is malformed.
+ * ------------------------------------------------------------------------- */
+
+/* Most drafted tokens of a record. */
+#define KVX_MAX_DRAFTS 64
+
+/* Norm of the elements [off, off + dim) of each head:
+ *   y = x * weight / sqrt(mean of x^2 + eps)
+ * the mean over these dim elements; the others stay as they are. */
+typedef struct kvx_norm {
+    const float *weight;         /* device, dim factors; NULL: all 1 */
+    int32_t dim, off;            /* multiples of 8; dim > 0, off >= 0, off + dim <= head_dim */
+    float eps;                   /* >= 0 */
+    int32_t reserved;            /* 0 */
+} kvx_norm;
+
+/* Positions of rows, on one axis or several (time, height and width of images
+ * and video): row x stands at positions[a * stride + x] on axis a, and pair j of
+ * a rotation turns with its position on axis[j]. */
+typedef struct kvx_positions {
+    const int32_t *positions;    /* device; any int32 values */
+    int64_t stride;              /* >= 0; with several axes at least k's num_rows */
+    const int32_t *axis;         /* device, rot_dim / 2 entries in [0, num_axes); NULL: all 0 */
+    int32_t num_axes;            /* 1 .. 16 */
+    int32_t reserved;            /* 0 */
+} kvx_positions;
+
+/* kvx_append, where q is first normed by q_norm and k by k_norm (each NULL: not),
+ * then rotated, for the positions of `positions` (NULL: those of the records, as
+ * kvx_append; else the records' position is not used, but a negative one is still
+ * malformed), and rounded once.  An axis outside [0, num_axes) raises
+ * KVX_DERR_BAD_REQ, and nothing is written.  rope must be given with positions.
+ * head_dim <= 1024. */
+int kvx_append_normed(const kvx_pool *pool, int32_t layer, const float *scales,
+                      const kvx_rows *q, const kvx_rows *q_out, const kvx_rows *k, const kvx_rows *v,
+                      const kvx_rope *rope, const kvx_norm *q_norm, const kvx_norm *k_norm,
+                      const kvx_positions *positions, const int32_t *pt, int64_t pt_len,
+                      const kvx_append_req *reqs, int32_t n_reqs, int32_t max_tokens,
+                      uint32_t *dev_err, void *stream);
+
+/* Scores of a query at position p with a key at position t:
+ *   s = scale * q . K(t);  with cap > 0  s = cap * tanh(s / cap);  with slopes
+ *   s = s - slopes[query head] * |p - t|;  with window > 0 only keys with
+ *   p - t < window take part. */
+typedef struct kvx_scores {
+    const float *slopes;         /* device, one for each query head; NULL: none */
+    float scale;
+    float cap;                   /* 0: not capped; else > 0 */
+    int32_t window;              /* 0: none; else >= 1 */
+    int32_t reserved;            /* 0 */
+} kvx_scores;
+
+/* Queries of a request (32 bytes): rows row_off .. row_off + n_queries - 1 of q
+ * and out, over positions [start, end) of its pages.  The queries' own keys are
+ * the last n_queries of the positions below end.  Malformed (its outputs are then
+ * not written): a negative field, end < start, end < n_queries, end - start >
+ * max_tokens, n_queries > max_queries, rows past q's or out's num_rows, for
+ * kvx_attend_tree n_queries > KVX_MAX_DRAFTS or prefix not 0.  Records must not
+ * share rows. */
+typedef struct kvx_queries_req {
+    int64_t pt_off;
+    int64_t row_off;
+    int32_t start, end;
+    int32_t n_queries;
+    int32_t prefix;              /* kvx_attend_prompt: positions below it are seen by all queries */
+} kvx_queries_req;
+
+/* Attention of the queries i < n_queries of each record, each at position
+ * p = end - n_queries + i: over the positions t of [start, end) with t <= p or t <
+ * prefix (and within the window).  prefix = end makes all see all; documents that
+ * lie in one request's pages one after the other are a record each.  With G = q
+ * heads / num_heads and K(t), V(t) as in kvx_attend and s as above,
+ *   m = max s,  w(t) = exp(s(t) - m),  l = sum w,
+ *   out[row_off + i, head] = sum w(t) V(t) / l,
+ *   lse[(row_off + i) * q heads + head] = m + log l.
+ * Positions that cannot be resolved take no part.  A query that sees no position
+ * (or with every score -inf) gives zeros and lse -inf; what stands in positions
+ * that it does not see, NaN and infinities too, does not reach it.
+ * w is rounded to the rows' type for its product with V (with up to 32 rows of
+ * max_queries x G held in two parts as in kvx_attend); sums, maxima and l are held
+ * in 32 bits.
+ * q heads, head_dim and v_dim as kvx_attend; max_queries x G at most 2^30.  lse:
+ * num_rows of q x q heads floats, or NULL.  Rows of no record keep what they hold.
+ * workspace: kvx_queries_workspace() bytes for the same arguments, or more,
+ * 16-byte aligned; what it holds before a call does not matter.  Calls that may
+ * run at the same time need one each. */
+int kvx_attend_prompt(const kvx_pool *pool, int32_t layer, const float *scales,
+                      const kvx_rows *q, const kvx_rows *out, float *lse, const kvx_scores *scores,
+                      const int32_t *pt, int64_t pt_len,
+                      const kvx_queries_req *reqs, int32_t n_reqs, int32_t max_queries, int32_t max_tokens,
+                      void *workspace, int64_t workspace_bytes, uint32_t *dev_err, void *stream);
+
+/* The same for drafted tokens: draft j of a record has its key at position
+ * end - n_queries + j, and stands at p = end - n_queries + depth, depth the number
+ * of its ancestors among the drafts.  Query i sees the positions of [start, end -
+ * n_queries), and draft j where bit j of tree[row_off + i] is set (from start on).
+ * The bits are its ancestors and itself: depth is the number of the bits below
+ * n_queries that are set, less one (0 if none is); bits from n_queries on are
+ * ignored.  Distances and windows go by p.  tree: device memory, num_rows of q
+ * entries, 8-byte aligned. */
+int kvx_attend_tree(const kvx_pool *pool, int32_t layer, const float *scales,
+                    const kvx_rows *q, const kvx_rows *out, float *lse, const kvx_scores *scores,
+                    const int32_t *pt, int64_t pt_len,
+                    const kvx_queries_req *reqs, const uint64_t *tree, int32_t n_reqs,
+                    int32_t max_queries, int32_t max_tokens,
+                    void *workspace, int64_t workspace_bytes, uint32_t *dev_err, void *stream);
+
+/* Bytes that kvx_attend_prompt and kvx_attend_tree need as workspace for up to
+ * n_reqs records of up to max_queries queries and max_tokens positions each; -1
+ * on arguments that they refuse. */
+int64_t kvx_queries_workspace(const kvx_pool *pool, int32_t n_reqs, int32_t q_heads, int32_t v_dim,
+                              int32_t max_queries, int32_t max_tokens);
+
+/* What a request accepted of its drafts (24 bytes). */
+typedef struct kvx_path_req {
+    int64_t pt_off;
+    int64_t path_off;            /* in path: entry 0 */
+    int32_t start;               /* position of draft 0 */
+    int32_t n_tokens;            /* accepted */
+} kvx_path_req;
+
+/* For every record, layer l, kv c, head h and i < n_tokens, in place:
+ *   pool(l, c, start + i, h, :) := pool(l, c, start + k, h, :), k = path[path_off + i],
+ * as they stood before the call.  A record's list ascends (k > the one before, so
+ * that k >= i).  Malformed: a negative field, a list that reaches outside path or
+ * does not ascend, start + k above 2^31 - 1, n_tokens > max_tokens.  max_tokens: at
+ * most KVX_MAX_DRAFTS.  A row is left out if either page cannot be resolved.  Any
+ * elem_bytes.  Records must not share the pages between start and start + their
+ * last k.  The pool may be pinned host memory. */
+int kvx_keep_path(const kvx_pool *pool, const int32_t *pt, int64_t pt_len,
+                  const kvx_path_req *reqs, int32_t n_reqs, int32_t max_tokens,
+                  const int32_t *path, int64_t path_len, uint32_t *dev_err, void *stream);
+
 /* Bytes a pool described by *pool occupies (-1 if the descriptor is invalid). */
 int64_t kvx_pool_bytes(const kvx_pool *pool);
 

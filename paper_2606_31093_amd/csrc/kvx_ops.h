@@ -56,6 +56,24 @@ struct AppendParams {
     FastDiv fd_items, fd_items_v, fd_token, fd_half;
 };
 
+// kvx_norm with a device weight; dim 0: none.
+struct HeadNorm {
+    const float *weight;
+    int32_t dim, off;
+    float eps;
+};
+
+struct NormedParams : AppendParams {
+    HeadNorm q_norm, k_norm;
+    const int32_t *positions;    // [axis][pos_stride]: of rows; nullptr: the records'
+    int64_t pos_stride;
+    const int32_t *axis;         // of each pair, or nullptr
+    int32_t num_axes;
+    // launch (with AppendParams' but items_v, fd_items, fd_items_v): lanes of a
+    // row, items of a lane; fd_token: heads
+    int32_t lanes, per_lane;
+};
+
 struct AttendParams {
     Layer pool;
     const float *scales;
@@ -124,8 +142,22 @@ struct KeptParams {
     FastDiv fd_Ts, fd_Td, fd_vpr;
 };
 
+struct PathParams {
+    Side pool;
+    const kvx_path_req *reqs;
+    int32_t n_reqs, max_tokens;
+    const int32_t *path;
+    int64_t path_len;
+    int64_t vectors;             // 16-byte vectors of a token in all layers
+    uint32_t *err;
+    int32_t C, blocks;           // workgroups per record
+    FastDiv fd_T, fd_H, fd_vpr;
+};
+
 // Each launches on `stream` and returns a hipError_t value.
 int launch_append(const AppendParams &p, hipStream_t stream);
+int launch_append_normed(const NormedParams &p, hipStream_t stream);
+int launch_path(const PathParams &p, hipStream_t stream);
 int launch_attend(const AttendParams &p, hipStream_t stream);
 int launch_select(const SelectParams &p, hipStream_t stream);
 int launch_kept(const KeptParams &p, hipStream_t stream);

@@ -10,6 +10,7 @@
 #include "kvx.h"
 #include "kvx_host.h"
 #include "kvx_ops.h"
+#include "kvx_queries_plan.h"
 
 using namespace kvx;
 
@@ -142,15 +143,10 @@ int check_attend(const Shape &s, int32_t n_reqs, int32_t q_heads, int32_t v_dim)
     return KVX_OK;
 }
 
-}  // namespace
-
-extern "C" {
-
-int kvx_append(const kvx_pool *pool, int32_t layer, const float *scales, const kvx_rows *q, const kvx_rows *q_out,
-               const kvx_rows *k, const kvx_rows *v, const kvx_rope *rope, const int32_t *pt, int64_t pt_len,
-               const kvx_append_req *reqs, int32_t n_reqs, int32_t max_tokens, uint32_t *dev_err, void *stream) {
-    g_last_error.clear();
-    Shape s;
+// What kvx_append and kvx_append_normed check on the host.
+int check_append(const kvx_pool *pool, int32_t layer, const float *scales, const kvx_rows *q, const kvx_rows *q_out,
+                 const kvx_rows *k, const kvx_rows *v, const kvx_rope *rope, const int32_t *pt, int64_t pt_len,
+                 const void *reqs, int32_t n_reqs, int32_t max_tokens, uint32_t *dev_err, Shape &s) {
     int st;
     if ((st = check_values(pool, layer, scales, s))) return st;
     if ((st = check_rows(k, "k"))) return st;
@@ -189,9 +185,16 @@ int kvx_append(const kvx_pool *pool, int32_t layer, const float *scales, const k
     }
     if ((st = check_records(reqs, n_reqs, max_tokens, dev_err))) return st;
     if ((st = check_table(pt, pt_len, "pt"))) return st;
-    if (n_reqs == 0) return KVX_OK;
-    AppendParams P{};
-    Known known;
+    return KVX_OK;
+}
+
+// Their parameters, with the device's view of every pointer.
+int fill_append(const kvx_pool *pool, int32_t layer, const float *scales, const kvx_rows *q, const kvx_rows *q_out,
+                const kvx_rows *k, const kvx_rows *v, const kvx_rope *rope, const int32_t *pt, int64_t pt_len,
+                const kvx_append_req *reqs, int32_t n_reqs, int32_t max_tokens, uint32_t *dev_err, const Shape &s,
+                Known &known, AppendParams &P) {
+    const int32_t rot = rope ? rope->rot_dim : 0;
+    int st;
     if ((st = view_layer(pool, layer, pt, pt_len, true, known, P.pool))) return st;
     if ((st = view(scales, (int64_t)s.C * s.H * 4, "scales", false, known, &P.scales))) return st;
     if (q && (st = view_rows(q, "q", false, known, P.q))) return st;
@@ -210,7 +213,183 @@ int kvx_append(const kvx_pool *pool, int32_t layer, const float *scales, const k
     P.max_tokens = max_tokens;
     P.f16 = k->dtype == KVX_F16;
     P.e4m3 = s.e == 1;
+    return KVX_OK;
+}
+
+int check_norm(const kvx_norm *n, int32_t D, const char *name) {
+    if (!n) return KVX_OK;
+    if (n->reserved != 0) return fail(KVX_ERR_RANGE, "%s: reserved field must be 0", name);
+    if (n->dim < 8 || n->dim % 8 || n->off < 0 || n->off % 8 || (int64_t)n->off + n->dim > D)
+        return fail(KVX_ERR_SHAPE, "%s: %d elements from %d on (multiples of 8) in a head_dim of %d", name, n->dim, n->off, D);
+    if (!(n->eps >= 0.f)) return fail(KVX_ERR_RANGE, "%s: eps must be >= 0", name);
+    if ((reinterpret_cast<uintptr_t>(n->weight) & 3u) != 0)
+        return fail(KVX_ERR_ALIGN, "%s: weight is not 4-byte aligned", name);
+    return KVX_OK;
+}
+
+int view_norm(const kvx_norm *n, const char *name, Known &known, HeadNorm &out) {
+    out = HeadNorm{nullptr, 0, 0, 0.f};
+    if (!n) return KVX_OK;
+    out = HeadNorm{nullptr, n->dim, n->off, n->eps};
+    return view(n->weight, (int64_t)n->dim * 4, name, false, known, &out.weight);
+}
+
+int check_scores(const kvx_scores *x) {
+    if (!x) return fail(KVX_ERR_NULL, "scores is NULL");
+    if (x->reserved != 0) return fail(KVX_ERR_RANGE, "scores: reserved field must be 0");
+    if (!(x->cap >= 0.f) || std::isinf(x->cap)) return fail(KVX_ERR_RANGE, "scores: cap must be 0 (none) or positive");
+    if (x->window < 0) return fail(KVX_ERR_RANGE, "scores: window %d must be >= 0", x->window);
+    if ((reinterpret_cast<uintptr_t>(x->slopes) & 3u) != 0) return fail(KVX_ERR_ALIGN, "slopes is not 4-byte aligned");
+    return KVX_OK;
+}
+
+int check_queries(const Shape &s, int32_t q_heads, int32_t max_queries) {
+    if (max_queries < 0 || max_queries > KVX_MAX_TOKENS)
+        return fail(KVX_ERR_RANGE, "max_queries %d outside [0, %d]", max_queries, KVX_MAX_TOKENS);
+    // a record's rows of a cache head are counted in 32 bits
+    if ((int64_t)max_queries * (q_heads / s.H) > (1 << 30))
+        return fail(KVX_ERR_RANGE, "max_queries %d of %d query heads a cache head: at most 2^30 rows", max_queries,
+                    q_heads / s.H);
+    return KVX_OK;
+}
+
+// What shapes the launch and the workspace of the attention of several queries.
+void shape_queries(const kvx_pool *pool, int32_t q_heads, int32_t v_dim, int32_t n_reqs, int32_t max_queries,
+                   int32_t max_tokens, QueriesParams &P) {
+    P.pool.C = pool->num_kv;
+    P.pool.H = pool->num_heads;
+    P.pool.D = pool->head_dim;
+    P.fd_G = make_fastdiv((uint32_t)(q_heads / pool->num_heads));
+    P.e4m3 = pool->elem_bytes == 1;
+    P.Dv = v_dim;
+    P.n_reqs = n_reqs;
+    P.max_queries = max_queries;
+    P.max_tokens = max_tokens;
+    plan_queries(P);
+}
+
+// kvx_attend_prompt, and with a tree kvx_attend_tree.
+int attend_queries(const kvx_pool *pool, int32_t layer, const float *scales, const kvx_rows *q, const kvx_rows *out,
+                   float *lse, const kvx_scores *scores, const int32_t *pt, int64_t pt_len, const kvx_queries_req *reqs,
+                   const uint64_t *tree, bool is_tree, int32_t n_reqs, int32_t max_queries, int32_t max_tokens,
+                   void *workspace, int64_t workspace_bytes, uint32_t *dev_err, void *stream) {
+    g_last_error.clear();
+    Shape s;
+    int st;
+    if ((st = check_values(pool, layer, scales, s))) return st;
+    if ((st = check_rows(q, "q"))) return st;
+    if ((st = check_rows(out, "out"))) return st;
+    if ((st = check_attend(s, n_reqs, q->num_heads, out->head_dim))) return st;
+    if (q->head_dim != s.D) return fail(KVX_ERR_SHAPE, "q has head_dim %d, the pool %d", q->head_dim, s.D);
+    if (out->num_heads != q->num_heads || out->dtype != q->dtype || out->num_rows != q->num_rows)
+        return fail(KVX_ERR_SHAPE, "out differs from q in heads, dtype or rows");
+    if ((st = check_apart(out, out->num_rows, "out"))) return st;
+    if ((st = check_scores(scores))) return st;
+    if ((st = check_records(reqs, n_reqs, max_tokens, dev_err))) return st;
+    if ((st = check_queries(s, q->num_heads, max_queries))) return st;
+    if ((st = check_table(pt, pt_len, "pt"))) return st;
+    if ((reinterpret_cast<uintptr_t>(lse) & 3u) != 0) return fail(KVX_ERR_ALIGN, "lse is not 4-byte aligned");
+    if ((reinterpret_cast<uintptr_t>(tree) & 7u) != 0) return fail(KVX_ERR_ALIGN, "tree is not 8-byte aligned");
+    if (is_tree && !tree && q->num_rows > 0) return fail(KVX_ERR_NULL, "tree is NULL");
+    if (q->num_rows > INT64_MAX / 8192) return fail(KVX_ERR_RANGE, "q holds %lld rows", (long long)q->num_rows);
+    if (n_reqs == 0) return KVX_OK;
+    QueriesParams P{};
+    shape_queries(pool, q->num_heads, out->head_dim, n_reqs, max_queries, max_tokens, P);
+    const int64_t need = queries_workspace(P, nullptr);
+    if (!workspace) return fail(KVX_ERR_NULL, "workspace is NULL");
+    if (!aligned16(workspace)) return fail(KVX_ERR_ALIGN, "workspace %p is not 16-byte aligned", workspace);
+    if (workspace_bytes < need)
+        return fail(KVX_ERR_RANGE, "workspace holds %lld bytes, this call needs %lld", (long long)workspace_bytes,
+                    (long long)need);
+    Known known;
+    char *ws;
+    if ((st = view_layer(pool, layer, pt, pt_len, false, known, P.pool))) return st;
+    if ((st = view(scales, (int64_t)s.C * s.H * 4, "scales", false, known, &P.scales))) return st;
+    if ((st = view_rows(q, "q", false, known, P.q))) return st;
+    if ((st = view_rows(out, "out", true, known, P.out))) return st;
+    if ((st = view(lse, q->num_rows * q->num_heads * 4, "lse", true, known, &P.lse))) return st;
+    if ((st = view(scores->slopes, (int64_t)q->num_heads * 4, "slopes", false, known, &P.slopes))) return st;
+    if ((st = view(tree, q->num_rows * 8, "tree", false, known, &P.tree))) return st;
+    if ((st = view(static_cast<char *>(workspace), need, "workspace", true, known, &ws))) return st;
+    if ((st = view(reqs, (int64_t)n_reqs * (int64_t)sizeof *reqs, "reqs", false, known, &P.reqs))) return st;
+    if ((st = view(dev_err, 4, "dev_err", true, known, &P.err))) return st;
+    // the kernel reads an entry for every position, also where none is in range
+    if (!P.pool.pt) P.pool.pt = reinterpret_cast<const int32_t *>(P.reqs);
+    // no rows: every record with queries is malformed, and no entry is read
+    if (is_tree && !P.tree) P.tree = reinterpret_cast<const uint64_t *>(P.reqs);
+    (void)queries_workspace(P, ws);
+    P.num_rows = q->num_rows;
+    P.scale = scores->scale;
+    P.cap = scores->cap;
+    P.window = scores->window;
+    P.f16 = q->dtype == KVX_F16;
+    return launched(launch_queries(P, static_cast<hipStream_t>(stream)));
+}
+
+}  // namespace
+
+extern "C" {
+
+int kvx_append(const kvx_pool *pool, int32_t layer, const float *scales, const kvx_rows *q, const kvx_rows *q_out,
+               const kvx_rows *k, const kvx_rows *v, const kvx_rope *rope, const int32_t *pt, int64_t pt_len,
+               const kvx_append_req *reqs, int32_t n_reqs, int32_t max_tokens, uint32_t *dev_err, void *stream) {
+    g_last_error.clear();
+    Shape s;
+    int st;
+    if ((st = check_append(pool, layer, scales, q, q_out, k, v, rope, pt, pt_len, reqs, n_reqs, max_tokens, dev_err, s)))
+        return st;
+    if (n_reqs == 0) return KVX_OK;
+    AppendParams P{};
+    Known known;
+    if ((st = fill_append(pool, layer, scales, q, q_out, k, v, rope, pt, pt_len, reqs, n_reqs, max_tokens, dev_err, s, known,
+                          P)))
+        return st;
     return launched(launch_append(P, static_cast<hipStream_t>(stream)));
+}
+
+int kvx_append_normed(const kvx_pool *pool, int32_t layer, const float *scales, const kvx_rows *q, const kvx_rows *q_out,
+                      const kvx_rows *k, const kvx_rows *v, const kvx_rope *rope, const kvx_norm *q_norm,
+                      const kvx_norm *k_norm, const kvx_positions *positions, const int32_t *pt, int64_t pt_len,
+                      const kvx_append_req *reqs, int32_t n_reqs, int32_t max_tokens, uint32_t *dev_err, void *stream) {
+    g_last_error.clear();
+    Shape s;
+    int st;
+    if ((st = check_append(pool, layer, scales, q, q_out, k, v, rope, pt, pt_len, reqs, n_reqs, max_tokens, dev_err, s)))
+        return st;
+    if (s.D > 1024) return fail(KVX_ERR_SHAPE, "head_dim %d: at most 1024", s.D);
+    if (q_norm && !q) return fail(KVX_ERR_NULL, "q_norm without q");
+    if ((st = check_norm(q_norm, s.D, "q_norm"))) return st;
+    if ((st = check_norm(k_norm, s.D, "k_norm"))) return st;
+    if (positions) {
+        if (!rope || rope->rot_dim == 0) return fail(KVX_ERR_NULL, "positions without a rotation");
+        if (positions->reserved != 0) return fail(KVX_ERR_RANGE, "positions: reserved field must be 0");
+        if (positions->num_axes < 1 || positions->num_axes > 16)
+            return fail(KVX_ERR_RANGE, "positions: num_axes %d outside [1, 16]", positions->num_axes);
+        if (positions->stride < 0 || (positions->num_axes > 1 && positions->stride < k->num_rows) ||
+            positions->stride > INT64_MAX / 128)
+            return fail(KVX_ERR_RANGE, "positions: stride %lld of axes of %lld rows", (long long)positions->stride,
+                        (long long)k->num_rows);
+        if (!positions->positions && k->num_rows > 0) return fail(KVX_ERR_NULL, "positions is NULL");
+        if (((reinterpret_cast<uintptr_t>(positions->positions) | reinterpret_cast<uintptr_t>(positions->axis)) & 3u) != 0)
+            return fail(KVX_ERR_ALIGN, "positions or axis is not 4-byte aligned");
+    }
+    if (n_reqs == 0) return KVX_OK;
+    NormedParams P{};
+    Known known;
+    if ((st = fill_append(pool, layer, scales, q, q_out, k, v, rope, pt, pt_len, reqs, n_reqs, max_tokens, dev_err, s, known,
+                          P)))
+        return st;
+    if ((st = view_norm(q_norm, "q_norm weight", known, P.q_norm))) return st;
+    if ((st = view_norm(k_norm, "k_norm weight", known, P.k_norm))) return st;
+    if (positions) {
+        P.num_axes = positions->num_axes;
+        P.pos_stride = positions->stride;
+        if ((st = view(positions->positions, ((P.num_axes - 1) * P.pos_stride + P.num_rows) * 4, "positions", false, known,
+                       &P.positions)))
+            return st;
+        if ((st = view(positions->axis, (int64_t)P.half * 4, "axis", false, known, &P.axis))) return st;
+    }
+    return launched(launch_append_normed(P, static_cast<hipStream_t>(stream)));
 }
 
 int64_t kvx_attend_workspace(const kvx_pool *pool, int32_t n_reqs, int32_t q_heads, int32_t v_dim,
@@ -379,6 +558,70 @@ int kvx_transfer_kept(const kvx_pool *src, const kvx_pool *dst, const kvx_slice 
     P.fd_Td = make_fastdiv((uint32_t)P.dst.T);
     P.fd_vpr = make_fastdiv((uint32_t)P.vpr);
     return launched(launch_kept(P, static_cast<hipStream_t>(stream)));
+}
+
+int64_t kvx_queries_workspace(const kvx_pool *pool, int32_t n_reqs, int32_t q_heads, int32_t v_dim,
+                              int32_t max_queries, int32_t max_tokens) {
+    g_last_error.clear();
+    Shape s;
+    if (pool_shape(pool, "pool", s) || check_attend(s, n_reqs, q_heads, v_dim) || check_queries(s, q_heads, max_queries)) return -1;
+    if (max_tokens < 0 || max_tokens > KVX_MAX_TOKENS) {
+        fail(KVX_ERR_RANGE, "max_tokens %d outside [0, %d]", max_tokens, KVX_MAX_TOKENS);
+        return -1;
+    }
+    QueriesParams P{};
+    shape_queries(pool, q_heads, v_dim, n_reqs, max_queries, max_tokens, P);
+    return queries_workspace_most(P);
+}
+
+int kvx_attend_prompt(const kvx_pool *pool, int32_t layer, const float *scales, const kvx_rows *q, const kvx_rows *out,
+                      float *lse, const kvx_scores *scores, const int32_t *pt, int64_t pt_len, const kvx_queries_req *reqs,
+                      int32_t n_reqs, int32_t max_queries, int32_t max_tokens, void *workspace, int64_t workspace_bytes,
+                      uint32_t *dev_err, void *stream) {
+    return attend_queries(pool, layer, scales, q, out, lse, scores, pt, pt_len, reqs, nullptr, false, n_reqs, max_queries,
+                          max_tokens, workspace, workspace_bytes, dev_err, stream);
+}
+
+int kvx_attend_tree(const kvx_pool *pool, int32_t layer, const float *scales, const kvx_rows *q, const kvx_rows *out,
+                    float *lse, const kvx_scores *scores, const int32_t *pt, int64_t pt_len, const kvx_queries_req *reqs,
+                    const uint64_t *tree, int32_t n_reqs, int32_t max_queries, int32_t max_tokens, void *workspace,
+                    int64_t workspace_bytes, uint32_t *dev_err, void *stream) {
+    return attend_queries(pool, layer, scales, q, out, lse, scores, pt, pt_len, reqs, tree, true, n_reqs, max_queries,
+                          max_tokens, workspace, workspace_bytes, dev_err, stream);
+}
+
+int kvx_keep_path(const kvx_pool *pool, const int32_t *pt, int64_t pt_len, const kvx_path_req *reqs, int32_t n_reqs,
+                  int32_t max_tokens, const int32_t *path, int64_t path_len, uint32_t *dev_err, void *stream) {
+    g_last_error.clear();
+    Shape s;
+    int st;
+    if ((st = check_pool(pool, "pool", s))) return st;
+    if ((st = check_records(reqs, n_reqs, max_tokens, dev_err))) return st;
+    if (max_tokens > KVX_MAX_DRAFTS)
+        return fail(KVX_ERR_RANGE, "max_tokens %d outside [0, %d]", max_tokens, KVX_MAX_DRAFTS);
+    if ((st = check_table(pt, pt_len, "pt"))) return st;
+    if ((st = check_table(path, path_len, "path"))) return st;
+    if (n_reqs == 0) return KVX_OK;
+    PathParams P{};
+    Known known;
+    char *base;
+    const int32_t *table;
+    if ((st = view(static_cast<char *>(pool->base), pool_bytes(pool), "pool base", false, known, &base))) return st;
+    if ((st = view(pt, pt_len * 4, "pt", false, known, &table))) return st;
+    if ((st = view(reqs, (int64_t)n_reqs * (int64_t)sizeof *reqs, "reqs", false, known, &P.reqs))) return st;
+    if ((st = view(path, path_len * 4, "path", false, known, &P.path))) return st;
+    if ((st = view(dev_err, 4, "dev_err", true, known, &P.err))) return st;
+    P.pool = pool_side(pool, base, table, pt_len, 0, 0, 0, s.H);
+    P.n_reqs = n_reqs;
+    P.max_tokens = max_tokens;
+    P.path_len = path_len;
+    const int64_t vpr = (int64_t)s.D * s.e / 16;
+    P.vectors = vpr * s.L * s.C * s.H;
+    P.C = s.C;
+    P.fd_T = make_fastdiv((uint32_t)pool->page_tokens);
+    P.fd_H = make_fastdiv((uint32_t)s.H);
+    P.fd_vpr = make_fastdiv((uint32_t)vpr);
+    return launched(launch_path(P, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

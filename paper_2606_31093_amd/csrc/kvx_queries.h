@@ -1,0 +1,796 @@
+// kvx_queries.h -- attention of several queries of a request over a paged cache
+// (gfx950): the kernel.
+//
+// Mathematics.  Rows are pairs (query, query head of the group), row x = query x / G,
+// head x % G: all rows of a cache head read the same keys.  s = q.K, capped and
+// biased, softmax over the positions that a row sees, out = w V, in one pass with a
+// running maximum m and sum l; scores are kept in units of log2.
+//
+// A workgroup's unit is a block of rows of one record and cache head; it goes over the
+// tiles of the positions that some row of the block sees.  A tile's keys and values
+// lie in LDS (16-bit; e4m3 is widened on the way, once for all wavefronts), twice, so
+// that the next tile is on its way while this one is used.
+//
+// Matrix products of 32 x 32, without a move between lanes.  With c = lane % 32, e =
+// lane / 32:
+// - scores, transposed: A = 32 rows of K, B = 32 queries (registers); lane (c, e) gets
+//   the scores of row c at positions 8 i + 4 e + j (i, j < 4): a row's maximum and sum
+//   are taken within a lane and its partner in the other half;
+// - these weights are one lane's part of the B operand of the second product, if its k
+//   index 8 e + x stands for position 4 e + x (x < 4) or 8 + 4 e + x - 4 (of 16);
+// - A = V transposed, by the loads from LDS that transpose: 16 lanes give the addresses
+//   of 4 rows x 16 elements, and lane c gets column c;
+// - out, transposed: lane (c, e) holds row c, so that a row's rescaling is its lane's.
+//
+// What a row does not see must not reach it, NaN and infinities too, and a product with
+// weight 0 would bring them: where some row of a tile does not see all of it, the
+// tile's values are looked over, and rows of V that are not finite are added by hand to
+// the rows that see them, and replaced by zeros for the product.
+#pragma once
+
+#include "kvx_attend.h"
+#include "kvx_queries_plan.h"
+
+namespace kvx {
+
+// Launches the first kernel, by the rows' and the pool's type, for units first ..
+// first + n - 1 (whole), or for records first .. first + n - 1.
+int launch_queries_bf16(const QueriesParams &p, int64_t first, int64_t n, hipStream_t stream);
+int launch_queries_f16(const QueriesParams &p, int64_t first, int64_t n, hipStream_t stream);
+int launch_queries_bf16_e4m3(const QueriesParams &p, int64_t first, int64_t n, hipStream_t stream);
+int launch_queries_f16_e4m3(const QueriesParams &p, int64_t first, int64_t n, hipStream_t stream);
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+
+__device__ __forceinline__ bool valid(const kvx_queries_req &q, const QueriesParams &p) {
+    return q.pt_off >= 0 && q.row_off >= 0 && q.start >= 0 && q.end >= q.start && q.n_queries >= 0 && q.prefix >= 0 &&
+           q.end >= q.n_queries && q.end - q.start <= p.max_tokens && q.n_queries <= p.max_queries &&
+           q.row_off <= p.num_rows - q.n_queries && (!p.tree || (q.n_queries <= KVX_MAX_DRAFTS && q.prefix == 0));
+}
+
+// Positions [lo, hi) that some query of several sees, at most.
+struct Span {
+    uint32_t lo, hi;
+};
+
+// Queries i0 .. i1 of a well-formed record.
+__device__ __forceinline__ Span span_of(const kvx_queries_req &q, const QueriesParams &p, int i0, int i1) {
+    const int base = q.end - q.n_queries;
+    const int near = (p.tree ? base : base + i0) - p.window + 1;
+    const int seen = p.tree ? q.end : base + i1 + 1 > q.prefix ? base + i1 + 1 : q.prefix;
+    return Span{(uint32_t)(p.window && near > q.start ? near : q.start), (uint32_t)(seen < q.end ? seen : q.end)};
+}
+
+__device__ __forceinline__ int blocks_of(const kvx_queries_req &q, const QueriesParams &p) {
+    return (int)(((int64_t)q.n_queries * p.fd_G.d + p.rows - 1) / p.rows);
+}
+
+// Rows x0 .. x1 of a record, its queries' rows (x1: or the last one).
+__device__ __forceinline__ Span span_of_rows(const kvx_queries_req &q, const QueriesParams &p, uint32_t x0, uint32_t x1) {
+    const int i0 = fd_div(p.fd_G, x0), i1 = fd_div(p.fd_G, x1);
+    return span_of(q, p, i0, i1 < q.n_queries ? i1 : q.n_queries - 1);
+}
+
+__device__ __forceinline__ int steps_of(const Span &s, const QueriesParams &p) {
+    return s.hi > s.lo ? (int)((s.hi - (s.lo & -kTile) + p.step - 1) / p.step) : 1;
+}
+
+__device__ __forceinline__ Span span_of_block(const kvx_queries_req &q, const QueriesParams &p, int b) {
+    return span_of_rows(q, p, (uint32_t)b * p.rows, (uint32_t)b * p.rows + p.rows - 1);
+}
+
+// Steps of one cache head of a record.
+__device__ __forceinline__ int64_t steps_of_head(const kvx_queries_req &q, const QueriesParams &p) {
+    if (!valid(q, p)) return 0;
+    int64_t sum = 0;
+    const int n = blocks_of(q, p);
+    for (int b = 0; b < n; ++b) sum += steps_of(span_of_block(q, p, b), p);
+    return sum;
+}
+
+__device__ __forceinline__ kvx_queries_req scalar(const kvx_queries_req &q) {
+    uint32_t w[8];
+    __builtin_memcpy(w, &q, sizeof w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = __builtin_amdgcn_readfirstlane(w[i]);
+    kvx_queries_req s;
+    __builtin_memcpy(&s, w, sizeof s);
+    return s;
+}
+
+__device__ __forceinline__ int64_t scalar(int64_t x) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 |
+                     (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+}
+
+// Part of a unit: positions [begin, end) for block b of cache head h.
+struct Piece {
+    kvx_queries_req rec;
+    int32_t h, b;
+    uint32_t begin, end;
+    int64_t place;               // of its partial results; -1: it is the whole unit
+};
+
+// The place of share k's part of a unit whose first of all steps is `first`: its first
+// part has the place k, one that begins inside the share place shares + k.
+__device__ __forceinline__ int64_t place_of(int64_t first, int64_t k, int64_t each, int64_t shares) {
+    return first > k * each ? shares + k : k;
+}
+
+__device__ __forceinline__ int64_t share_of(int64_t total, int64_t shares) {
+    const int64_t each = quotient(total + shares - 1, shares);
+    return each < 1 ? 1 : each;
+}
+
+// bits below x
+__device__ __forceinline__ uint64_t ones(int64_t x) { return x <= 0 ? 0 : x >= 64 ? ~0ull : (1ull << x) - 1; }
+
+// A row's permutation of its 16-byte chunks, in each 8 of them: one chunk of 8
+// successive rows (keys) and two chunks of 4 (values) lie in different banks.
+__device__ __forceinline__ int swirl(int r) { return (r & 3) << 1 | (r >> 2 & 1); }
+
+// 16 bytes a lane to LDS, in order of lanes from `to` on.  In assembly, since the compiler
+// would wait for all of them before reads of LDS; nothing reads what they bring before
+// the wait and the barrier of arrive().
+__device__ __forceinline__ void load_to_lds(const char *from, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+}
+
+// The lane, computed where it is used, so that what follows from it is not kept in
+// registers from tile to tile.
+__device__ __forceinline__ int lane_again() {
+    int zero = 0;
+    asm volatile("" : "+s"(zero));
+    return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, zero));
+}
+
+static __device__ const uint4 kvx_zeros = {0, 0, 0, 0};
+
+template <bool F16>
+__device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+    if constexpr (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(bits<f16x8>(a), bits<f16x8>(b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(bits<bf16x8>(a), bits<bf16x8>(b), c, 0, 0, 0);
+}
+
+// Whether one of two 16-bit values is infinite or NaN.
+template <bool F16>
+__device__ __forceinline__ bool not_finite(uint32_t w) {
+    const uint32_t e = F16 ? 0x7c00u : 0x7f80u;
+    return (w & e) == e || (w >> 16 & e) == e;
+}
+
+// DK: elements of a row in LDS (head_dim is up to that), DV: of a value; RB: blocks of 32
+// rows of a wavefront; TEAM: wavefronts that share a tile (4, the workgroup's, each with
+// its rows; or 1: each takes tiles of its own for the same rows, and they join at the
+// end); TILE: positions; GENERAL: scores may be capped or biased.
+template <bool F16, bool E4M3, int DK, int DV, int RB, int TEAM, int TILE, bool GENERAL>
+struct Queries {
+    typedef Half<F16> V;
+    static constexpr int KS = DK / 16, DB = DV / 32, PB = TILE / 32, PITCH = 2 * DK;
+    static constexpr int SRC = DK * (E4M3 ? 1 : 2) / 16;       // 16-byte chunks of a row in memory
+    static constexpr int LOADS = (TILE * SRC + 64 * TEAM - 1) / (64 * TEAM);   // a wavefront's of a tile, for K or for V
+    static constexpr bool PARTS = TEAM == 1;                   // weights in two parts
+    static constexpr uint64_t ALL = TILE == 64 ? ~0ull : 0xffffffffull;
+    static_assert((E4M3 || LOADS * 64 * TEAM == TILE * SRC) && (TILE == 32 || TILE == 64), "tile");
+
+    const QueriesParams &p;
+    int64_t *row_off;            // [TILE], this wavefront's: the tile's that is asked for
+    float *depth;                // [64], this wavefront's
+    char *lds;                   // [2][rows of K, rows of V if there are two]
+    float *ml;                   // [wavefronts][32][2]
+    char *all_lds;
+    int lane, wave, c, e;
+    bool two;
+    int tile_bytes;
+    // of the piece
+    kvx_queries_req rec;
+    const char *kbase;
+    uint32_t first, end, bad;
+    u32x4 staged[E4M3 ? LOADS : 1][2];
+
+    __device__ __forceinline__ uint64_t entry(uint32_t t) const { return (uint64_t)rec.pt_off + fd_div(p.pool.fd_T, t); }
+    // the page id of position t0 + lane
+    __device__ __forceinline__ int32_t look(uint32_t t0) const {
+        const uint32_t t = t0 + lane;
+        const uint64_t idx = entry(t < end ? t : end - 1);
+        return p.pool.pt[idx < (uint64_t)p.pool.pt_len ? idx : 0];
+    }
+    // A tile's row offsets (-1: none) to LDS; the positions that are there.
+    __device__ __forceinline__ uint64_t resolve(uint32_t t0, int32_t page) {
+        const uint32_t t = t0 + lane;
+        const bool in = lane < TILE && t >= first && t < end;
+        const uint32_t at = t < end ? t : end - 1;
+        const bool known = entry(at) < (uint64_t)p.pool.pt_len;
+        const bool ok = in && known && (uint32_t)page < (uint32_t)p.pool.N;
+        if (in && !ok) bad |= known ? KVX_DERR_SRC_PAGE : KVX_DERR_PT_RANGE;
+        const int64_t off = page * p.pool.s_p + (int64_t)(at - fd_div(p.pool.fd_T, at) * p.pool.fd_T.d) * p.pool.s_t;
+        if (TILE == 64 || lane < TILE) row_off[lane] = ok ? off : -1;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        return (uint64_t)__ballot(ok);
+    }
+    // Asks for a tile's rows, zeros where there is none and behind head_dim.
+    __device__ __forceinline__ void load(int buf, int part) {
+        const int have = (E4M3 ? 1 : 2) * p.pool.D / 16, ln = lane_again();
+        const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)(lds + buf * tile_bytes);
+#pragma unroll
+        for (int x = 0; x < LOADS; ++x) {
+            const int u = (part * LOADS + x) * 64 + ln, row = u / SRC;
+            int chunk = u % SRC;
+            if (!E4M3) chunk ^= swirl(row);
+            if (LOADS * 64 * TEAM != TILE * SRC && row >= TILE) chunk = have;
+            const int64_t off = row_off[LOADS * 64 * TEAM != TILE * SRC ? row & (TILE - 1) : row];
+            const bool ok = off >= 0 && chunk < have;
+            const char *k = ok ? kbase + off + 16 * chunk : reinterpret_cast<const char *>(&kvx_zeros);
+            const char *v = ok ? k + p.pool.s_c : k;
+            if constexpr (E4M3) {
+                staged[x][0] = *reinterpret_cast<const u32x4 *>(k);
+                if (two) staged[x][1] = *reinterpret_cast<const u32x4 *>(v);
+            } else {
+                const uint32_t at = __builtin_amdgcn_readfirstlane(to + (part * LOADS + x) * 1024);
+                load_to_lds(k, at);
+                if (two) load_to_lds(v, at + TILE * PITCH);
+            }
+        }
+    }
+    // e4m3: what load() has brought, widened, to LDS.
+    __device__ __forceinline__ void put(int buf, int part) {
+        if constexpr (E4M3) {
+            char *to = lds + buf * tile_bytes;
+            const int ln = lane_again();
+#pragma unroll
+            for (int x = 0; x < LOADS; ++x) {
+                const int u = (part * LOADS + x) * 64 + ln, row = u / SRC, chunk = u % SRC * 2;
+                if (LOADS * 64 * TEAM != TILE * SRC && row >= TILE) continue;
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    if (kv && !two) continue;
+                    const u32x4 y = staged[x][kv];
+                    const uint32_t w[4] = {y[0], y[1], y[2], y[3]};
+                    char *at = to + (kv * TILE + row) * PITCH;
+                    *reinterpret_cast<u32x4 *>(at + 16 * (chunk ^ swirl(row))) = widen<F16, true>(w);
+                    *reinterpret_cast<u32x4 *>(at + 16 * ((chunk + 1) ^ swirl(row))) = widen<F16, true>(w + 2);
+                }
+            }
+        }
+    }
+    // What this wavefront has asked for and put is in LDS, and the team's is.
+    __device__ __forceinline__ void arrive() const {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        if (TEAM > 1) __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    }
+
+    // Addresses in LDS: a row's permutation concerns the low 3 bits of a chunk's number, so
+    // that there are few of them and the rest is in the instructions.
+    // - K: the lane's row, chunks 2 k + e for k % 4
+    // - V, 32 columns from 32 db on for db % 2: 16 lanes give the addresses of 4 rows x 16
+    //   elements, positions 32 pb + 16 s + 4 e + x and 8 behind, x < 4
+    int k_at[4], v_at[2];
+    __device__ __forceinline__ void address() {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) k_at[k] = c * PITCH + 16 * ((2 * k + e) ^ swirl(c));
+        const int l = lane & 15, row = 4 * e + l / 4;
+#pragma unroll
+        for (int d = 0; d < 2; ++d)
+            v_at[d] = row * PITCH + 16 * ((4 * d + (lane >> 4 & 1) * 2 + (l >> 1 & 1)) ^ swirl(row)) + (l & 1) * 8;
+    }
+    __device__ __forceinline__ u32x4 keys(const char *k, int pb, int step) const {
+        return *reinterpret_cast<const u32x4 *>(k + k_at[step % 4] + (32 * pb * PITCH + step / 4 * 128));
+    }
+    __device__ __forceinline__ u32x4 columns(const char *v, int pb, int s, int db) const {
+        const char *a = v + v_at[db % 2] + ((32 * pb + 16 * s) * PITCH + db / 2 * 128), *b = a + 8 * PITCH;
+        const u32x2 x = bits<u32x2>(__builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)a));
+        const u32x2 y = bits<u32x2>(__builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)b));
+        return u32x4{x[0], x[1], y[0], y[1]};
+    }
+
+    // Rows r0 .. r0 + n - 1 of V that hold values which are not finite.
+    __device__ __forceinline__ uint64_t spoilt(const char *v, int r0, int n) const {
+        uint64_t rows = 0;
+        for (int r = r0; r < r0 + n; ++r) {
+            bool found = false;
+            if (lane < DV / 8) {
+                const u32x4 w = *reinterpret_cast<const u32x4 *>(v + r * PITCH + 16 * (lane ^ swirl(r)));
+                found = not_finite<F16>(w[0]) || not_finite<F16>(w[1]) || not_finite<F16>(w[2]) || not_finite<F16>(w[3]);
+            }
+            if (__any(found)) rows |= 1ull << r;
+        }
+        return rows;
+    }
+    __device__ __forceinline__ bool any_spoilt(const char *v, int r0, int n) const {
+        bool found = false;
+#pragma unroll 4
+        for (int u = lane; u < n * (DV / 8); u += 64) {
+            const int r = r0 + u / (DV / 8), chunk = u % (DV / 8);
+            const u32x4 w = *reinterpret_cast<const u32x4 *>(v + r * PITCH + 16 * (chunk ^ swirl(r)));
+            found |= not_finite<F16>(w[0]) || not_finite<F16>(w[1]) || not_finite<F16>(w[2]) || not_finite<F16>(w[3]);
+        }
+        return __any(found);
+    }
+
+    __device__ __forceinline__ void run(const Piece &piece) {
+        rec = piece.rec;
+        const int G = p.fd_G.d, h = piece.h, n_rows = rec.n_queries * G, base = rec.end - rec.n_queries;
+        const int part = TEAM > 1 ? wave : 0, streams = p.waves / TEAM;
+        kbase = p.pool.base + h * p.pool.s_h;
+        const uint32_t begin = piece.begin;
+        end = piece.end;
+        first = rec.start;
+        bad = 0;
+
+        // Scores are taken times unit > 0: a sign goes into the queries.
+        float unit = p.scale * (p.scales ? p.scales[h] : 1.f) * kLog2e;
+        const uint32_t flip = unit < 0.f ? 0x80008000u : 0;
+        const bool none = unit == 0.f;
+        unit = none ? 1.f : fabsf(unit);
+        const float cap2 = p.cap * kLog2e, cap_unit = GENERAL && p.cap > 0.f ? 2.f * unit / p.cap : 0.f;
+
+        // This lane's row of each block of 32; past the last one, that one once more.
+        const int block0 = piece.b * p.rows, x0 = block0 + part * 32 * RB;
+        const bool active = x0 < n_rows;
+        int at[RB];                      // its position
+        uint32_t lo[RB], hi[RB];         // it sees [lo, hi)
+        uint64_t drafts[RB];             // and these drafts
+        float slope[RB];
+        u32x4 qv[RB][KS];
+        if (p.tree) {
+            if (lane < rec.n_queries) {
+                const int k = __popcll(p.tree[rec.row_off + lane] & ones(rec.n_queries));
+                depth[lane] = k > 0 ? k - 1 : 0;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            const int x = x0 + 32 * rb + c, row = x < n_rows ? x : n_rows - 1;
+            const int i = fd_div(p.fd_G, row), g = row - i * G;
+            at[rb] = base + i;
+            drafts[rb] = 0;
+            if (p.tree) {
+                const int mine = (int)depth[i];
+                at[rb] = base + mine;
+                drafts[rb] = p.tree[rec.row_off + i] & ones(rec.n_queries) & ~ones((int64_t)rec.start - base);
+                if (p.window)
+                    for (int j = 0; j < rec.n_queries; ++j)
+                        if (mine - (int)depth[j] >= p.window) drafts[rb] &= ~(1ull << j);
+            }
+            const int near = at[rb] - p.window + 1;
+            lo[rb] = p.window && near > rec.start ? near : rec.start;
+            const int seen = p.tree ? base : at[rb] + 1 > rec.prefix ? at[rb] + 1 : rec.prefix;
+            hi[rb] = seen < rec.end ? seen : rec.end;
+            slope[rb] = GENERAL && p.slopes ? p.slopes[h * G + g] * kLog2e : 0.f;
+            const char *src = p.q.base + (rec.row_off + i) * p.q.s_row + (int64_t)(h * G + g) * p.q.s_head;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const int d = 16 * k + 8 * e;
+                qv[rb][k] = u32x4{0, 0, 0, 0};
+                if (d < p.pool.D && !none) qv[rb][k] = *reinterpret_cast<const u32x4 *>(src + 2 * d);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) qv[rb][k][w] ^= flip;
+            }
+        }
+        // Positions that all rows of the wavefront see, that some see, and that all of the
+        // workgroup see.  In a tree depths differ within a block: the drafts and the last
+        // position's window bound them.
+        Span all, some, block_all;
+        {
+            const auto bounds = [&](int xa, int xz, Span &a, Span &s) {
+                xa = xa < n_rows ? xa : n_rows - 1;
+                xz = xz < n_rows ? xz : n_rows - 1;
+                s = span_of_rows(rec, p, xa, xz);
+                a.hi = p.tree ? (uint32_t)base : span_of_rows(rec, p, xa, xa).hi;
+                const int last = rec.end - p.window;
+                a.lo = !p.tree ? span_of_rows(rec, p, xz, xz).lo : (uint32_t)(p.window && last > rec.start ? last : rec.start);
+            };
+            Span unused;
+            bounds(x0, x0 + 32 * RB - 1, all, some);
+            bounds(block0, block0 + p.rows - 1, block_all, unused);
+        }
+
+        f32x16 o[RB][DB];
+        float m[RB], l[RB];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[rb][d][i] = 0.f;
+            m[rb] = -INFINITY;
+            l[rb] = 0.f;
+        }
+
+        uint32_t t0 = begin + (TEAM > 1 ? 0 : wave * TILE);
+        const uint32_t step = TILE * streams;
+        if (t0 < end) {
+            uint64_t here = resolve(t0, look(t0));
+            load(0, part);
+            put(0, part);
+            int32_t page = look(t0 + step);
+            for (int buf = 0; t0 < end; t0 += step, buf ^= 1) {
+                arrive();
+                const uint64_t next = resolve(t0 + step, page);
+                const bool more = t0 + step < end;
+                if (more) load(buf ^ 1, part);
+                page = look(t0 + 2 * step);
+                const char *kt = lds + buf * tile_bytes, *vt = kt + (two ? TILE * PITCH : 0);
+                const bool on = active && t0 < some.hi && t0 + TILE > some.lo;
+                const bool edge = here != ALL || t0 < all.lo || t0 + TILE > all.hi;        // some row does not see all
+                const bool team_edge = here != ALL || t0 < block_all.lo || t0 + TILE > block_all.hi;
+                f32x16 s[RB][PB];        // scores, then weights
+                uint64_t sees[RB];
+                if (on) {
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                        for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) s[rb][pb][i] = 0.f;
+#pragma unroll
+                    for (int k = 0; k < KS; ++k)
+#pragma unroll
+                        for (int pb = 0; pb < PB; ++pb) {
+                            const u32x4 a = keys(kt, pb, k);
+#pragma unroll
+                            for (int rb = 0; rb < RB; ++rb) s[rb][pb] = mfma32<F16>(a, qv[rb][k], s[rb][pb]);
+                        }
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) {
+                        if (GENERAL) {
+                            if (p.cap > 0.f) {
+#pragma unroll
+                                for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+                                    for (int i = 0; i < 16; ++i)
+                                        s[rb][pb][i] = cap2 - 2.f * cap2 * __builtin_amdgcn_rcpf(1.f + exp2_fast(s[rb][pb][i] * cap_unit));
+                            } else {
+#pragma unroll
+                                for (int pb = 0; pb < PB; ++pb) s[rb][pb] *= unit;
+                            }
+                            if (p.slopes) {
+                                const float far = (float)(at[rb] - (int)(t0 + 4 * e));
+                                const bool by_depth = p.tree && t0 + TILE > (uint32_t)base;
+#pragma unroll
+                                for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+                                    for (int i = 0; i < 16; ++i) {
+                                        const int off = 32 * pb + 8 * (i / 4) + i % 4;
+                                        float d = fabsf(far - (float)off);
+                                        if (by_depth) {
+                                            const int j = (int)(t0 + 4 * e + off) - base;
+                                            if (j >= 0 && j < rec.n_queries) d = fabsf((float)(at[rb] - base) - depth[j]);
+                                        }
+                                        s[rb][pb][i] -= slope[rb] * d;
+                                    }
+                            }
+                        }
+                        const float from = GENERAL ? 1.f : unit;
+                        sees[rb] = ALL;
+                        if (edge) {
+                            uint64_t v = ones((int64_t)hi[rb] - t0) & ~ones((int64_t)lo[rb] - t0);
+                            const int64_t to = (int64_t)base - t0;
+                            if (p.tree && to < 64 && to > -64) v |= to >= 0 ? drafts[rb] << to : drafts[rb] >> -to;
+                            sees[rb] = v & here;
+                            const uint64_t mine = sees[rb] >> (4 * e);
+#pragma unroll
+                            for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+                                for (int i = 0; i < 16; ++i)
+                                    if (!((uint32_t)(mine >> (32 * pb)) >> (8 * (i / 4) + i % 4) & 1)) s[rb][pb][i] = -INFINITY;
+                        }
+                        float top = s[rb][0][0];
+#pragma unroll
+                        for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[rb][pb][i]);
+                        top = fmaxf(top, __shfl_xor(top, 32)) * from;
+                        if (__any(top - kLift<F16> > m[rb] + kSlack)) {
+                            const float raised = fmaxf(m[rb], top - kLift<F16>), f = weight(m[rb], raised);
+                            m[rb] = raised;
+                            l[rb] *= f;
+#pragma unroll
+                            for (int d = 0; d < DB; ++d) o[rb][d] *= f;
+                        }
+                        const float ref = m[rb] == -INFINITY ? 0.f : m[rb];      // then every score is -inf
+#pragma unroll
+                        for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                s[rb][pb][i] = exp2_fast(__builtin_fmaf(s[rb][pb][i], from, -ref));
+                                l[rb] += s[rb][pb][i];
+                            }
+                    }
+                }
+                if (team_edge) {
+                    // The tile is the team's: it looks over its values together.
+                    constexpr int MINE = TILE / TEAM;
+                    char *v = const_cast<char *>(vt);
+                    bool found = any_spoilt(v, part * MINE, MINE);
+                    if (TEAM > 1) found = __syncthreads_or(found);
+                    if (found) {
+                        const uint64_t rows = spoilt(v, 0, TILE);
+                        for (uint64_t left = rows; left && on; left &= left - 1) {
+                            const int r = __ffsll((unsigned long long)left) - 1;
+                            const int held = r / 32 * 16 + r % 32 / 8 * 4 + r % 4, owner = c + 32 * (r / 4 % 2);
+#pragma unroll
+                            for (int rb = 0; rb < RB; ++rb) {
+                                float x = 0.f;
+#pragma unroll
+                                for (int i = 0; i < 16 * PB; ++i) x = i == held ? s[rb][i / 16][i % 16] : x;
+                                x = __shfl(x, owner);
+                                if (!(sees[rb] >> r & 1)) continue;
+#pragma unroll
+                                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) {
+                                        const u32x2 y = *reinterpret_cast<const u32x2 *>(v + r * PITCH + 16 * ((4 * d + i) ^ swirl(r)) + 8 * e);
+                                        o[rb][d][4 * i] += x * V::lo(y[0]);
+                                        o[rb][d][4 * i + 1] += x * V::hi(y[0]);
+                                        o[rb][d][4 * i + 2] += x * V::lo(y[1]);
+                                        o[rb][d][4 * i + 3] += x * V::hi(y[1]);
+                                    }
+                            }
+                        }
+                        if (TEAM > 1) __syncthreads();
+                        for (int r = part * MINE; r < (part + 1) * MINE; ++r)
+                            if (rows >> r & 1)
+                                for (int x = lane; x < DK / 8; x += 64) *reinterpret_cast<u32x4 *>(v + r * PITCH + 16 * x) = u32x4{0, 0, 0, 0};
+                        if (TEAM > 1) __syncthreads();
+                        else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    }
+                }
+                if (on) {
+#pragma unroll
+                    for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+                        for (int s2 = 0; s2 < 2; ++s2) {
+                            u32x4 a[RB], rest[RB];
+#pragma unroll
+                            for (int rb = 0; rb < RB; ++rb) {
+                                float x[8];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) x[i] = s[rb][pb][8 * s2 + i];
+                                if (PARTS) split<F16>(x, a[rb], rest[rb]);
+                                else a[rb] = u32x4{V::pack(x[0], x[1]), V::pack(x[2], x[3]), V::pack(x[4], x[5]), V::pack(x[6], x[7])};
+                            }
+#pragma unroll
+                            for (int d = 0; d < DB; ++d) {
+                                const u32x4 v = columns(vt, pb, s2, d);
+#pragma unroll
+                                for (int rb = 0; rb < RB; ++rb) {
+                                    o[rb][d] = mfma32<F16>(v, a[rb], o[rb][d]);
+                                    if (PARTS) o[rb][d] = mfma32<F16>(v, rest[rb], o[rb][d]);
+                                }
+                            }
+                        }
+                }
+                here = next;
+                if (more) put(buf ^ 1, part);
+            }
+        }
+        if (bad && p.err) atomicOr(p.err, bad);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) l[rb] += __shfl_xor(l[rb], 32);
+
+        // Join the wavefronts of the same rows: each scales to the common maximum, then they
+        // add up in LDS, one after the other.
+        if (TEAM == 1 && streams > 1) {
+            if (e == 0) {
+                ml[(wave * 32 + c) * 2] = m[0];
+                ml[(wave * 32 + c) * 2 + 1] = l[0];
+            }
+            __syncthreads();
+            float top = -INFINITY, sum = 0.f;
+            for (int k = 0; k < streams; ++k) top = fmaxf(top, ml[(k * 32 + c) * 2]);
+            for (int k = 0; k < streams; ++k) sum += ml[(k * 32 + c) * 2 + 1] * weight(ml[(k * 32 + c) * 2], top);
+            const float f = weight(m[0], top);
+            m[0] = top;
+            l[0] = sum;
+            f32x4 *joined = reinterpret_cast<f32x4 *>(all_lds) + lane;         // [value / 4][lane]
+            for (int turn = 0; turn < streams; ++turn) {
+                if (wave == turn) {
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) {
+                        o[0][d] *= f;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            f32x4 x = {o[0][d][4 * i], o[0][d][4 * i + 1], o[0][d][4 * i + 2], o[0][d][4 * i + 3]};
+                            if (turn > 0) x += joined[64 * (4 * d + i)];
+                            if (turn < streams - 1) joined[64 * (4 * d + i)] = x;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) o[0][d][4 * i + j] = x[j];
+                        }
+                    }
+                }
+                __syncthreads();
+            }
+            if (wave != streams - 1) return;
+        }
+        const float v_scale = p.scales ? p.scales[(p.pool.C - 1) * p.pool.H + h] : 1.f;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            const int x = x0 + 32 * rb + c;
+            if (x >= n_rows) continue;
+            const int i = fd_div(p.fd_G, x), head = h * G + x - i * G;
+            if (piece.place < 0) {
+                const float f = l[rb] == 0.f ? 0.f : v_scale / l[rb];
+                if (p.lse && e == 0)
+                    p.lse[(rec.row_off + i) * p.pool.H * G + head] =
+                        l[rb] > 0.f || l[rb] != l[rb] ? (m[rb] + __builtin_amdgcn_logf(l[rb])) * kLn2 : -INFINITY;
+                char *dst = p.out.base + (rec.row_off + i) * p.out.s_row + head * p.out.s_head;
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int at = 32 * d + 8 * j + 4 * e;
+                        if (at < p.Dv)
+                            *reinterpret_cast<u32x2 *>(dst + 2 * at) = u32x2{V::pack(o[rb][d][4 * j] * f, o[rb][d][4 * j + 1] * f),
+                                                                            V::pack(o[rb][d][4 * j + 2] * f, o[rb][d][4 * j + 3] * f)};
+                    }
+            } else {
+                const int64_t row = piece.place * p.rows + x - block0;
+                if (e == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * row) = make_float2(m[rb], l[rb]);
+                float *dst = p.part_o + row * p.Dv;
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int at = 32 * d + 8 * j + 4 * e;
+                        if (at < p.Dv)
+                            *reinterpret_cast<f32x4 *>(dst + at) = f32x4{o[rb][d][4 * j], o[rb][d][4 * j + 1], o[rb][d][4 * j + 2], o[rb][d][4 * j + 3]};
+                    }
+            }
+        }
+    }
+};
+
+template <bool F16, bool E4M3, int DK, int DV, int RB, int TEAM, int TILE, bool GENERAL>
+__global__ void __launch_bounds__(256, 1) kvx_queries_kernel(QueriesParams p, int64_t first, int32_t n) {
+    __shared__ int64_t before[kQueriesGroup + 1];        // steps of one cache head of the records before
+    __shared__ __align__(16) int64_t row_off[4][TILE];
+    __shared__ float depth[4][KVX_MAX_DRAFTS];
+    __shared__ float ml[4 * 32 * 2];
+    __shared__ int64_t sums[4];
+    extern __shared__ __align__(256) char lds[];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), H = p.pool.H;
+    const int tile_bytes = TILE * 2 * DK * p.pool.C;
+    Queries<F16, E4M3, DK, DV, RB, TEAM, TILE, GENERAL> work{p, row_off[wave], depth[wave],
+                                                              lds + (TEAM > 1 ? 0 : wave * 2 * tile_bytes), ml, lds, lane, wave,
+                                                              lane & 31, lane >> 5, p.pool.C == 2, tile_bytes};
+    work.address();
+    const kvx_queries_req *reqs = p.whole ? p.reqs : p.reqs + first;
+    int64_t at = 0, stop = 1, each = 0;
+    int share = 0;
+    if (!p.whole) {
+        // steps of the records before each
+        const int threads = blockDim.x, some = (n + threads - 1) / threads;
+        int64_t sum = 0;
+        for (int r = threadIdx.x * some; r < (int)(threadIdx.x + 1) * some && r < n; ++r) {
+            before[r] = steps_of_head(reqs[r], p);
+            sum += before[r];
+        }
+        int64_t upto = sum;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int64_t x = __shfl_up(upto, d);
+            if (lane >= d) upto += x;
+        }
+        if (lane == 63) sums[wave] = upto;
+        __syncthreads();
+        for (int k = 0; k < wave; ++k) upto += sums[k];
+        upto -= sum;
+        for (int r = threadIdx.x * some; r < (int)(threadIdx.x + 1) * some && r < n; ++r) {
+            const int64_t x = before[r];
+            before[r] = upto;
+            upto += x;
+        }
+        if ((int)threadIdx.x == threads - 1) before[n] = upto;
+        __syncthreads();
+        // successive shares on one die
+        share = p.shares % 8 == 0 ? blockIdx.x % 8 * (p.shares / 8) + blockIdx.x / 8 : blockIdx.x;
+        const int64_t total = scalar(before[n]) * H;
+        each = share_of(total, p.shares);
+        if (share == 0) {
+            if (threadIdx.x == 0) *p.total = total;
+            for (int r = threadIdx.x; r < n; r += blockDim.x)
+                if (p.err && !valid(reqs[r], p)) atomicOr(p.err, KVX_DERR_BAD_REQ);
+        }
+        at = share * each;
+        stop = at + each < total ? at + each : total;
+    }
+    while (at < stop) {
+        Piece piece;
+        Span s;
+        int64_t here = 1;
+        if (p.whole) {
+            // Longest first: a record's last blocks see most.  Blocks of a record and head are n_reqs x H
+            // workgroups apart: with a multiple of 8 of them on one die, whose cache holds their keys.
+            const int64_t id = first + blockIdx.x, lists = (int64_t)p.n_reqs * H, rank = quotient(id, lists);
+            const int list = (int)(id - rank * lists), r = list / H;
+            piece.h = list - r * H;
+            piece.rec = scalar(reqs[r]);
+            if (!valid(piece.rec, p)) {
+                if (rank == 0 && piece.h == 0 && threadIdx.x == 0 && p.err) atomicOr(p.err, KVX_DERR_BAD_REQ);
+                return;
+            }
+            const int blocks = blocks_of(piece.rec, p);
+            if (rank >= blocks) return;
+            piece.b = blocks - 1 - (int)rank;
+            s = span_of_block(piece.rec, p, piece.b);
+            piece.place = -1;
+            piece.begin = s.lo & -kTile;
+            piece.end = s.hi;
+        } else {
+            int lo = 0, hi = n;          // the record: the last one whose steps begin at or before `at`
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) / 2;
+                if (before[mid] * H <= at) lo = mid;
+                else hi = mid;
+            }
+            const int r = __builtin_amdgcn_readfirstlane(lo);
+            const int64_t base = scalar(before[r]) * H, per = scalar(before[r + 1]) - scalar(before[r]);
+            piece.rec = scalar(reqs[r]);
+            piece.h = (int)quotient(at - base, per);
+            int64_t in = at - base - piece.h * per;
+            int steps;
+            for (piece.b = 0;; ++piece.b) {
+                s = span_of_block(piece.rec, p, piece.b);
+                steps = steps_of(s, p);
+                if (in < steps) break;
+                in -= steps;
+            }
+            here = stop - at < steps - in ? stop - at : steps - in;
+            piece.place = here < steps ? place_of(at - in, share, each, p.shares) : -1;
+            piece.begin = (s.lo & -kTile) + (uint32_t)in * p.step;
+            const uint32_t to = piece.begin + (uint32_t)here * p.step;
+            piece.end = to < s.hi ? to : s.hi;
+            if (in == 0 && threadIdx.x == 0) p.units[((int64_t)r * H + piece.h) * p.blocks + piece.b] = UnitSteps{at, steps};
+        }
+        if (s.hi <= s.lo) piece.end = piece.begin;
+        work.run(piece);
+        at += here;
+        __syncthreads();                 // the next piece uses the same LDS
+    }
+}
+
+// Bytes of LDS of a workgroup's tiles.
+inline size_t lds_bytes(const QueriesParams &p, int dk, int tile) {
+    return (size_t)2 * tile * 2 * dk * p.pool.C * (p.waves / p.team);
+}
+
+template <bool F16, bool E4M3, int DK, int DV, int RB, int TEAM, int TILE>
+int launch_form(const QueriesParams &p, int64_t first, int64_t n, hipStream_t stream) {
+    // scales of 0 and the sign are the kernel's; what it does to scores beyond them is GENERAL
+    const bool general = p.cap > 0.f || p.slopes;
+    const auto kernel = TEAM == 1 || general ? kvx_queries_kernel<F16, E4M3, DK, DV, RB, TEAM, TILE, true>
+                                             : kvx_queries_kernel<F16, E4M3, DK, DV, RB, TEAM, TILE, TEAM == 1>;
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.whole ? n : p.shares)), dim3(64 * p.waves), lds_bytes(p, DK, TILE), stream, p,
+                       first, (int32_t)n);
+    return hipGetLastError();
+}
+
+template <bool F16, bool E4M3>
+int launch_type(const QueriesParams &p, int64_t first, int64_t n, hipStream_t stream) {
+    const int D = p.pool.D;
+    if (p.team == 1) {
+        if (D <= 64) return launch_form<F16, E4M3, 64, 64, 1, 1, 32>(p, first, n, stream);
+        if (D <= 128) return launch_form<F16, E4M3, 128, 128, 1, 1, 32>(p, first, n, stream);
+        if (D <= 256) return launch_form<F16, E4M3, 256, 256, 1, 1, 32>(p, first, n, stream);
+        return launch_form<F16, E4M3, 576, 512, 1, 1, 32>(p, first, n, stream);
+    }
+    if (D <= 64) return launch_form<F16, E4M3, 64, 64, 2, 4, 64>(p, first, n, stream);
+    if (D <= 128)
+        return p.rows == 128 ? launch_form<F16, E4M3, 128, 128, 1, 4, 64>(p, first, n, stream)
+                             : launch_form<F16, E4M3, 128, 128, 2, 4, 64>(p, first, n, stream);
+    if (D <= 256) return launch_form<F16, E4M3, 256, 256, 1, 4, 64>(p, first, n, stream);
+    return launch_form<F16, E4M3, 576, 512, 1, 4, 32>(p, first, n, stream);
+}
+
+}  // namespace
+
+}  // namespace kvx

@@ -1,0 +1,209 @@
+// kvx_queries.hip -- attention of several queries of a request over a paged cache
+// (gfx950): the division of the work, the launches, and the second kernel, which
+// joins the parts of units that lie in several shares.
+
+#include "kvx_queries.h"
+
+namespace kvx {
+namespace {
+
+constexpr int kThreads = 256;
+
+// A workgroup joins some rows of a unit: out = sum 2^(m_c - M) o_c / sum 2^(m_c - M) l_c.
+// Dv / 4 threads side by side take a row's values; `split` such rows of threads share its
+// parts and add up in LDS.
+template <bool F16>
+__global__ void __launch_bounds__(kThreads) kvx_queries_join_kernel(QueriesParams p, int64_t r0, int64_t first, int32_t runs,
+                                                                    int32_t split) {
+    extern __shared__ __align__(16) float sums[];        // [row of threads][Dv], then their m and l
+    const int64_t id = first + blockIdx.x, unit = id / runs;
+    const int run = (int)(id - unit * runs), H = p.pool.H, G = p.fd_G.d;
+    const int64_t list = unit / p.blocks;
+    const int b = (int)(unit - list * p.blocks), r = (int)(list / H), h = (int)(list - (int64_t)r * H);
+    const kvx_queries_req rec = p.reqs[r0 + r];
+    if (!valid(rec, p) || b >= blocks_of(rec, p)) return;
+    const UnitSteps u = p.units[unit];
+    const int64_t each = share_of(*p.total, p.shares);
+    const int64_t k0 = quotient(u.first, each), k1 = quotient(u.first + u.steps - 1, each);
+    if (k0 == k1) return;                                // written by the first launch
+    const int cols = p.Dv / 4, lines = kThreads / cols, col = threadIdx.x % cols, line = threadIdx.x / cols;
+    const int per = lines / split, mine = line % split;
+    const int x = run * per + line / split;              // row of the block
+    const int64_t row = (int64_t)b * p.rows + x;
+    const bool on = line < per * split && x < p.rows && row < (int64_t)rec.n_queries * G;
+    float m = -INFINITY, l = 0.f;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    if (on) {
+        for (int64_t k = k0 + mine; k <= k1; k += 8 * split) {
+            f32x4 y[8];
+            float2 ml[8];
+            // all on their way at once; past the end the last one, without weight
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int64_t part = k + i * split <= k1 ? k + i * split : k1;
+                const int64_t at = place_of(u.first, part, each, p.shares) * p.rows + x;
+                ml[i] = *reinterpret_cast<const float2 *>(p.part_ml + 2 * at);
+                y[i] = *reinterpret_cast<const f32x4 *>(p.part_o + at * p.Dv + 4 * col);
+            }
+            float top = m;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, ml[i].x);
+            const float f = weight(m, top);
+            m = top;
+            l *= f;
+            sum *= f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (k + i * split > k1) continue;
+                const float w = weight(ml[i].x, m);
+                l += ml[i].y * w;
+                sum += y[i] * w;
+            }
+        }
+    }
+    if (split > 1) {
+        float *ml = sums + (int64_t)lines * p.Dv;
+        if (line < lines) {
+            *reinterpret_cast<f32x4 *>(sums + line * p.Dv + 4 * col) = sum;
+            if (col == 0) {
+                ml[2 * line] = m;
+                ml[2 * line + 1] = l;
+            }
+        }
+        __syncthreads();
+        if (!on || mine != 0) return;
+        float top = -INFINITY;
+        for (int k = 0; k < split; ++k) top = fmaxf(top, ml[2 * (line + k)]);
+        m = top;
+        l = 0.f;
+        sum = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < split; ++k) {
+            const float w = weight(ml[2 * (line + k)], m);
+            l += ml[2 * (line + k) + 1] * w;
+            sum += *reinterpret_cast<const f32x4 *>(sums + (line + k) * p.Dv + 4 * col) * w;
+        }
+    }
+    if (!on) return;
+    const int i = (int)(row / G), head = h * G + (int)(row - (int64_t)i * G);
+    if (p.lse && col == 0)
+        p.lse[(rec.row_off + i) * H * G + head] = l > 0.f || l != l ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    const float v_scale = p.scales ? p.scales[(p.pool.C - 1) * H + h] : 1.f;
+    sum *= l == 0.f ? 0.f : v_scale / l;
+    char *dst = p.out.base + (rec.row_off + i) * p.out.s_row + head * p.out.s_head;
+    *reinterpret_cast<u32x2 *>(dst + 8 * col) = u32x2{Half<F16>::pack(sum[0], sum[1]), Half<F16>::pack(sum[2], sum[3])};
+}
+
+constexpr int kResident = 256;           // workgroups that the device holds at a time
+// Units of up to this many steps, or this many units and more, are not split.
+constexpr int kWholeSteps = 8;
+constexpr int kWholeUnits = 4 * kResident;
+// Fewer steps than this are not worth a share.
+constexpr int kLeastShare = 4;
+
+int tile_of(const QueriesParams &p) { return p.team == 1 || p.pool.D > 256 ? 32 : 64; }
+
+// The kernel for records of up to `most` rows a cache head, and its shape.
+void shape(QueriesParams &p, int64_t most) {
+    const int D = p.pool.D;
+    // Up to 32 rows: wavefronts take positions of their own; as many as LDS holds tiles for.
+    p.team = most <= 32 ? 1 : 4;
+    p.waves = p.team == 4 || D <= 128 ? 4 : D <= 256 || p.pool.C == 1 ? 2 : 1;
+    p.rows = p.team == 1 ? 32 : D <= 64 || (D <= 128 && most > 128) ? 256 : 128;
+    p.step = tile_of(p) * (p.waves / p.team);
+    p.blocks = (int32_t)((most + p.rows - 1) / p.rows);
+    if (p.blocks < 1) p.blocks = 1;
+}
+
+int64_t most_steps(const QueriesParams &p) { return ((int64_t)p.max_tokens + kTile - 1 + p.step - 1) / p.step; }
+
+// Shares for so many units of the longest records.
+int32_t shares_for(const QueriesParams &p, int64_t units) {
+    const int64_t steps = most_steps(p), n = (units * (steps > 0 ? steps : 1) + kLeastShare - 1) / kLeastShare;
+    return (int32_t)(n < kResident ? (n > 0 ? n : 1) : kResident);
+}
+
+// Workspace of `units` units.
+int64_t split_bytes(const QueriesParams &p, int64_t units) {
+    // two parts a share, its first and its last
+    const int64_t rows = 2 * (int64_t)p.shares * p.rows;
+    return 16 + units * (int64_t)sizeof(UnitSteps) + rows * 8 + rows * p.Dv * 4 + 64;
+}
+
+int64_t units_of(const QueriesParams &p) {
+    return (p.n_reqs < kQueriesGroup ? p.n_reqs : (int64_t)kQueriesGroup) * p.pool.H * p.blocks;
+}
+
+}  // namespace
+
+void plan_queries(QueriesParams &p) {
+    shape(p, (int64_t)p.max_queries * p.fd_G.d);
+    p.whole = most_steps(p) <= kWholeSteps || (int64_t)p.n_reqs * p.pool.H * p.blocks >= kWholeUnits;
+    p.shares = shares_for(p, units_of(p));
+}
+
+int64_t queries_workspace_most(const QueriesParams &p0) {
+    // Fewer queries may take another kernel, fewer records or positions make more or less whole:
+    // of each kernel the most units that are split.
+    const int64_t most = (int64_t)p0.max_queries * p0.fd_G.d;
+    int64_t bytes = 0;
+    for (const int64_t rows : {most < 32 ? most : 32, most < 128 ? most : 128, most}) {
+        QueriesParams p = p0;
+        shape(p, rows);
+        const int64_t units = units_of(p) < kWholeUnits ? units_of(p) : kWholeUnits;
+        p.shares = shares_for(p, units);
+        const int64_t need = split_bytes(p, units);
+        if (need > bytes) bytes = need;
+    }
+    return bytes;
+}
+
+int64_t queries_workspace(QueriesParams &p, char *base) {
+    int64_t at = 0;
+    const auto take = [&](int64_t bytes) {
+        char *x = base ? base + at : nullptr;
+        at += (bytes + 15) / 16 * 16;
+        return x;
+    };
+    const int64_t rows = 2 * (int64_t)p.shares * p.rows;
+    p.total = reinterpret_cast<int64_t *>(take(16));
+    if (p.whole) return at;
+    p.units = reinterpret_cast<UnitSteps *>(take(units_of(p) * (int64_t)sizeof(UnitSteps)));
+    p.part_ml = reinterpret_cast<float *>(take(rows * 8));
+    p.part_o = reinterpret_cast<float *>(take(rows * p.Dv * 4));
+    return at;
+}
+
+int launch_queries(const QueriesParams &p, hipStream_t stream) {
+    const auto launch = p.f16 ? (p.e4m3 ? launch_queries_f16_e4m3 : launch_queries_f16)
+                              : (p.e4m3 ? launch_queries_bf16_e4m3 : launch_queries_bf16);
+    int e;
+    if (p.whole) {
+        const int64_t units = (int64_t)p.n_reqs * p.pool.H * p.blocks;
+        for (int64_t at = 0; at < units; at += kMaxBlocks) {
+            const int64_t n = units - at < kMaxBlocks ? units - at : kMaxBlocks;
+            if ((e = launch(p, at, n, stream)) != hipSuccess) return e;
+        }
+        return hipSuccess;
+    }
+    for (int64_t r0 = 0; r0 < p.n_reqs; r0 += kQueriesGroup) {
+        const int64_t n = p.n_reqs - r0 < kQueriesGroup ? p.n_reqs - r0 : kQueriesGroup;
+        if ((e = launch(p, r0, n, stream)) != hipSuccess) return e;
+        const int64_t units = n * p.pool.H * p.blocks;
+        // Rows of threads that share a row's parts: as many as there are parts, on average.
+        const int lines = kThreads / (p.Dv / 4);
+        int split = 1;
+        while (2 * split <= lines && units * 8 * split < p.shares) split *= 2;
+        const int rows = p.blocks == 1 && (int64_t)p.max_queries * p.fd_G.d < p.rows ? p.max_queries * p.fd_G.d : p.rows;
+        const int32_t runs = (rows + lines / split - 1) / (lines / split);
+        const size_t lds = split > 1 ? sizeof(float) * lines * (p.Dv + 2) : 0;
+        for (int64_t at = 0; at < units * runs; at += kMaxBlocks) {
+            const int64_t some = units * runs - at < kMaxBlocks ? units * runs - at : kMaxBlocks;
+            hipLaunchKernelGGL(p.f16 ? kvx_queries_join_kernel<true> : kvx_queries_join_kernel<false>, dim3((uint32_t)some),
+                               dim3(kThreads), lds, stream, p, r0, at, runs, split);
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+        }
+    }
+    return hipSuccess;
+}
+
+}  // namespace kvx

@@ -1,0 +1,55 @@
+// kvx_queries_plan.h -- attention of several queries of a request: launch parameters
+// and the division of the work.  Not part of the public interface (include/kvx.h).
+#pragma once
+
+#include "kvx_ops.h"
+
+namespace kvx {
+
+// Records of one launch with shares.
+#ifndef KVX_QUERIES_GROUP
+#define KVX_QUERIES_GROUP 512
+#endif
+constexpr int kQueriesGroup = KVX_QUERIES_GROUP;
+
+// Where a unit's steps lie among all steps of a launch with shares.
+struct UnitSteps {
+    int64_t first, steps;
+};
+
+struct QueriesParams {
+    Layer pool;
+    const float *scales;
+    Rows q, out;
+    int64_t num_rows;            // of q and out, the fewer
+    int32_t Dv;
+    float scale, cap;            // cap 0: none
+    const float *slopes;
+    int32_t window;              // 0: none
+    float *lse;
+    const kvx_queries_req *reqs;
+    const uint64_t *tree;        // nullptr: prompts
+    int32_t n_reqs, max_queries, max_tokens;
+    uint32_t *err;
+    int32_t f16, e4m3;
+    FastDiv fd_G;
+    // launch: wavefronts of a workgroup, and how many share a tile; rows of a block,
+    // blocks of a record and cache head at most; positions of a step; whether every
+    // unit has its own workgroup (whole), else the shares of the steps
+    int32_t waves, team, rows, blocks, step, whole, shares;
+    // workspace
+    int64_t *total;              // steps of the launch
+    UnitSteps *units;            // [record of the launch][cache head][block]
+    float *part_ml;              // [place][row][2]
+    float *part_o;               // [place][row][Dv]
+};
+
+// The division of a call's work, from the sizes alone; the workspace of a planned
+// call: its parts at `base`, or without one the bytes that serve it.
+void plan_queries(QueriesParams &p);
+int64_t queries_workspace(QueriesParams &p, char *base);
+// Bytes that serve every call of up to so many records, queries and positions.
+int64_t queries_workspace_most(const QueriesParams &p);
+int launch_queries(const QueriesParams &p, hipStream_t stream);
+
+}  // namespace kvx

@@ -7,8 +7,10 @@ The functions keep the C names: ``kvx_transfer``, ``kvx_transfer_slice``,
 ``kvx_transfer_layered``, ``kvx_transfer_planned``,
 ``kvx_transfer_layered_planned``, ``kvx_gather``, ``kvx_scatter``,
 ``kvx_gather_slice``, ``kvx_scatter_slice`` and ``kvx_page_hashes``, and the
-calls of a decode step over a paged cache, ``kvx_append``, ``kvx_attend``,
-``kvx_select_kept`` and ``kvx_transfer_kept``.  A missing or unloadable
+calls that compute with a paged cache, ``kvx_append``, ``kvx_attend``,
+``kvx_select_kept`` and ``kvx_transfer_kept`` for a decode step, and
+``kvx_append_normed``, ``kvx_attend_prompt``, ``kvx_attend_tree`` and
+``kvx_keep_path`` for several tokens of a request.  A missing or unloadable
 library raises; there is no fallback path.
 
 Pool and buffer shapes are duck-typed: a pool shape has integer attributes
@@ -162,6 +164,16 @@ def load(path: str) -> ctypes.CDLL:
     L.kvx_last_launch.restype = ctypes.c_int
     L.kvx_append.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp, i64, vp, i32, i32, vp, vp]
     L.kvx_append.restype = ctypes.c_int
+    L.kvx_append_normed.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp, i32, i32, vp, vp]
+    L.kvx_append_normed.restype = ctypes.c_int
+    for f in (L.kvx_attend_prompt, L.kvx_attend_tree):
+        f.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, i64, vp] + [vp] * (f is L.kvx_attend_tree) + [i32, i32, i32, vp, i64,
+                                                                                                 vp, vp]
+        f.restype = ctypes.c_int
+    L.kvx_queries_workspace.argtypes = [vp, i32, i32, i32, i32, i32]
+    L.kvx_queries_workspace.restype = i64
+    L.kvx_keep_path.argtypes = [vp, vp, i64, vp, i32, i32, vp, i64, vp, vp]
+    L.kvx_keep_path.restype = ctypes.c_int
     L.kvx_attend.argtypes = [vp, i32, vp, vp, vp, vp, ctypes.c_float, vp, i64, vp, i32, i32, vp, i64, i64, vp, i64, vp,
                              vp]
     L.kvx_attend.restype = ctypes.c_int
@@ -861,3 +873,182 @@ def kvx_transfer_kept(src, src_spec, dst, dst_spec, src_pt, dst_pt, reqs, max_to
     kp, n_k = _table(kept, "kept")
     _check(lib().kvx_transfer_kept(S, D, X, spt, n_spt, dpt, n_dpt, reqs.data_ptr(), _n_reqs(reqs), int(max_tokens),
                                    kp, n_k, int(kept_stride), _err_word(dev_err), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# several tokens of a request
+# ---------------------------------------------------------------------------
+
+QUERIES_REQ_DTYPE = np.dtype([("pt_off", "<i8"), ("row_off", "<i8"), ("start", "<i4"), ("end", "<i4"),
+                              ("n_queries", "<i4"), ("prefix", "<i4")])
+PATH_REQ_DTYPE = np.dtype([("pt_off", "<i8"), ("path_off", "<i8"), ("start", "<i4"), ("n_tokens", "<i4")])
+MAX_DRAFTS = 64
+
+_NORM_PACK = struct.Struct("=Q2ifi").pack
+_POSITIONS_PACK = struct.Struct("=QqQ2i").pack
+_SCORES_PACK = struct.Struct("=Q2f2i").pack
+
+
+def device_queries_reqs(rows, device="cuda"):
+    """(pt_off, row_off, start, end, n_queries, prefix) rows as kvx_queries_req
+    records on the device."""
+    return _device(_pack(rows, QUERIES_REQ_DTYPE), device)
+
+
+def device_path_reqs(rows, device="cuda"):
+    """(pt_off, path_off, start, n_tokens) rows as kvx_path_req records on the device."""
+    return _device(_pack(rows, PATH_REQ_DTYPE), device)
+
+
+@dataclass(frozen=True)
+class Norm:
+    """A norm of each head (kvx_norm): ``weight`` a float32 device tensor of
+    factors, one for each normed element from ``off`` on; None for factors of
+    1, with ``dim`` elements.  A model that stores its factors less one adds
+    the one when it loads them."""
+    weight: Any = None
+    off: int = 0
+    eps: float = 1e-6
+    dim: int = 0
+
+
+def _norm_arg(norm, name: str):
+    if norm is None:
+        return None
+    ptr, n = _floats(norm.weight, name + ".weight")
+    if norm.weight is not None and norm.dim not in (0, n):
+        raise ValueError(f"{name}: dim {norm.dim}, but {n} weights")
+    return _NORM_PACK(ptr or 0, n if norm.weight is not None else int(norm.dim), int(norm.off), float(norm.eps), 0)
+
+
+def _positions_arg(positions, axis, k, rope):
+    """The kvx_positions of an int32 tensor [rows] or [axes, rows] and an optional
+    int32 tensor of each pair's axis."""
+    if positions is None:
+        if axis is not None:
+            raise ValueError("axis is given without positions")
+        return None
+    if positions.element_size() != 4 or positions.is_floating_point() or positions.dim() not in (1, 2):
+        raise ValueError(f"positions must be an int32 tensor [rows] or [axes, rows] (got {positions.dtype})")
+    axes = positions.shape[0] if positions.dim() == 2 else 1
+    if positions.shape[-1] != k.shape[0] or (positions.shape[-1] > 1 and positions.stride(-1) != 1):
+        raise ValueError(f"positions must have contiguous entries for k's {k.shape[0]} rows")
+    a, n = None, 0
+    if axis is not None:
+        a, n = _table(axis, "axis")
+        if rope is None or n != rope.freq.numel():
+            raise ValueError(f"axis holds {n} entries: one for each rotated pair is needed")
+    stride = positions.stride(0) if positions.dim() == 2 and axes > 1 else 0
+    return _POSITIONS_PACK(positions.data_ptr(), stride, a or 0, axes, 0)
+
+
+def kvx_append_normed(pool, spec, layer, k, v, pt, reqs, max_tokens, q=None, q_out=None, rope=None, q_norm=None,
+                      k_norm=None, positions=None, axis=None, scales=None, dev_err=None, stream=None) -> None:
+    """kvx_append with queries and keys normed per head before they are rotated,
+    and with positions of their own (see kvx_append_normed in include/kvx.h).
+    ``q_norm`` and ``k_norm`` a ``Norm`` or None; ``positions`` an int32 device
+    tensor [rows] or [axes, rows] or None (those of the records); ``axis`` an
+    int32 device tensor with the axis of each rotated pair, None for all on axis
+    0; everything else as ``kvx_append``."""
+    P = _pool_arg(spec, pool, "pool")
+    table, n_pt = _table(pt, "pt")
+    rec, n = _reqs_arg(reqs, APPEND_REQ_DTYPE)
+    R = None
+    if rope is not None:
+        f, pairs = _floats(rope.freq, "rope.freq")
+        R = _ROPE_PACK(f or 0, 2 * pairs, int(rope.rot_off), int(bool(rope.interleaved)), float(rope.amplitude))
+    _check(lib().kvx_append_normed(P, int(layer), _scales(scales, spec), None if q is None else _rows_arg(q, "q"),
+                                   None if q_out is None else _rows_arg(q_out, "q_out"), _rows_arg(k, "k"),
+                                   None if v is None else _rows_arg(v, "v"), R, _norm_arg(q_norm, "q_norm"),
+                                   _norm_arg(k_norm, "k_norm"), _positions_arg(positions, axis, k, rope), table, n_pt, rec, n,
+                                   int(max_tokens), _err_word(dev_err), _stream(stream)))
+
+
+@dataclass(frozen=True)
+class Scores:
+    """What becomes of q . k (kvx_scores): ``scale`` (None: head_dim ** -0.5),
+    ``cap`` (cap * tanh(s / cap); 0: none), ``slopes`` a float32 device tensor, one
+    for each query head, of a bias -slope * distance, ``window`` the positions seen
+    from a query back, its own included (0: all)."""
+    scale: Any = None
+    cap: float = 0.0
+    slopes: Any = None
+    window: int = 0
+
+
+def queries_workspace_bytes(spec, n_reqs: int, q_heads: int, max_queries: int, max_tokens: int, v_dim=None) -> int:
+    """kvx_queries_workspace for a pool shape; ``v_dim`` defaults to head_dim."""
+    n = int(lib().kvx_queries_workspace(bytes(pool_desc(spec, 0)), int(n_reqs), int(q_heads),
+                                        int(spec.D if v_dim is None else v_dim), int(max_queries), int(max_tokens)))
+    if n < 0:
+        raise KvxError(-5, lib().kvx_last_error().decode())
+    return n
+
+
+def queries_workspace(spec, n_reqs: int, q_heads: int, max_queries: int, max_tokens: int, v_dim=None, device="cuda"):
+    """A workspace for kvx_attend_prompt and kvx_attend_tree calls of up to
+    ``n_reqs`` records, ``max_queries`` queries and ``max_tokens`` positions each:
+    device memory, whatever it holds."""
+    import torch
+    return torch.empty(queries_workspace_bytes(spec, n_reqs, q_heads, max_queries, max_tokens, v_dim), dtype=torch.uint8,
+                       device=device)
+
+
+def _attend_queries(q, out, pool, spec, layer, pt, reqs, tree, max_queries, max_tokens, workspace, scores, scales, lse,
+                    dev_err, stream):
+    P = _pool_arg(spec, pool, "pool")
+    table, n_pt = _table(pt, "pt")
+    rec, n = _reqs_arg(reqs, QUERIES_REQ_DTYPE)
+    lse_ptr, n_lse = _floats(lse, "lse")
+    if lse is not None and n_lse < q.shape[0] * q.shape[1]:
+        raise ValueError(f"lse holds {n_lse} values, {q.shape[0]} rows x {q.shape[1]} heads need more")
+    s = scores or Scores()
+    slopes, n_slopes = _floats(s.slopes, "slopes")
+    if s.slopes is not None and n_slopes != q.shape[1]:
+        raise ValueError(f"slopes holds {n_slopes} values for {q.shape[1]} query heads")
+    if tree is not None and (tree.element_size() != 8 or tree.is_floating_point() or not tree.is_contiguous()
+                             or tree.numel() < q.shape[0]):
+        raise ValueError(f"tree must be a contiguous 64-bit integer tensor with an entry for each of {q.shape[0]} rows")
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    X = _SCORES_PACK(slopes or 0, float(spec.D ** -0.5 if s.scale is None else s.scale), float(s.cap), int(s.window), 0)
+    head = (P, int(layer), _scales(scales, spec), _rows_arg(q, "q"), _rows_arg(out, "out"), lse_ptr, X, table, n_pt, rec)
+    rest = (n, int(max_queries), int(max_tokens), workspace.data_ptr(), workspace.nbytes, _err_word(dev_err),
+            _stream(stream))
+    if tree is None:
+        return _check(lib().kvx_attend_prompt(*head, *rest))
+    _check(lib().kvx_attend_tree(*head, tree.data_ptr(), *rest))
+
+
+def kvx_attend_prompt(q, out, pool, spec, layer, pt, reqs, max_queries, max_tokens, workspace, scores=None, scales=None,
+                      lse=None, dev_err=None, stream=None) -> None:
+    """Attention of the last queries of each record's positions over a layer's
+    pages (see kvx_attend_prompt in include/kvx.h).  ``q`` [rows, q heads,
+    head_dim] and ``out`` [rows, q heads, v_dim]; ``reqs`` from
+    ``device_queries_reqs``; ``scores`` a ``Scores``; ``workspace`` from
+    ``queries_workspace``; ``lse`` an optional float32 tensor [rows, q heads]."""
+    _attend_queries(q, out, pool, spec, layer, pt, reqs, None, max_queries, max_tokens, workspace, scores, scales, lse,
+                    dev_err, stream)
+
+
+def kvx_attend_tree(q, out, pool, spec, layer, pt, reqs, tree, max_queries, max_tokens, workspace, scores=None,
+                    scales=None, lse=None, dev_err=None, stream=None) -> None:
+    """Attention of drafted tokens that form a tree (see kvx_attend_tree in
+    include/kvx.h): ``tree`` a 64-bit integer device tensor, for each row the bits
+    of the drafts that it sees, its ancestors and itself; everything else as
+    ``kvx_attend_prompt``."""
+    if tree is None:
+        raise ValueError("tree is needed")
+    _attend_queries(q, out, pool, spec, layer, pt, reqs, tree, max_queries, max_tokens, workspace, scores, scales, lse,
+                    dev_err, stream)
+
+
+def kvx_keep_path(pool, spec, pt, reqs, max_tokens, path, dev_err=None, stream=None) -> None:
+    """Accepted drafts' rows to the front of the drafts' slots, in every layer, in
+    place (see kvx_keep_path in include/kvx.h): ``reqs`` from
+    ``device_path_reqs``, ``path`` an int32 tensor of their ascending lists."""
+    P = _pool_arg(spec, pool, "pool")
+    table, n_pt = _table(pt, "pt")
+    rec, n = _reqs_arg(reqs, PATH_REQ_DTYPE)
+    pp, n_path = _table(path, "path")
+    _check(lib().kvx_keep_path(P, table, n_pt, rec, n, int(max_tokens), pp, n_path, _err_word(dev_err), _stream(stream)))
