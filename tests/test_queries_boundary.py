@@ -229,7 +229,7 @@ def test_definitions():
     rec = (0, 0, 2, 30, n, 0)
     for window in (0, 1, 4, 12):
         for i in range(n):
-            for t in range(32):
-                assert ref.sees(rec, i, t, window, bits) == ref.sees(rec, i, t, window, None) or t >= 30
+            for t in range(30):
+                assert ref.sees(rec, i, t, window, bits) == ref.sees(rec, i, t, window, None)
     x = np.random.default_rng(1).standard_normal((3, 64))
     assert np.allclose((ref.norm(x, np.ones(32), 16, 0.0)[:, 16:48] ** 2).mean(axis=-1), 1)
