@@ -164,11 +164,32 @@ __device__ __forceinline__ bool not_finite(uint32_t w) {
     return (w & e) == e || (w >> 16 & e) == e;
 }
 
-// DK: elements of a row in LDS (head_dim is up to that), DV: of a value; RB: blocks of 32
-// rows of a wavefront; TEAM: wavefronts that share a tile (4, the workgroup's, each with
-// its rows; or 1: each takes tiles of its own for the same rows, and they join at the
-// end); TILE: positions; GENERAL: scores may be capped or biased.
-template <bool F16, bool E4M3, int DK, int DV, int RB, int TEAM, int TILE, bool GENERAL>
+// The larger of three; what is not a number counts for nothing.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float x;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(x) : "v"(a), "v"(b), "v"(c));
+    return x;
+}
+
+// x of this lane and of the lane in the other half.
+__device__ __forceinline__ float max_of_halves(float x) {
+    const auto y = __builtin_amdgcn_permlane32_swap(bits<uint32_t>(x), bits<uint32_t>(x), false, false);
+    return fmaxf(bits<float>((uint32_t)y[0]), bits<float>((uint32_t)y[1]));
+}
+
+// The kernel's parameters, its first argument, read anew: kept from the kernel's begin to
+// its end they would take more scalar registers than there are.
+__device__ __forceinline__ QueriesParams again() {
+    const auto *p = (const __attribute__((address_space(4))) QueriesParams *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const QueriesParams *)p;
+}
+
+// DK: elements of a row in LDS (head_dim is up to that), DV: of a value; TEAM: wavefronts
+// that share a tile, each with 32 rows (all of the workgroup; or 1: each takes tiles of
+// its own for the same 32 rows, and they join at the end); TILE: positions; GENERAL: scores
+// may be capped or biased.
+template <bool F16, bool E4M3, int DK, int DV, int TEAM, int TILE, bool GENERAL>
 struct Queries {
     typedef Half<F16> V;
     static constexpr int KS = DK / 16, DB = DV / 32, PB = TILE / 32, PITCH = 2 * DK;
@@ -178,55 +199,64 @@ struct Queries {
     static constexpr uint64_t ALL = TILE == 64 ? ~0ull : 0xffffffffull;
     static_assert((E4M3 || LOADS * 64 * TEAM == TILE * SRC) && (TILE == 32 || TILE == 64), "tile");
 
-    const QueriesParams &p;
-    int64_t *row_off;            // [TILE], this wavefront's: the tile's that is asked for
-    float *depth;                // [64], this wavefront's
-    char *lds;                   // [2][rows of K, rows of V if there are two]
+    // Of TEAM tiles, and the next TEAM ones: row offsets (-1: none) and which are there.
+    struct Rows {
+        int64_t off[2][TEAM][TILE];
+        uint64_t there[2][TEAM];
+    };
+    Rows &rows;                  // the team's
+    float *depth;                // [64], the wavefront's
+    char *lds;                   // [2][rows of K, rows of V if there are two], the team's
     float *ml;                   // [wavefronts][32][2]
-    char *all_lds;
-    int lane, wave, c, e;
+    char *all_lds;               // the workgroup's
+    int lane, wave, part, c, e;  // part: of the team
     bool two;
     int tile_bytes;
     // of the piece
     kvx_queries_req rec;
     const char *kbase;
+    int64_t s_p, s_c, s_t, pt_len;
+    const int32_t *pt;
+    FastDiv fd_T;
+    int32_t N, have;             // pages; 16-byte chunks of a row
     uint32_t first, end, bad;
     u32x4 staged[E4M3 ? LOADS : 1][2];
 
-    __device__ __forceinline__ uint64_t entry(uint32_t t) const { return (uint64_t)rec.pt_off + fd_div(p.pool.fd_T, t); }
+    __device__ __forceinline__ uint64_t entry(uint32_t t) const { return (uint64_t)rec.pt_off + fd_div(fd_T, t); }
     // the page id of position t0 + lane
     __device__ __forceinline__ int32_t look(uint32_t t0) const {
         const uint32_t t = t0 + lane;
         const uint64_t idx = entry(t < end ? t : end - 1);
-        return p.pool.pt[idx < (uint64_t)p.pool.pt_len ? idx : 0];
+        return pt[idx < (uint64_t)pt_len ? idx : 0];
     }
-    // A tile's row offsets (-1: none) to LDS; the positions that are there.
-    __device__ __forceinline__ uint64_t resolve(uint32_t t0, int32_t page) {
+    // A tile's row offsets, to place `slot` of half `ring`.
+    __device__ __forceinline__ void resolve(uint32_t t0, int32_t page, int ring, int slot) {
         const uint32_t t = t0 + lane;
         const bool in = lane < TILE && t >= first && t < end;
         const uint32_t at = t < end ? t : end - 1;
-        const bool known = entry(at) < (uint64_t)p.pool.pt_len;
-        const bool ok = in && known && (uint32_t)page < (uint32_t)p.pool.N;
+        const bool known = entry(at) < (uint64_t)pt_len;
+        const bool ok = in && known && (uint32_t)page < (uint32_t)N;
         if (in && !ok) bad |= known ? KVX_DERR_SRC_PAGE : KVX_DERR_PT_RANGE;
-        const int64_t off = page * p.pool.s_p + (int64_t)(at - fd_div(p.pool.fd_T, at) * p.pool.fd_T.d) * p.pool.s_t;
-        if (TILE == 64 || lane < TILE) row_off[lane] = ok ? off : -1;
+        const int64_t off = page * s_p + (int64_t)(at - fd_div(fd_T, at) * fd_T.d) * s_t;
+        if (TILE == 64 || lane < TILE) rows.off[ring][slot][lane] = ok ? off : -1;
+        const uint64_t there = __ballot(ok);
+        if (lane == 0) rows.there[ring][slot] = there;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        return (uint64_t)__ballot(ok);
     }
-    // Asks for a tile's rows, zeros where there is none and behind head_dim.
-    __device__ __forceinline__ void load(int buf, int part) {
-        const int have = (E4M3 ? 1 : 2) * p.pool.D / 16, ln = lane_again();
+    // Asks for this wavefront's share of a tile's rows, zeros where there is none and behind head_dim.
+    __device__ __forceinline__ void load(int buf, const int64_t *off_of) {
         const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)(lds + buf * tile_bytes);
+        const int ln = lane_again();
 #pragma unroll
         for (int x = 0; x < LOADS; ++x) {
             const int u = (part * LOADS + x) * 64 + ln, row = u / SRC;
             int chunk = u % SRC;
             if (!E4M3) chunk ^= swirl(row);
             if (LOADS * 64 * TEAM != TILE * SRC && row >= TILE) chunk = have;
-            const int64_t off = row_off[LOADS * 64 * TEAM != TILE * SRC ? row & (TILE - 1) : row];
+            const int64_t off = off_of[LOADS * 64 * TEAM != TILE * SRC ? row & (TILE - 1) : row];
             const bool ok = off >= 0 && chunk < have;
             const char *k = ok ? kbase + off + 16 * chunk : reinterpret_cast<const char *>(&kvx_zeros);
-            const char *v = ok ? k + p.pool.s_c : k;
+            const char *v = ok ? k + s_c : k;
             if constexpr (E4M3) {
                 staged[x][0] = *reinterpret_cast<const u32x4 *>(k);
                 if (two) staged[x][1] = *reinterpret_cast<const u32x4 *>(v);
@@ -238,7 +268,7 @@ struct Queries {
         }
     }
     // e4m3: what load() has brought, widened, to LDS.
-    __device__ __forceinline__ void put(int buf, int part) {
+    __device__ __forceinline__ void put(int buf) {
         if constexpr (E4M3) {
             char *to = lds + buf * tile_bytes;
             const int ln = lane_again();
@@ -292,16 +322,16 @@ struct Queries {
 
     // Rows r0 .. r0 + n - 1 of V that hold values which are not finite.
     __device__ __forceinline__ uint64_t spoilt(const char *v, int r0, int n) const {
-        uint64_t rows = 0;
+        uint64_t found_rows = 0;
         for (int r = r0; r < r0 + n; ++r) {
             bool found = false;
             if (lane < DV / 8) {
                 const u32x4 w = *reinterpret_cast<const u32x4 *>(v + r * PITCH + 16 * (lane ^ swirl(r)));
                 found = not_finite<F16>(w[0]) || not_finite<F16>(w[1]) || not_finite<F16>(w[2]) || not_finite<F16>(w[3]);
             }
-            if (__any(found)) rows |= 1ull << r;
+            if (__any(found)) found_rows |= 1ull << r;
         }
-        return rows;
+        return found_rows;
     }
     __device__ __forceinline__ bool any_spoilt(const char *v, int r0, int n) const {
         bool found = false;
@@ -316,195 +346,210 @@ struct Queries {
 
     __device__ __forceinline__ void run(const Piece &piece) {
         rec = piece.rec;
-        const int G = p.fd_G.d, h = piece.h, n_rows = rec.n_queries * G, base = rec.end - rec.n_queries;
-        const int part = TEAM > 1 ? wave : 0, streams = p.waves / TEAM;
-        kbase = p.pool.base + h * p.pool.s_h;
+        const int base = rec.end - rec.n_queries;
         const uint32_t begin = piece.begin;
         end = piece.end;
         first = rec.start;
         bad = 0;
-
-        // Scores are taken times unit > 0: a sign goes into the queries.
-        float unit = p.scale * (p.scales ? p.scales[h] : 1.f) * kLog2e;
-        const uint32_t flip = unit < 0.f ? 0x80008000u : 0;
-        const bool none = unit == 0.f;
-        unit = none ? 1.f : fabsf(unit);
-        const float cap2 = p.cap * kLog2e, cap_unit = GENERAL && p.cap > 0.f ? 2.f * unit / p.cap : 0.f;
-
-        // This lane's row of each block of 32; past the last one, that one once more.
-        const int block0 = piece.b * p.rows, x0 = block0 + part * 32 * RB;
-        const bool active = x0 < n_rows;
-        int at[RB];                      // its position
-        uint32_t lo[RB], hi[RB];         // it sees [lo, hi)
-        uint64_t drafts[RB];             // and these drafts
-        float slope[RB];
-        u32x4 qv[RB][KS];
-        if (p.tree) {
-            if (lane < rec.n_queries) {
-                const int k = __popcll(p.tree[rec.row_off + lane] & ones(rec.n_queries));
-                depth[lane] = k > 0 ? k - 1 : 0;
-            }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        }
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            const int x = x0 + 32 * rb + c, row = x < n_rows ? x : n_rows - 1;
-            const int i = fd_div(p.fd_G, row), g = row - i * G;
-            at[rb] = base + i;
-            drafts[rb] = 0;
-            if (p.tree) {
-                const int mine = (int)depth[i];
-                at[rb] = base + mine;
-                drafts[rb] = p.tree[rec.row_off + i] & ones(rec.n_queries) & ~ones((int64_t)rec.start - base);
-                if (p.window)
-                    for (int j = 0; j < rec.n_queries; ++j)
-                        if (mine - (int)depth[j] >= p.window) drafts[rb] &= ~(1ull << j);
-            }
-            const int near = at[rb] - p.window + 1;
-            lo[rb] = p.window && near > rec.start ? near : rec.start;
-            const int seen = p.tree ? base : at[rb] + 1 > rec.prefix ? at[rb] + 1 : rec.prefix;
-            hi[rb] = seen < rec.end ? seen : rec.end;
-            slope[rb] = GENERAL && p.slopes ? p.slopes[h * G + g] * kLog2e : 0.f;
-            const char *src = p.q.base + (rec.row_off + i) * p.q.s_row + (int64_t)(h * G + g) * p.q.s_head;
-#pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                const int d = 16 * k + 8 * e;
-                qv[rb][k] = u32x4{0, 0, 0, 0};
-                if (d < p.pool.D && !none) qv[rb][k] = *reinterpret_cast<const u32x4 *>(src + 2 * d);
-#pragma unroll
-                for (int w = 0; w < 4; ++w) qv[rb][k][w] ^= flip;
-            }
-        }
+        int x0, streams, h_rows;
+        bool active;
+        // This lane's row; past the last one, that one once more.
+        int at;                          // its position
+        uint32_t lo, hi;                 // it sees [lo, hi)
+        uint64_t drafts = 0;             // and these drafts
+        float slope = 0.f, cap2 = 0.f, cap_unit = 0.f, unit;
+        bool is_tree, biased;
+        u32x4 qv[KS];
         // Positions that all rows of the wavefront see, that some see, and that all of the
         // workgroup see.  In a tree depths differ within a block: the drafts and the last
         // position's window bound them.
         Span all, some, block_all;
         {
+            const QueriesParams p = again();
+            const int G = p.fd_G.d, h = piece.h, n_rows = rec.n_queries * G;
+            h_rows = n_rows;
+            streams = p.waves / TEAM;
+            kbase = p.pool.base + h * p.pool.s_h;
+            s_p = p.pool.s_p;
+            s_c = p.pool.s_c;
+            s_t = p.pool.s_t;
+            pt = p.pool.pt;
+            pt_len = p.pool.pt_len;
+            fd_T = p.pool.fd_T;
+            N = p.pool.N;
+            have = (E4M3 ? 1 : 2) * p.pool.D / 16;
+            is_tree = p.tree;
+            biased = GENERAL && p.slopes;
+            // Scores are taken times unit > 0: a sign goes into the queries.
+            unit = p.scale * (p.scales ? p.scales[h] : 1.f) * kLog2e;
+            const uint32_t flip = unit < 0.f ? 0x80008000u : 0;
+            const bool none = unit == 0.f;
+            unit = none ? 1.f : fabsf(unit);
+            if (GENERAL && p.cap > 0.f) {
+                cap2 = p.cap * kLog2e;
+                cap_unit = 2.f * unit / p.cap;
+            }
+            const int block0 = piece.b * p.rows;
+            x0 = block0 + part * 32;
+            active = x0 < n_rows;
+            if (is_tree) {
+                if (lane < rec.n_queries) {
+                    const int k = __popcll(p.tree[rec.row_off + lane] & ones(rec.n_queries));
+                    depth[lane] = k > 0 ? k - 1 : 0;
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            }
+            const int x = x0 + c, row = x < n_rows ? x : n_rows - 1;
+            const int i = fd_div(p.fd_G, row), g = row - i * G;
+            at = base + i;
+            if (is_tree) {
+                const int mine = (int)depth[i];
+                at = base + mine;
+                drafts = p.tree[rec.row_off + i] & ones(rec.n_queries) & ~ones((int64_t)rec.start - base);
+                if (p.window)
+                    for (int j = 0; j < rec.n_queries; ++j)
+                        if (mine - (int)depth[j] >= p.window) drafts &= ~(1ull << j);
+            }
+            const int near = at - p.window + 1;
+            lo = p.window && near > rec.start ? near : rec.start;
+            const int seen = is_tree ? base : at + 1 > rec.prefix ? at + 1 : rec.prefix;
+            hi = seen < rec.end ? seen : rec.end;
+            if (biased) slope = p.slopes[h * G + g] * kLog2e;
+            const char *src = p.q.base + (rec.row_off + i) * p.q.s_row + (int64_t)(h * G + g) * p.q.s_head;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const int d = 16 * k + 8 * e;
+                qv[k] = u32x4{0, 0, 0, 0};
+                if (d < p.pool.D && !none) qv[k] = *reinterpret_cast<const u32x4 *>(src + 2 * d);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) qv[k][w] ^= flip;
+            }
             const auto bounds = [&](int xa, int xz, Span &a, Span &s) {
                 xa = xa < n_rows ? xa : n_rows - 1;
                 xz = xz < n_rows ? xz : n_rows - 1;
                 s = span_of_rows(rec, p, xa, xz);
-                a.hi = p.tree ? (uint32_t)base : span_of_rows(rec, p, xa, xa).hi;
+                a.hi = is_tree ? (uint32_t)base : span_of_rows(rec, p, xa, xa).hi;
                 const int last = rec.end - p.window;
-                a.lo = !p.tree ? span_of_rows(rec, p, xz, xz).lo : (uint32_t)(p.window && last > rec.start ? last : rec.start);
+                a.lo = !is_tree ? span_of_rows(rec, p, xz, xz).lo : (uint32_t)(p.window && last > rec.start ? last : rec.start);
             };
             Span unused;
-            bounds(x0, x0 + 32 * RB - 1, all, some);
+            bounds(x0, x0 + 31, all, some);
             bounds(block0, block0 + p.rows - 1, block_all, unused);
         }
 
-        f32x16 o[RB][DB];
-        float m[RB], l[RB];
+        f32x16 o[DB];
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
+        for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int d = 0; d < DB; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[rb][d][i] = 0.f;
-            m[rb] = -INFINITY;
-            l[rb] = 0.f;
-        }
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+        float m = -INFINITY, l = 0.f;
 
         uint32_t t0 = begin + (TEAM > 1 ? 0 : wave * TILE);
         const uint32_t step = TILE * streams;
         if (t0 < end) {
-            uint64_t here = resolve(t0, look(t0));
-            load(0, part);
-            put(0, part);
-            int32_t page = look(t0 + step);
-            for (int buf = 0; t0 < end; t0 += step, buf ^= 1) {
+            // Tiles are resolved TEAM at a time, one by each wavefront, while the TEAM before are used;
+            // their page ids are asked for as much earlier.
+            const uint32_t mine = t0 + part * step;
+            resolve(mine, look(mine), 0, part);
+            if (TEAM > 1) __syncthreads();
+            load(0, rows.off[0][0]);
+            put(0);
+            int32_t page = look(mine + TEAM * step);
+            for (int k = 0; t0 < end; t0 += step, ++k) {
+                const int buf = k & 1, slot = k & (TEAM - 1), ring = k / TEAM & 1;
                 arrive();
-                const uint64_t next = resolve(t0 + step, page);
+                if (slot == 0) {
+                    resolve(t0 + (TEAM + part) * step, page, ring ^ 1, part);
+                    page = look(t0 + (2 * TEAM + part) * step);
+                }
                 const bool more = t0 + step < end;
-                if (more) load(buf ^ 1, part);
-                page = look(t0 + 2 * step);
+                const int next = k + 1;
+                if (more) load(buf ^ 1, rows.off[next / TEAM & 1][next & (TEAM - 1)]);
+                const uint64_t here = scalar((int64_t)rows.there[ring][slot]);
                 const char *kt = lds + buf * tile_bytes, *vt = kt + (two ? TILE * PITCH : 0);
                 const bool on = active && t0 < some.hi && t0 + TILE > some.lo;
                 const bool edge = here != ALL || t0 < all.lo || t0 + TILE > all.hi;        // some row does not see all
                 const bool team_edge = here != ALL || t0 < block_all.lo || t0 + TILE > block_all.hi;
-                f32x16 s[RB][PB];        // scores, then weights
-                uint64_t sees[RB];
+                f32x16 s[PB];            // scores, then weights
+                uint64_t sees = ALL;
                 if (on) {
 #pragma unroll
-                    for (int rb = 0; rb < RB; ++rb)
+                    for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
-                        for (int pb = 0; pb < PB; ++pb)
+                        for (int i = 0; i < 16; ++i) s[pb][i] = 0.f;
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) s[rb][pb][i] = 0.f;
+                    for (int j = 0; j < KS; ++j)
 #pragma unroll
-                    for (int k = 0; k < KS; ++k)
-#pragma unroll
-                        for (int pb = 0; pb < PB; ++pb) {
-                            const u32x4 a = keys(kt, pb, k);
-#pragma unroll
-                            for (int rb = 0; rb < RB; ++rb) s[rb][pb] = mfma32<F16>(a, qv[rb][k], s[rb][pb]);
-                        }
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) {
-                        if (GENERAL) {
-                            if (p.cap > 0.f) {
-#pragma unroll
-                                for (int pb = 0; pb < PB; ++pb)
-#pragma unroll
-                                    for (int i = 0; i < 16; ++i)
-                                        s[rb][pb][i] = cap2 - 2.f * cap2 * __builtin_amdgcn_rcpf(1.f + exp2_fast(s[rb][pb][i] * cap_unit));
-                            } else {
-#pragma unroll
-                                for (int pb = 0; pb < PB; ++pb) s[rb][pb] *= unit;
-                            }
-                            if (p.slopes) {
-                                const float far = (float)(at[rb] - (int)(t0 + 4 * e));
-                                const bool by_depth = p.tree && t0 + TILE > (uint32_t)base;
-#pragma unroll
-                                for (int pb = 0; pb < PB; ++pb)
-#pragma unroll
-                                    for (int i = 0; i < 16; ++i) {
-                                        const int off = 32 * pb + 8 * (i / 4) + i % 4;
-                                        float d = fabsf(far - (float)off);
-                                        if (by_depth) {
-                                            const int j = (int)(t0 + 4 * e + off) - base;
-                                            if (j >= 0 && j < rec.n_queries) d = fabsf((float)(at[rb] - base) - depth[j]);
-                                        }
-                                        s[rb][pb][i] -= slope[rb] * d;
-                                    }
-                            }
-                        }
-                        const float from = GENERAL ? 1.f : unit;
-                        sees[rb] = ALL;
-                        if (edge) {
-                            uint64_t v = ones((int64_t)hi[rb] - t0) & ~ones((int64_t)lo[rb] - t0);
-                            const int64_t to = (int64_t)base - t0;
-                            if (p.tree && to < 64 && to > -64) v |= to >= 0 ? drafts[rb] << to : drafts[rb] >> -to;
-                            sees[rb] = v & here;
-                            const uint64_t mine = sees[rb] >> (4 * e);
+                        for (int pb = 0; pb < PB; ++pb) s[pb] = mfma32<F16>(keys(kt, pb, j), qv[j], s[pb]);
+                    if (GENERAL) {
+                        if (cap_unit > 0.f) {
 #pragma unroll
                             for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
                                 for (int i = 0; i < 16; ++i)
-                                    if (!((uint32_t)(mine >> (32 * pb)) >> (8 * (i / 4) + i % 4) & 1)) s[rb][pb][i] = -INFINITY;
+                                    s[pb][i] = __builtin_fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + exp2_fast(s[pb][i] * cap_unit)), cap2);
+                        } else {
+#pragma unroll
+                            for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) s[pb][i] *= unit;
                         }
-                        float top = s[rb][0][0];
+                        if (biased) {
+                            const float far = (float)(at - (int)(t0 + 4 * e));
+                            if (is_tree && t0 + TILE > (uint32_t)base) {
 #pragma unroll
-                        for (int pb = 0; pb < PB; ++pb)
+                                for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[rb][pb][i]);
-                        top = fmaxf(top, __shfl_xor(top, 32)) * from;
-                        if (__any(top - kLift<F16> > m[rb] + kSlack)) {
-                            const float raised = fmaxf(m[rb], top - kLift<F16>), f = weight(m[rb], raised);
-                            m[rb] = raised;
-                            l[rb] *= f;
+                                    for (int i = 0; i < 16; ++i) {
+                                        const int off = 32 * pb + 8 * (i / 4) + i % 4, j = (int)(t0 + 4 * e + off) - base;
+                                        const bool draft = j >= 0 && j < rec.n_queries;
+                                        const float d = draft ? (float)(at - base) - depth[draft ? j : 0] : far - (float)off;
+                                        s[pb][i] = __builtin_fmaf(-slope, fabsf(d), s[pb][i]);
+                                    }
+                            } else {
 #pragma unroll
-                            for (int d = 0; d < DB; ++d) o[rb][d] *= f;
-                        }
-                        const float ref = m[rb] == -INFINITY ? 0.f : m[rb];      // then every score is -inf
+                                for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
-                        for (int pb = 0; pb < PB; ++pb)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                s[rb][pb][i] = exp2_fast(__builtin_fmaf(s[rb][pb][i], from, -ref));
-                                l[rb] += s[rb][pb][i];
+                                    for (int i = 0; i < 16; ++i)
+                                        s[pb][i] = __builtin_fmaf(-slope, fabsf(far - (float)(32 * pb + 8 * (i / 4) + i % 4)), s[pb][i]);
                             }
+                        }
                     }
+                    const float from = GENERAL ? 1.f : unit;
+                    if (edge) {
+                        uint64_t v = ones((int64_t)hi - t0) & ~ones((int64_t)lo - t0);
+                        const int64_t to = (int64_t)base - t0;
+                        if (is_tree && to < 64 && to > -64) v |= to >= 0 ? drafts << to : drafts >> -to;
+                        sees = v & here;
+                        const uint64_t shown = sees >> (4 * e);
+#pragma unroll
+                        for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                if (!((uint32_t)(shown >> (32 * pb)) >> (8 * (i / 4) + i % 4) & 1)) s[pb][i] = -INFINITY;
+                    }
+                    float top = s[0][0];
+#pragma unroll
+                    for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2) top = max3(top, s[pb][i], s[pb][i + 1]);
+                    top *= from;
+                    if (__any(top - kLift<F16> > m + kSlack)) {
+                        top = max_of_halves(top);
+                        const float raised = fmaxf(m, top - kLift<F16>), f = weight(m, raised);
+                        m = raised;
+                        l *= f;
+#pragma unroll
+                        for (int d = 0; d < DB; ++d) o[d] *= f;
+                    }
+                    const float ref = m == -INFINITY ? 0.f : m;      // then every score is -inf
+#pragma unroll
+                    for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            s[pb][i] = exp2_fast(__builtin_fmaf(s[pb][i], from, -ref));
+                            l += s[pb][i];
+                        }
                 }
                 if (team_edge) {
                     // The tile is the team's: it looks over its values together.
@@ -513,32 +558,29 @@ struct Queries {
                     bool found = any_spoilt(v, part * MINE, MINE);
                     if (TEAM > 1) found = __syncthreads_or(found);
                     if (found) {
-                        const uint64_t rows = spoilt(v, 0, TILE);
-                        for (uint64_t left = rows; left && on; left &= left - 1) {
+                        const uint64_t spoilt_rows = spoilt(v, 0, TILE);
+                        for (uint64_t left = spoilt_rows; left && on; left &= left - 1) {
                             const int r = __ffsll((unsigned long long)left) - 1;
                             const int held = r / 32 * 16 + r % 32 / 8 * 4 + r % 4, owner = c + 32 * (r / 4 % 2);
+                            float x = 0.f;
 #pragma unroll
-                            for (int rb = 0; rb < RB; ++rb) {
-                                float x = 0.f;
+                            for (int i = 0; i < 16 * PB; ++i) x = i == held ? s[i / 16][i % 16] : x;
+                            x = __shfl(x, owner);
+                            if (!(sees >> r & 1)) continue;
 #pragma unroll
-                                for (int i = 0; i < 16 * PB; ++i) x = i == held ? s[rb][i / 16][i % 16] : x;
-                                x = __shfl(x, owner);
-                                if (!(sees[rb] >> r & 1)) continue;
+                            for (int d = 0; d < DB; ++d)
 #pragma unroll
-                                for (int d = 0; d < DB; ++d)
-#pragma unroll
-                                    for (int i = 0; i < 4; ++i) {
-                                        const u32x2 y = *reinterpret_cast<const u32x2 *>(v + r * PITCH + 16 * ((4 * d + i) ^ swirl(r)) + 8 * e);
-                                        o[rb][d][4 * i] += x * V::lo(y[0]);
-                                        o[rb][d][4 * i + 1] += x * V::hi(y[0]);
-                                        o[rb][d][4 * i + 2] += x * V::lo(y[1]);
-                                        o[rb][d][4 * i + 3] += x * V::hi(y[1]);
-                                    }
-                            }
+                                for (int i = 0; i < 4; ++i) {
+                                    const u32x2 y = *reinterpret_cast<const u32x2 *>(v + r * PITCH + 16 * ((4 * d + i) ^ swirl(r)) + 8 * e);
+                                    o[d][4 * i] += x * V::lo(y[0]);
+                                    o[d][4 * i + 1] += x * V::hi(y[0]);
+                                    o[d][4 * i + 2] += x * V::lo(y[1]);
+                                    o[d][4 * i + 3] += x * V::hi(y[1]);
+                                }
                         }
                         if (TEAM > 1) __syncthreads();
                         for (int r = part * MINE; r < (part + 1) * MINE; ++r)
-                            if (rows >> r & 1)
+                            if (spoilt_rows >> r & 1)
                                 for (int x = lane; x < DK / 8; x += 64) *reinterpret_cast<u32x4 *>(v + r * PITCH + 16 * x) = u32x4{0, 0, 0, 0};
                         if (TEAM > 1) __syncthreads();
                         else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -549,61 +591,55 @@ struct Queries {
                     for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
                         for (int s2 = 0; s2 < 2; ++s2) {
-                            u32x4 a[RB], rest[RB];
+                            u32x4 a, rest;
+                            float x[8];
 #pragma unroll
-                            for (int rb = 0; rb < RB; ++rb) {
-                                float x[8];
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) x[i] = s[rb][pb][8 * s2 + i];
-                                if (PARTS) split<F16>(x, a[rb], rest[rb]);
-                                else a[rb] = u32x4{V::pack(x[0], x[1]), V::pack(x[2], x[3]), V::pack(x[4], x[5]), V::pack(x[6], x[7])};
-                            }
+                            for (int i = 0; i < 8; ++i) x[i] = s[pb][8 * s2 + i];
+                            if (PARTS) split<F16>(x, a, rest);
+                            else a = u32x4{V::pack(x[0], x[1]), V::pack(x[2], x[3]), V::pack(x[4], x[5]), V::pack(x[6], x[7])};
 #pragma unroll
                             for (int d = 0; d < DB; ++d) {
                                 const u32x4 v = columns(vt, pb, s2, d);
-#pragma unroll
-                                for (int rb = 0; rb < RB; ++rb) {
-                                    o[rb][d] = mfma32<F16>(v, a[rb], o[rb][d]);
-                                    if (PARTS) o[rb][d] = mfma32<F16>(v, rest[rb], o[rb][d]);
-                                }
+                                o[d] = mfma32<F16>(v, a, o[d]);
+                                if (PARTS) o[d] = mfma32<F16>(v, rest, o[d]);
                             }
                         }
                 }
-                here = next;
-                if (more) put(buf ^ 1, part);
+                if (more) put(buf ^ 1);
             }
         }
+        const QueriesParams p = again();
+        const int G = p.fd_G.d, h = piece.h, block0 = piece.b * p.rows;
         if (bad && p.err) atomicOr(p.err, bad);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) l[rb] += __shfl_xor(l[rb], 32);
+        l += __shfl_xor(l, 32);
 
         // Join the wavefronts of the same rows: each scales to the common maximum, then they
         // add up in LDS, one after the other.
         if (TEAM == 1 && streams > 1) {
             if (e == 0) {
-                ml[(wave * 32 + c) * 2] = m[0];
-                ml[(wave * 32 + c) * 2 + 1] = l[0];
+                ml[(wave * 32 + c) * 2] = m;
+                ml[(wave * 32 + c) * 2 + 1] = l;
             }
             __syncthreads();
             float top = -INFINITY, sum = 0.f;
             for (int k = 0; k < streams; ++k) top = fmaxf(top, ml[(k * 32 + c) * 2]);
             for (int k = 0; k < streams; ++k) sum += ml[(k * 32 + c) * 2 + 1] * weight(ml[(k * 32 + c) * 2], top);
-            const float f = weight(m[0], top);
-            m[0] = top;
-            l[0] = sum;
+            const float f = weight(m, top);
+            m = top;
+            l = sum;
             f32x4 *joined = reinterpret_cast<f32x4 *>(all_lds) + lane;         // [value / 4][lane]
             for (int turn = 0; turn < streams; ++turn) {
                 if (wave == turn) {
 #pragma unroll
                     for (int d = 0; d < DB; ++d) {
-                        o[0][d] *= f;
+                        o[d] *= f;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            f32x4 x = {o[0][d][4 * i], o[0][d][4 * i + 1], o[0][d][4 * i + 2], o[0][d][4 * i + 3]};
+                            f32x4 x = {o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
                             if (turn > 0) x += joined[64 * (4 * d + i)];
                             if (turn < streams - 1) joined[64 * (4 * d + i)] = x;
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) o[0][d][4 * i + j] = x[j];
+                            for (int j = 0; j < 4; ++j) o[d][4 * i + j] = x[j];
                         }
                     }
                 }
@@ -611,57 +647,55 @@ struct Queries {
             }
             if (wave != streams - 1) return;
         }
-        const float v_scale = p.scales ? p.scales[(p.pool.C - 1) * p.pool.H + h] : 1.f;
+        const int x = x0 + c;
+        if (x >= h_rows) return;
+        const int i = fd_div(p.fd_G, x), head = h * G + x - i * G;
+        if (piece.place < 0) {
+            const float v_scale = p.scales ? p.scales[(p.pool.C - 1) * p.pool.H + h] : 1.f;
+            const float f = l == 0.f ? 0.f : v_scale / l;
+            if (p.lse && e == 0)
+                p.lse[(rec.row_off + i) * p.pool.H * G + head] =
+                    l > 0.f || l != l ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+            char *dst = p.out.base + (rec.row_off + i) * p.out.s_row + head * p.out.s_head;
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            const int x = x0 + 32 * rb + c;
-            if (x >= n_rows) continue;
-            const int i = fd_div(p.fd_G, x), head = h * G + x - i * G;
-            if (piece.place < 0) {
-                const float f = l[rb] == 0.f ? 0.f : v_scale / l[rb];
-                if (p.lse && e == 0)
-                    p.lse[(rec.row_off + i) * p.pool.H * G + head] =
-                        l[rb] > 0.f || l[rb] != l[rb] ? (m[rb] + __builtin_amdgcn_logf(l[rb])) * kLn2 : -INFINITY;
-                char *dst = p.out.base + (rec.row_off + i) * p.out.s_row + head * p.out.s_head;
+            for (int d = 0; d < DB; ++d)
 #pragma unroll
-                for (int d = 0; d < DB; ++d)
+                for (int j = 0; j < 4; ++j) {
+                    const int to = 32 * d + 8 * j + 4 * e;
+                    if (to < p.Dv)
+                        *reinterpret_cast<u32x2 *>(dst + 2 * to) = u32x2{V::pack(o[d][4 * j] * f, o[d][4 * j + 1] * f),
+                                                                        V::pack(o[d][4 * j + 2] * f, o[d][4 * j + 3] * f)};
+                }
+        } else {
+            const int64_t row = piece.place * p.rows + x - block0;
+            if (e == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * row) = make_float2(m, l);
+            float *dst = p.part_o + row * p.Dv;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int at = 32 * d + 8 * j + 4 * e;
-                        if (at < p.Dv)
-                            *reinterpret_cast<u32x2 *>(dst + 2 * at) = u32x2{V::pack(o[rb][d][4 * j] * f, o[rb][d][4 * j + 1] * f),
-                                                                            V::pack(o[rb][d][4 * j + 2] * f, o[rb][d][4 * j + 3] * f)};
-                    }
-            } else {
-                const int64_t row = piece.place * p.rows + x - block0;
-                if (e == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * row) = make_float2(m[rb], l[rb]);
-                float *dst = p.part_o + row * p.Dv;
+            for (int d = 0; d < DB; ++d)
 #pragma unroll
-                for (int d = 0; d < DB; ++d)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int at = 32 * d + 8 * j + 4 * e;
-                        if (at < p.Dv)
-                            *reinterpret_cast<f32x4 *>(dst + at) = f32x4{o[rb][d][4 * j], o[rb][d][4 * j + 1], o[rb][d][4 * j + 2], o[rb][d][4 * j + 3]};
-                    }
-            }
+                for (int j = 0; j < 4; ++j) {
+                    const int to = 32 * d + 8 * j + 4 * e;
+                    if (to < p.Dv)
+                        *reinterpret_cast<f32x4 *>(dst + to) = f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
+                }
         }
     }
 };
 
-template <bool F16, bool E4M3, int DK, int DV, int RB, int TEAM, int TILE, bool GENERAL>
-__global__ void __launch_bounds__(256, 1) kvx_queries_kernel(QueriesParams p, int64_t first, int32_t n) {
+// With rows of up to 128 two wavefronts lie on a SIMD.
+template <bool F16, bool E4M3, int DK, int DV, int WAVES, int TEAM, int TILE, bool GENERAL>
+__global__ void __launch_bounds__(64 * WAVES, DK <= 128 ? 2 : 1) kvx_queries_kernel(QueriesParams p, int64_t first, int32_t n) {
+    typedef Queries<F16, E4M3, DK, DV, TEAM, TILE, GENERAL> Work;
     __shared__ int64_t before[kQueriesGroup + 1];        // steps of one cache head of the records before
-    __shared__ __align__(16) int64_t row_off[4][TILE];
-    __shared__ float depth[4][KVX_MAX_DRAFTS];
-    __shared__ float ml[4 * 32 * 2];
-    __shared__ int64_t sums[4];
+    __shared__ __align__(16) typename Work::Rows rows[WAVES / TEAM];
+    __shared__ float depth[WAVES][KVX_MAX_DRAFTS];
+    __shared__ float ml[TEAM == 1 ? WAVES * 32 * 2 : 1];
+    __shared__ int64_t sums[WAVES];
     extern __shared__ __align__(256) char lds[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), H = p.pool.H;
     const int tile_bytes = TILE * 2 * DK * p.pool.C;
-    Queries<F16, E4M3, DK, DV, RB, TEAM, TILE, GENERAL> work{p, row_off[wave], depth[wave],
-                                                              lds + (TEAM > 1 ? 0 : wave * 2 * tile_bytes), ml, lds, lane, wave,
-                                                              lane & 31, lane >> 5, p.pool.C == 2, tile_bytes};
+    Work work{rows[TEAM > 1 ? 0 : wave], depth[wave], lds + (TEAM > 1 ? 0 : wave * 2 * tile_bytes), ml, lds, lane, wave,
+              TEAM > 1 ? wave : 0, lane & 31, lane >> 5, p.pool.C == 2, tile_bytes};
     work.address();
     const kvx_queries_req *reqs = p.whole ? p.reqs : p.reqs + first;
     int64_t at = 0, stop = 1, each = 0;
@@ -704,6 +738,9 @@ __global__ void __launch_bounds__(256, 1) kvx_queries_kernel(QueriesParams p, in
         stop = at + each < total ? at + each : total;
     }
     while (at < stop) {
+        const QueriesParams p = again();
+        const int H = p.pool.H;
+        const kvx_queries_req *reqs = p.whole ? p.reqs : p.reqs + first;
         Piece piece;
         Span s;
         int64_t here = 1;
@@ -758,19 +795,14 @@ __global__ void __launch_bounds__(256, 1) kvx_queries_kernel(QueriesParams p, in
     }
 }
 
-// Bytes of LDS of a workgroup's tiles.
-inline size_t lds_bytes(const QueriesParams &p, int dk, int tile) {
-    return (size_t)2 * tile * 2 * dk * p.pool.C * (p.waves / p.team);
-}
-
-template <bool F16, bool E4M3, int DK, int DV, int RB, int TEAM, int TILE>
+template <bool F16, bool E4M3, int DK, int DV, int WAVES, int TEAM, int TILE>
 int launch_form(const QueriesParams &p, int64_t first, int64_t n, hipStream_t stream) {
-    // scales of 0 and the sign are the kernel's; what it does to scores beyond them is GENERAL
-    const bool general = p.cap > 0.f || p.slopes;
-    const auto kernel = TEAM == 1 || general ? kvx_queries_kernel<F16, E4M3, DK, DV, RB, TEAM, TILE, true>
-                                             : kvx_queries_kernel<F16, E4M3, DK, DV, RB, TEAM, TILE, TEAM == 1>;
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.whole ? n : p.shares)), dim3(64 * p.waves), lds_bytes(p, DK, TILE), stream, p,
-                       first, (int32_t)n);
+    // few rows are bound by memory, and take one kernel for all scores
+    const bool general = TEAM == 1 || p.cap > 0.f || p.slopes;
+    const auto kernel = general ? kvx_queries_kernel<F16, E4M3, DK, DV, WAVES, TEAM, TILE, true>
+                                : kvx_queries_kernel<F16, E4M3, DK, DV, WAVES, TEAM, TILE, TEAM == 1>;
+    const size_t lds = (size_t)2 * TILE * 2 * DK * p.pool.C * (p.waves / TEAM);
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.whole ? n : p.shares)), dim3(64 * p.waves), lds, stream, p, first, (int32_t)n);
     return hipGetLastError();
 }
 
@@ -778,17 +810,17 @@ template <bool F16, bool E4M3>
 int launch_type(const QueriesParams &p, int64_t first, int64_t n, hipStream_t stream) {
     const int D = p.pool.D;
     if (p.team == 1) {
-        if (D <= 64) return launch_form<F16, E4M3, 64, 64, 1, 1, 32>(p, first, n, stream);
-        if (D <= 128) return launch_form<F16, E4M3, 128, 128, 1, 1, 32>(p, first, n, stream);
-        if (D <= 256) return launch_form<F16, E4M3, 256, 256, 1, 1, 32>(p, first, n, stream);
-        return launch_form<F16, E4M3, 576, 512, 1, 1, 32>(p, first, n, stream);
+        if (D <= 64) return launch_form<F16, E4M3, 64, 64, 4, 1, 32>(p, first, n, stream);
+        if (D <= 128) return launch_form<F16, E4M3, 128, 128, 4, 1, 32>(p, first, n, stream);
+        if (D <= 256) return launch_form<F16, E4M3, 256, 256, 2, 1, 32>(p, first, n, stream);
+        return launch_form<F16, E4M3, 576, 512, 2, 1, 32>(p, first, n, stream);
     }
-    if (D <= 64) return launch_form<F16, E4M3, 64, 64, 2, 4, 64>(p, first, n, stream);
+    if (D <= 64) return launch_form<F16, E4M3, 64, 64, 8, 8, 64>(p, first, n, stream);
     if (D <= 128)
-        return p.rows == 128 ? launch_form<F16, E4M3, 128, 128, 1, 4, 64>(p, first, n, stream)
-                             : launch_form<F16, E4M3, 128, 128, 2, 4, 64>(p, first, n, stream);
-    if (D <= 256) return launch_form<F16, E4M3, 256, 256, 1, 4, 64>(p, first, n, stream);
-    return launch_form<F16, E4M3, 576, 512, 1, 4, 32>(p, first, n, stream);
+        return p.team == 4 ? launch_form<F16, E4M3, 128, 128, 4, 4, 64>(p, first, n, stream)
+                           : launch_form<F16, E4M3, 128, 128, 8, 8, 64>(p, first, n, stream);
+    if (D <= 256) return launch_form<F16, E4M3, 256, 256, 4, 4, 64>(p, first, n, stream);
+    return launch_form<F16, E4M3, 576, 512, 4, 4, 32>(p, first, n, stream);
 }
 
 }  // namespace

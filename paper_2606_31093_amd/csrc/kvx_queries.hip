@@ -93,10 +93,12 @@ __global__ void __launch_bounds__(kThreads) kvx_queries_join_kernel(QueriesParam
     *reinterpret_cast<u32x2 *>(dst + 8 * col) = u32x2{Half<F16>::pack(sum[0], sum[1]), Half<F16>::pack(sum[2], sum[3])};
 }
 
-constexpr int kResident = 256;           // workgroups that the device holds at a time
+// Workgroups that the device holds at a time, by their LDS and registers: its 256 compute
+// units have room for one, or for two of four wavefronts.
+int resident(const QueriesParams &p) { return (p.team == 4 && p.pool.D <= 128) || (p.team == 1 && p.pool.D <= 64) ? 512 : 256; }
 // Units of up to this many steps, or this many units and more, are not split.
 constexpr int kWholeSteps = 8;
-constexpr int kWholeUnits = 4 * kResident;
+constexpr int kWholeUnits = 1024;
 // Fewer steps than this are not worth a share.
 constexpr int kLeastShare = 4;
 
@@ -106,9 +108,9 @@ int tile_of(const QueriesParams &p) { return p.team == 1 || p.pool.D > 256 ? 32 
 void shape(QueriesParams &p, int64_t most) {
     const int D = p.pool.D;
     // Up to 32 rows: wavefronts take positions of their own; as many as LDS holds tiles for.
-    p.team = most <= 32 ? 1 : 4;
-    p.waves = p.team == 4 || D <= 128 ? 4 : D <= 256 || p.pool.C == 1 ? 2 : 1;
-    p.rows = p.team == 1 ? 32 : D <= 64 || (D <= 128 && most > 128) ? 256 : 128;
+    p.team = most <= 32 ? 1 : D <= 64 || (D <= 128 && most > 128) ? 8 : 4;
+    p.waves = p.team > 1 ? p.team : D <= 128 ? 4 : D <= 256 || p.pool.C == 1 ? 2 : 1;
+    p.rows = 32 * p.team;
     p.step = tile_of(p) * (p.waves / p.team);
     p.blocks = (int32_t)((most + p.rows - 1) / p.rows);
     if (p.blocks < 1) p.blocks = 1;
@@ -119,7 +121,7 @@ int64_t most_steps(const QueriesParams &p) { return ((int64_t)p.max_tokens + kTi
 // Shares for so many units of the longest records.
 int32_t shares_for(const QueriesParams &p, int64_t units) {
     const int64_t steps = most_steps(p), n = (units * (steps > 0 ? steps : 1) + kLeastShare - 1) / kLeastShare;
-    return (int32_t)(n < kResident ? (n > 0 ? n : 1) : kResident);
+    return (int32_t)(n < resident(p) ? (n > 0 ? n : 1) : resident(p));
 }
 
 // Workspace of `units` units.
