@@ -40,6 +40,9 @@ int launch_queries_f16(const QueriesParams &p, int64_t first, int64_t n, hipStre
 int launch_queries_bf16_e4m3(const QueriesParams &p, int64_t first, int64_t n, hipStream_t stream);
 int launch_queries_f16_e4m3(const QueriesParams &p, int64_t first, int64_t n, hipStream_t stream);
 
+#ifndef KVX_AHEAD
+#define KVX_AHEAD 3
+#endif
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -164,6 +167,9 @@ __device__ __forceinline__ bool not_finite(uint32_t w) {
     return (w & e) == e || (w >> 16 & e) == e;
 }
 
+// Whether LDS has room for one tile only.
+__host__ __device__ constexpr bool one_tile(int dk, int kv) { return dk > 256 && kv == 2; }
+
 // The larger of three; what is not a number counts for nothing.
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float x;
@@ -186,18 +192,26 @@ __device__ __forceinline__ QueriesParams again() {
 }
 
 // DK: elements of a row in LDS (head_dim is up to that), DV: of a value; TEAM: wavefronts
-// that share a tile, each with 32 rows (all of the workgroup; or 1: each takes tiles of
-// its own for the same 32 rows, and they join at the end); TILE: positions; GENERAL: scores
-// may be capped or biased.
-template <bool F16, bool E4M3, int DK, int DV, int TEAM, int TILE, bool GENERAL>
+// that share a tile (all of the workgroup; or 1: each takes tiles of its own for the same
+// 32 rows, and they join at the end); SPLIT: wavefronts that share 32 rows (wide rows: a
+// query and its outputs would not leave registers for a second wavefront on the SIMD;
+// each takes a part of the elements for the scores, which they add up through LDS, and a
+// part of the values); TILE: positions; GENERAL: scores may be capped or biased.
+template <bool F16, bool E4M3, int DK, int DV, int TEAM, int SPLIT, int TILE, bool GENERAL>
 struct Queries {
     typedef Half<F16> V;
-    static constexpr int KS = DK / 16, DB = DV / 32, PB = TILE / 32, PITCH = 2 * DK;
+    // of a wavefront: steps of 16 elements of K, blocks of 32 values
+    static constexpr int KS = DK / 16 / SPLIT, DB = DV / 32 / SPLIT;
+    static constexpr int PB = TILE / 32, PITCH = 2 * DK;
     static constexpr int SRC = DK * (E4M3 ? 1 : 2) / 16;       // 16-byte chunks of a row in memory
-    static constexpr int LOADS = (TILE * SRC + 64 * TEAM - 1) / (64 * TEAM);   // a wavefront's of a tile, for K or for V
+    // loads of a wavefront for a tile's K or V, of them all a wavefront's at most
+    static constexpr int ALL_LOADS = TILE * SRC / 64, LOADS = (ALL_LOADS + TEAM - 1) / TEAM;
     static constexpr bool PARTS = TEAM == 1;                   // weights in two parts
+    // Reads of LDS are kept so many products ahead where registers are short (left alone the
+    // compiler reads more than there are registers for).
+    static constexpr int AHEAD = SPLIT > 1 ? KVX_AHEAD : 0;
     static constexpr uint64_t ALL = TILE == 64 ? ~0ull : 0xffffffffull;
-    static_assert((E4M3 || LOADS * 64 * TEAM == TILE * SRC) && (TILE == 32 || TILE == 64), "tile");
+    static_assert(TILE * SRC % 64 == 0 && (TILE == 32 || TILE == 64), "tile");
 
     // Of TEAM tiles, and the next TEAM ones: row offsets (-1: none) and which are there.
     struct Rows {
@@ -209,8 +223,9 @@ struct Queries {
     char *lds;                   // [2][rows of K, rows of V if there are two], the team's
     float *ml;                   // [wavefronts][32][2]
     char *all_lds;               // the workgroup's
+    f32x4 *shared;               // [wavefront][4][64]: scores that wavefronts of the same rows add up
     int lane, wave, part, c, e;  // part: of the team
-    bool two;
+    bool two, once;              // V apart from K; LDS has room for one tile only
     int tile_bytes;
     // of the piece
     kvx_queries_req rec;
@@ -249,11 +264,12 @@ struct Queries {
         const int ln = lane_again();
 #pragma unroll
         for (int x = 0; x < LOADS; ++x) {
-            const int u = (part * LOADS + x) * 64 + ln, row = u / SRC;
+            const int piece = x * TEAM + part;
+            if (ALL_LOADS % TEAM && piece >= ALL_LOADS) continue;
+            const int u = piece * 64 + ln, row = u / SRC;
             int chunk = u % SRC;
             if (!E4M3) chunk ^= swirl(row);
-            if (LOADS * 64 * TEAM != TILE * SRC && row >= TILE) chunk = have;
-            const int64_t off = off_of[LOADS * 64 * TEAM != TILE * SRC ? row & (TILE - 1) : row];
+            const int64_t off = off_of[row];
             const bool ok = off >= 0 && chunk < have;
             const char *k = ok ? kbase + off + 16 * chunk : reinterpret_cast<const char *>(&kvx_zeros);
             const char *v = ok ? k + s_c : k;
@@ -261,7 +277,7 @@ struct Queries {
                 staged[x][0] = *reinterpret_cast<const u32x4 *>(k);
                 if (two) staged[x][1] = *reinterpret_cast<const u32x4 *>(v);
             } else {
-                const uint32_t at = __builtin_amdgcn_readfirstlane(to + (part * LOADS + x) * 1024);
+                const uint32_t at = __builtin_amdgcn_readfirstlane(to + piece * 1024);
                 load_to_lds(k, at);
                 if (two) load_to_lds(v, at + TILE * PITCH);
             }
@@ -274,8 +290,9 @@ struct Queries {
             const int ln = lane_again();
 #pragma unroll
             for (int x = 0; x < LOADS; ++x) {
-                const int u = (part * LOADS + x) * 64 + ln, row = u / SRC, chunk = u % SRC * 2;
-                if (LOADS * 64 * TEAM != TILE * SRC && row >= TILE) continue;
+                const int piece = x * TEAM + part;
+                if (ALL_LOADS % TEAM && piece >= ALL_LOADS) continue;
+                const int u = piece * 64 + ln, row = u / SRC, chunk = u % SRC * 2;
 #pragma unroll
                 for (int kv = 0; kv < 2; ++kv) {
                     if (kv && !two) continue;
@@ -298,17 +315,21 @@ struct Queries {
 
     // Addresses in LDS: a row's permutation concerns the low 3 bits of a chunk's number, so
     // that there are few of them and the rest is in the instructions.
-    // - K: the lane's row, chunks 2 k + e for k % 4
+    // - K: the lane's row, chunks 2 k + e from the wavefront's first step on, for k % 4
     // - V, 32 columns from 32 db on for db % 2: 16 lanes give the addresses of 4 rows x 16
     //   elements, positions 32 pb + 16 s + 4 e + x and 8 behind, x < 4
     int k_at[4], v_at[2];
     __device__ __forceinline__ void address() {
+        const int mine = wave % SPLIT;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) k_at[k] = c * PITCH + 16 * ((2 * k + e) ^ swirl(c));
+        for (int k = 0; k < 4; ++k) {
+            const int chunk = 2 * (mine * KS + k) + e;
+            k_at[k] = c * PITCH + 16 * (chunk ^ swirl(c));
+        }
         const int l = lane & 15, row = 4 * e + l / 4;
 #pragma unroll
         for (int d = 0; d < 2; ++d)
-            v_at[d] = row * PITCH + 16 * ((4 * d + (lane >> 4 & 1) * 2 + (l >> 1 & 1)) ^ swirl(row)) + (l & 1) * 8;
+            v_at[d] = row * PITCH + 16 * ((4 * (mine * DB + d) + (lane >> 4 & 1) * 2 + (l >> 1 & 1)) ^ swirl(row)) + (l & 1) * 8;
     }
     __device__ __forceinline__ u32x4 keys(const char *k, int pb, int step) const {
         return *reinterpret_cast<const u32x4 *>(k + k_at[step % 4] + (32 * pb * PITCH + step / 4 * 128));
@@ -390,7 +411,7 @@ struct Queries {
                 cap_unit = 2.f * unit / p.cap;
             }
             const int block0 = piece.b * p.rows;
-            x0 = block0 + part * 32;
+            x0 = block0 + part / SPLIT * 32;
             active = x0 < n_rows;
             if (is_tree) {
                 if (lane < rec.n_queries) {
@@ -418,7 +439,7 @@ struct Queries {
             const char *src = p.q.base + (rec.row_off + i) * p.q.s_row + (int64_t)(h * G + g) * p.q.s_head;
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                const int d = 16 * k + 8 * e;
+                const int d = 16 * (wave % SPLIT * KS + k) + 8 * e;
                 qv[k] = u32x4{0, 0, 0, 0};
                 if (d < p.pool.D && !none) qv[k] = *reinterpret_cast<const u32x4 *>(src + 2 * d);
 #pragma unroll
@@ -456,13 +477,20 @@ struct Queries {
             put(0);
             int32_t page = look(mine + TEAM * step);
             for (int k = 0; t0 < end; t0 += step, ++k) {
-                const int buf = k & 1, slot = k & (TEAM - 1), ring = k / TEAM & 1;
+                const int buf = SPLIT > 1 && once ? 0 : k & 1, slot = k & (TEAM - 1), ring = k / TEAM & 1;
+                if (SPLIT > 1 && once && k > 0) {
+                    // the tile before has been used
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    __builtin_amdgcn_s_barrier();
+                    load(0, rows.off[ring][slot]);
+                    put(0);
+                }
                 arrive();
                 if (slot == 0) {
                     resolve(t0 + (TEAM + part) * step, page, ring ^ 1, part);
                     page = look(t0 + (2 * TEAM + part) * step);
                 }
-                const bool more = t0 + step < end;
+                const bool more = t0 + step < end && !(SPLIT > 1 && once);
                 const int next = k + 1;
                 if (more) load(buf ^ 1, rows.off[next / TEAM & 1][next & (TEAM - 1)]);
                 const uint64_t here = scalar((int64_t)rows.there[ring][slot]);
@@ -472,15 +500,46 @@ struct Queries {
                 const bool team_edge = here != ALL || t0 < block_all.lo || t0 + TILE > block_all.hi;
                 f32x16 s[PB];            // scores, then weights
                 uint64_t sees = ALL;
+#pragma unroll
+                for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[pb][i] = 0.f;
                 if (on) {
+                    if constexpr (AHEAD == 0) {
 #pragma unroll
-                    for (int pb = 0; pb < PB; ++pb)
+                        for (int j = 0; j < KS; ++j)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[pb][i] = 0.f;
+                            for (int pb = 0; pb < PB; ++pb) s[pb] = mfma32<F16>(keys(kt, pb, j), qv[j], s[pb]);
+                    } else {
+                        u32x4 a[AHEAD + 1];
 #pragma unroll
-                    for (int j = 0; j < KS; ++j)
+                        for (int u = 0; u < AHEAD; ++u) a[u] = keys(kt, u % PB, u / PB);
+                        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                        for (int pb = 0; pb < PB; ++pb) s[pb] = mfma32<F16>(keys(kt, pb, j), qv[j], s[pb]);
+                        for (int u = 0; u < KS * PB; ++u) {
+                            if (u + AHEAD < KS * PB) a[(u + AHEAD) % (AHEAD + 1)] = keys(kt, (u + AHEAD) % PB, (u + AHEAD) / PB);
+                            s[u % PB] = mfma32<F16>(a[u % (AHEAD + 1)], qv[u / PB], s[u % PB]);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
+                }
+                if constexpr (SPLIT > 1) {
+                    static_assert(PB == 1 && SPLIT == 2, "pairs");
+                    f32x4 *mine = shared + wave * 256 + lane;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mine[64 * i] = f32x4{s[0][4 * i], s[0][4 * i + 1], s[0][4 * i + 2], s[0][4 * i + 3]};
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
+                    const f32x4 *other = shared + (wave ^ 1) * 256 + lane;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const f32x4 x = other[64 * i];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) s[0][4 * i + j] += x[j];
+                    }
+                }
+                if (on) {
                     if (GENERAL) {
                         if (cap_unit > 0.f) {
 #pragma unroll
@@ -571,7 +630,7 @@ struct Queries {
                             for (int d = 0; d < DB; ++d)
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) {
-                                    const u32x2 y = *reinterpret_cast<const u32x2 *>(v + r * PITCH + 16 * ((4 * d + i) ^ swirl(r)) + 8 * e);
+                                    const u32x2 y = *reinterpret_cast<const u32x2 *>(v + r * PITCH + 16 * ((4 * (wave % SPLIT * DB + d) + i) ^ swirl(r)) + 8 * e);
                                     o[d][4 * i] += x * V::lo(y[0]);
                                     o[d][4 * i + 1] += x * V::hi(y[0]);
                                     o[d][4 * i + 2] += x * V::lo(y[1]);
@@ -587,23 +646,38 @@ struct Queries {
                     }
                 }
                 if (on) {
+                    u32x4 w[2 * PB], rest[2 * PB];
 #pragma unroll
-                    for (int pb = 0; pb < PB; ++pb)
+                    for (int u = 0; u < 2 * PB; ++u) {
+                        float x[8];
 #pragma unroll
-                        for (int s2 = 0; s2 < 2; ++s2) {
-                            u32x4 a, rest;
-                            float x[8];
+                        for (int i = 0; i < 8; ++i) x[i] = s[u / 2][8 * (u % 2) + i];
+                        if (PARTS) split<F16>(x, w[u], rest[u]);
+                        else w[u] = u32x4{V::pack(x[0], x[1]), V::pack(x[2], x[3]), V::pack(x[4], x[5]), V::pack(x[6], x[7])};
+                    }
+                    if constexpr (AHEAD == 0) {
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) x[i] = s[pb][8 * s2 + i];
-                            if (PARTS) split<F16>(x, a, rest);
-                            else a = u32x4{V::pack(x[0], x[1]), V::pack(x[2], x[3]), V::pack(x[4], x[5]), V::pack(x[6], x[7])};
+                        for (int u = 0; u < 2 * PB; ++u)
 #pragma unroll
                             for (int d = 0; d < DB; ++d) {
-                                const u32x4 v = columns(vt, pb, s2, d);
-                                o[d] = mfma32<F16>(v, a, o[d]);
-                                if (PARTS) o[d] = mfma32<F16>(v, rest, o[d]);
+                                const u32x4 v = columns(vt, u / 2, u % 2, d);
+                                o[d] = mfma32<F16>(v, w[u], o[d]);
+                                if (PARTS) o[d] = mfma32<F16>(v, rest[u], o[d]);
                             }
+                    } else {
+                        u32x4 v[AHEAD + 1];
+#pragma unroll
+                        for (int x = 0; x < AHEAD; ++x) v[x] = columns(vt, x / DB / 2, x / DB % 2, x % DB);
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int x = 0; x < 2 * PB * DB; ++x) {
+                            const int y = x + AHEAD;
+                            if (y < 2 * PB * DB) v[y % (AHEAD + 1)] = columns(vt, y / DB / 2, y / DB % 2, y % DB);
+                            o[x % DB] = mfma32<F16>(v[x % (AHEAD + 1)], w[x / DB], o[x % DB]);
+                            if (PARTS) o[x % DB] = mfma32<F16>(v[x % (AHEAD + 1)], rest[x / DB], o[x % DB]);
+                            __builtin_amdgcn_sched_barrier(0);
                         }
+                    }
                 }
                 if (more) put(buf ^ 1);
             }
@@ -653,7 +727,7 @@ struct Queries {
         if (piece.place < 0) {
             const float v_scale = p.scales ? p.scales[(p.pool.C - 1) * p.pool.H + h] : 1.f;
             const float f = l == 0.f ? 0.f : v_scale / l;
-            if (p.lse && e == 0)
+            if (p.lse && e == 0 && wave % SPLIT == 0)
                 p.lse[(rec.row_off + i) * p.pool.H * G + head] =
                     l > 0.f || l != l ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
             char *dst = p.out.base + (rec.row_off + i) * p.out.s_row + head * p.out.s_head;
@@ -661,20 +735,20 @@ struct Queries {
             for (int d = 0; d < DB; ++d)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int to = 32 * d + 8 * j + 4 * e;
+                    const int to = 32 * (wave % SPLIT * DB + d) + 8 * j + 4 * e;
                     if (to < p.Dv)
                         *reinterpret_cast<u32x2 *>(dst + 2 * to) = u32x2{V::pack(o[d][4 * j] * f, o[d][4 * j + 1] * f),
                                                                         V::pack(o[d][4 * j + 2] * f, o[d][4 * j + 3] * f)};
                 }
         } else {
             const int64_t row = piece.place * p.rows + x - block0;
-            if (e == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * row) = make_float2(m, l);
+            if (e == 0 && wave % SPLIT == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * row) = make_float2(m, l);
             float *dst = p.part_o + row * p.Dv;
 #pragma unroll
             for (int d = 0; d < DB; ++d)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int to = 32 * d + 8 * j + 4 * e;
+                    const int to = 32 * (wave % SPLIT * DB + d) + 8 * j + 4 * e;
                     if (to < p.Dv)
                         *reinterpret_cast<f32x4 *>(dst + to) = f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
                 }
@@ -682,20 +756,21 @@ struct Queries {
     }
 };
 
-// With rows of up to 128 two wavefronts lie on a SIMD.
-template <bool F16, bool E4M3, int DK, int DV, int WAVES, int TEAM, int TILE, bool GENERAL>
-__global__ void __launch_bounds__(64 * WAVES, DK <= 128 ? 2 : 1) kvx_queries_kernel(QueriesParams p, int64_t first, int32_t n) {
-    typedef Queries<F16, E4M3, DK, DV, TEAM, TILE, GENERAL> Work;
+// Two wavefronts lie on a SIMD.
+template <bool F16, bool E4M3, int DK, int DV, int WAVES, int TEAM, int SPLIT, int TILE, bool GENERAL>
+__global__ void __launch_bounds__(64 * WAVES, DK <= 128 || SPLIT > 1 ? 2 : 1) kvx_queries_kernel(QueriesParams p, int64_t first, int32_t n) {
+    typedef Queries<F16, E4M3, DK, DV, TEAM, SPLIT, TILE, GENERAL> Work;
     __shared__ int64_t before[kQueriesGroup + 1];        // steps of one cache head of the records before
     __shared__ __align__(16) typename Work::Rows rows[WAVES / TEAM];
     __shared__ float depth[WAVES][KVX_MAX_DRAFTS];
     __shared__ float ml[TEAM == 1 ? WAVES * 32 * 2 : 1];
+    __shared__ __align__(16) f32x4 shared[SPLIT > 1 ? WAVES * 256 : 1];
     __shared__ int64_t sums[WAVES];
     extern __shared__ __align__(256) char lds[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), H = p.pool.H;
     const int tile_bytes = TILE * 2 * DK * p.pool.C;
-    Work work{rows[TEAM > 1 ? 0 : wave], depth[wave], lds + (TEAM > 1 ? 0 : wave * 2 * tile_bytes), ml, lds, lane, wave,
-              TEAM > 1 ? wave : 0, lane & 31, lane >> 5, p.pool.C == 2, tile_bytes};
+    Work work{rows[TEAM > 1 ? 0 : wave], depth[wave], lds + (TEAM > 1 ? 0 : wave * 2 * tile_bytes), ml, lds, shared, lane, wave,
+              TEAM > 1 ? wave : 0, lane & 31, lane >> 5, p.pool.C == 2, one_tile(DK, p.pool.C), tile_bytes};
     work.address();
     const kvx_queries_req *reqs = p.whole ? p.reqs : p.reqs + first;
     int64_t at = 0, stop = 1, each = 0;
@@ -795,13 +870,13 @@ __global__ void __launch_bounds__(64 * WAVES, DK <= 128 ? 2 : 1) kvx_queries_ker
     }
 }
 
-template <bool F16, bool E4M3, int DK, int DV, int WAVES, int TEAM, int TILE>
+template <bool F16, bool E4M3, int DK, int DV, int WAVES, int TEAM, int SPLIT, int TILE>
 int launch_form(const QueriesParams &p, int64_t first, int64_t n, hipStream_t stream) {
     // few rows are bound by memory, and take one kernel for all scores
     const bool general = TEAM == 1 || p.cap > 0.f || p.slopes;
-    const auto kernel = general ? kvx_queries_kernel<F16, E4M3, DK, DV, WAVES, TEAM, TILE, true>
-                                : kvx_queries_kernel<F16, E4M3, DK, DV, WAVES, TEAM, TILE, TEAM == 1>;
-    const size_t lds = (size_t)2 * TILE * 2 * DK * p.pool.C * (p.waves / TEAM);
+    const auto kernel = general ? kvx_queries_kernel<F16, E4M3, DK, DV, WAVES, TEAM, SPLIT, TILE, true>
+                                : kvx_queries_kernel<F16, E4M3, DK, DV, WAVES, TEAM, SPLIT, TILE, TEAM == 1>;
+    const size_t lds = (size_t)(one_tile(DK, p.pool.C) ? 1 : 2) * TILE * 2 * DK * p.pool.C * (p.waves / TEAM);
     hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.whole ? n : p.shares)), dim3(64 * p.waves), lds, stream, p, first, (int32_t)n);
     return hipGetLastError();
 }
@@ -809,18 +884,17 @@ int launch_form(const QueriesParams &p, int64_t first, int64_t n, hipStream_t st
 template <bool F16, bool E4M3>
 int launch_type(const QueriesParams &p, int64_t first, int64_t n, hipStream_t stream) {
     const int D = p.pool.D;
+    if (D > 256) return launch_form<F16, E4M3, 576, 512, 8, 8, 2, 32>(p, first, n, stream);
     if (p.team == 1) {
-        if (D <= 64) return launch_form<F16, E4M3, 64, 64, 4, 1, 32>(p, first, n, stream);
-        if (D <= 128) return launch_form<F16, E4M3, 128, 128, 4, 1, 32>(p, first, n, stream);
-        if (D <= 256) return launch_form<F16, E4M3, 256, 256, 2, 1, 32>(p, first, n, stream);
-        return launch_form<F16, E4M3, 576, 512, 2, 1, 32>(p, first, n, stream);
+        if (D <= 64) return launch_form<F16, E4M3, 64, 64, 4, 1, 1, 32>(p, first, n, stream);
+        if (D <= 128) return launch_form<F16, E4M3, 128, 128, 4, 1, 1, 32>(p, first, n, stream);
+        return launch_form<F16, E4M3, 256, 256, 2, 1, 1, 32>(p, first, n, stream);
     }
-    if (D <= 64) return launch_form<F16, E4M3, 64, 64, 8, 8, 64>(p, first, n, stream);
+    if (D <= 64) return launch_form<F16, E4M3, 64, 64, 8, 8, 1, 64>(p, first, n, stream);
     if (D <= 128)
-        return p.team == 4 ? launch_form<F16, E4M3, 128, 128, 4, 4, 64>(p, first, n, stream)
-                           : launch_form<F16, E4M3, 128, 128, 8, 8, 64>(p, first, n, stream);
-    if (D <= 256) return launch_form<F16, E4M3, 256, 256, 4, 4, 64>(p, first, n, stream);
-    return launch_form<F16, E4M3, 576, 512, 4, 4, 32>(p, first, n, stream);
+        return p.team == 4 ? launch_form<F16, E4M3, 128, 128, 4, 4, 1, 64>(p, first, n, stream)
+                           : launch_form<F16, E4M3, 128, 128, 8, 8, 1, 64>(p, first, n, stream);
+    return launch_form<F16, E4M3, 256, 256, 8, 8, 2, 32>(p, first, n, stream);
 }
 
 }  // namespace

@@ -102,15 +102,15 @@ constexpr int kWholeUnits = 1024;
 // Fewer steps than this are not worth a share.
 constexpr int kLeastShare = 4;
 
-int tile_of(const QueriesParams &p) { return p.team == 1 || p.pool.D > 256 ? 32 : 64; }
+int tile_of(const QueriesParams &p) { return p.team == 1 || p.pool.D > 128 ? 32 : 64; }
 
 // The kernel for records of up to `most` rows a cache head, and its shape.
 void shape(QueriesParams &p, int64_t most) {
     const int D = p.pool.D;
     // Up to 32 rows: wavefronts take positions of their own; as many as LDS holds tiles for.
-    p.team = most <= 32 ? 1 : D <= 64 || (D <= 128 && most > 128) ? 8 : 4;
-    p.waves = p.team > 1 ? p.team : D <= 128 ? 4 : D <= 256 || p.pool.C == 1 ? 2 : 1;
-    p.rows = 32 * p.team;
+    p.team = D > 256 ? 8 : most <= 32 ? 1 : D > 64 && D <= 128 && most <= 128 ? 4 : 8;
+    p.waves = p.team > 1 ? p.team : D <= 128 ? 4 : 2;
+    p.rows = D > 128 && p.team > 1 ? 128 : 32 * p.team;      // two wavefronts for 32 wide rows
     p.step = tile_of(p) * (p.waves / p.team);
     p.blocks = (int32_t)((most + p.rows - 1) / p.rows);
     if (p.blocks < 1) p.blocks = 1;
