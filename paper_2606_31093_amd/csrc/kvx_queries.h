@@ -41,7 +41,10 @@ int launch_queries_bf16_e4m3(const QueriesParams &p, int64_t first, int64_t n, h
 int launch_queries_f16_e4m3(const QueriesParams &p, int64_t first, int64_t n, hipStream_t stream);
 
 #ifndef KVX_AHEAD
-#define KVX_AHEAD 3
+#define KVX_AHEAD 4
+#endif
+#ifndef KVX_AHEAD_SPLIT
+#define KVX_AHEAD_SPLIT 3
 #endif
 namespace {
 
@@ -133,10 +136,6 @@ __device__ __forceinline__ int64_t share_of(int64_t total, int64_t shares) {
 // bits below x
 __device__ __forceinline__ uint64_t ones(int64_t x) { return x <= 0 ? 0 : x >= 64 ? ~0ull : (1ull << x) - 1; }
 
-// A row's permutation of its 16-byte chunks, in each 8 of them: one chunk of 8
-// successive rows (keys) and two chunks of 4 (values) lie in different banks.
-__device__ __forceinline__ int swirl(int r) { return (r & 3) << 1 | (r >> 2 & 1); }
-
 // 16 bytes a lane to LDS, in order of lanes from `to` on.  In assembly, since the compiler
 // would wait for all of them before reads of LDS; nothing reads what they bring before
 // the wait and the barrier of arrive().
@@ -207,9 +206,9 @@ struct Queries {
     // loads of a wavefront for a tile's K or V, of them all a wavefront's at most
     static constexpr int ALL_LOADS = TILE * SRC / 64, LOADS = (ALL_LOADS + TEAM - 1) / TEAM;
     static constexpr bool PARTS = TEAM == 1;                   // weights in two parts
-    // Reads of LDS are kept so many products ahead where registers are short (left alone the
-    // compiler reads more than there are registers for).
-    static constexpr int AHEAD = SPLIT > 1 ? KVX_AHEAD : 0;
+    // Reads of LDS are kept so many products ahead (left alone the compiler waits for each one
+    // where registers are few, or reads more than there are registers for).
+    static constexpr int AHEAD = SPLIT > 1 ? KVX_AHEAD_SPLIT : KVX_AHEAD;
     static constexpr uint64_t ALL = TILE == 64 ? ~0ull : 0xffffffffull;
     static_assert(TILE * SRC % 64 == 0 && (TILE == 32 || TILE == 64), "tile");
 
@@ -266,11 +265,11 @@ struct Queries {
         for (int x = 0; x < LOADS; ++x) {
             const int piece = x * TEAM + part;
             if (ALL_LOADS % TEAM && piece >= ALL_LOADS) continue;
-            const int u = piece * 64 + ln, row = u / SRC;
-            int chunk = u % SRC;
+            const uint32_t u = piece * 64 + ln, row = u / SRC;
+            uint32_t chunk = u % SRC;
             if (!E4M3) chunk ^= swirl(row);
             const int64_t off = off_of[row];
-            const bool ok = off >= 0 && chunk < have;
+            const bool ok = off >= 0 && (int)chunk < have;
             const char *k = ok ? kbase + off + 16 * chunk : reinterpret_cast<const char *>(&kvx_zeros);
             const char *v = ok ? k + s_c : k;
             if constexpr (E4M3) {
@@ -313,29 +312,39 @@ struct Queries {
         __builtin_amdgcn_sched_barrier(0);
     }
 
-    // Addresses in LDS: a row's permutation concerns the low 3 bits of a chunk's number, so
-    // that there are few of them and the rest is in the instructions.
-    // - K: the lane's row, chunks 2 k + e from the wavefront's first step on, for k % 4
-    // - V, 32 columns from 32 db on for db % 2: 16 lanes give the addresses of 4 rows x 16
-    //   elements, positions 32 pb + 16 s + 4 e + x and 8 behind, x < 4
-    int k_at[4], v_at[2];
+    // LDS.  Chunk x (16 bytes) of row r lies at place x ^ swirl(r) of the row, so that the
+    // 64 banks are read without conflicts: one chunk of 16 rows (keys), and 64 bytes of 4
+    // successive rows (values) lie in different banks.  Where rows begin 128 bytes apart
+    // of 256, two rows lie side by side.
+    static constexpr bool APART = PITCH % 256 != 0;
+    static constexpr int TURNS = APART ? 8 : 16;               // chunks that a row's permutation moves
+    static __device__ __forceinline__ int swirl(int r) {
+        return APART ? (r >> 1 & 1) << 2 | (r >> 2 & 3) : (r & 3) << 2 | (r >> 2 & 3);
+    }
+    // Addresses, those that the permutation makes; the rest is in the instructions.
+    // - K: the lane's row, chunks 2 k + e from the wavefront's first step on
+    // - V, 32 columns from 32 db on: 16 lanes give the addresses of 4 rows x 16 elements,
+    //   positions 32 pb + 16 s + 4 e + x, and 8 behind, x < 4
+    int k_at[TURNS / 2], v_at[TURNS / 4][2];
     __device__ __forceinline__ void address() {
         const int mine = wave % SPLIT;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int chunk = 2 * (mine * KS + k) + e;
-            k_at[k] = c * PITCH + 16 * (chunk ^ swirl(c));
-        }
-        const int l = lane & 15, row = 4 * e + l / 4;
+        for (int k = 0; k < TURNS / 2; ++k) k_at[k] = c * PITCH + 16 * ((2 * (mine * KS + k) + e) ^ swirl(c));
+        const int l = lane & 15;
 #pragma unroll
-        for (int d = 0; d < 2; ++d)
-            v_at[d] = row * PITCH + 16 * ((4 * (mine * DB + d) + (lane >> 4 & 1) * 2 + (l >> 1 & 1)) ^ swirl(row)) + (l & 1) * 8;
+        for (int d = 0; d < TURNS / 4; ++d)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int row = 4 * e + l / 4 + 8 * x;
+                v_at[d][x] = row * PITCH + 16 * ((4 * (mine * DB + d) + (lane >> 4 & 1) * 2 + (l >> 1 & 1)) ^ swirl(row)) + (l & 1) * 8;
+            }
     }
     __device__ __forceinline__ u32x4 keys(const char *k, int pb, int step) const {
-        return *reinterpret_cast<const u32x4 *>(k + k_at[step % 4] + (32 * pb * PITCH + step / 4 * 128));
+        return *reinterpret_cast<const u32x4 *>(k + k_at[step % (TURNS / 2)] + (32 * pb * PITCH + step / (TURNS / 2) * 16 * TURNS));
     }
     __device__ __forceinline__ u32x4 columns(const char *v, int pb, int s, int db) const {
-        const char *a = v + v_at[db % 2] + ((32 * pb + 16 * s) * PITCH + db / 2 * 128), *b = a + 8 * PITCH;
+        const int far = (32 * pb + 16 * s) * PITCH + db / (TURNS / 4) * 16 * TURNS;
+        const char *a = v + v_at[db % (TURNS / 4)][0] + far, *b = v + v_at[db % (TURNS / 4)][1] + far;
         const u32x2 x = bits<u32x2>(__builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)a));
         const u32x2 y = bits<u32x2>(__builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)b));
         return u32x4{x[0], x[1], y[0], y[1]};
@@ -587,12 +596,14 @@ struct Queries {
                             for (int i = 0; i < 16; ++i)
                                 if (!((uint32_t)(shown >> (32 * pb)) >> (8 * (i / 4) + i % 4) & 1)) s[pb][i] = -INFINITY;
                     }
-                    float top = s[0][0];
+                    float tops[4] = {s[0][0], s[0][1], s[0][2], s[0][3]};
 #pragma unroll
                     for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
-                        for (int i = 0; i < 16; i += 2) top = max3(top, s[pb][i], s[pb][i + 1]);
-                    top *= from;
+                        for (int i = 0; i < 16; i += 8)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) tops[j] = max3(tops[j], s[pb][i + 2 * j], s[pb][i + 2 * j + 1]);
+                    float top = max3(tops[0], tops[1], fmaxf(tops[2], tops[3])) * from;
                     if (__any(top - kLift<F16> > m + kSlack)) {
                         top = max_of_halves(top);
                         const float raised = fmaxf(m, top - kLift<F16>), f = weight(m, raised);
@@ -602,13 +613,15 @@ struct Queries {
                         for (int d = 0; d < DB; ++d) o[d] *= f;
                     }
                     const float ref = m == -INFINITY ? 0.f : m;      // then every score is -inf
+                    float sums[2] = {0.f, 0.f};
 #pragma unroll
                     for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             s[pb][i] = exp2_fast(__builtin_fmaf(s[pb][i], from, -ref));
-                            l += s[pb][i];
+                            sums[i % 2] += s[pb][i];
                         }
+                    l += sums[0] + sums[1];
                 }
                 if (team_edge) {
                     // The tile is the team's: it looks over its values together.
@@ -772,6 +785,9 @@ __global__ void __launch_bounds__(64 * WAVES, DK <= 128 || SPLIT > 1 ? 2 : 1) kv
     Work work{rows[TEAM > 1 ? 0 : wave], depth[wave], lds + (TEAM > 1 ? 0 : wave * 2 * tile_bytes), ml, lds, shared, lane, wave,
               TEAM > 1 ? wave : 0, lane & 31, lane >> 5, p.pool.C == 2, one_tile(DK, p.pool.C), tile_bytes};
     work.address();
+    // Two wavefronts of a workgroup lie on a SIMD: with one of them preferred, their products and
+    // the other's exponentials fall together, not products and products.
+    if (WAVES == 8 && wave < 4) __builtin_amdgcn_s_setprio(1);
     const kvx_queries_req *reqs = p.whole ? p.reqs : p.reqs + first;
     int64_t at = 0, stop = 1, each = 0;
     int share = 0;
