@@ -261,6 +261,7 @@ void shape_queries(const kvx_pool *pool, int32_t q_heads, int32_t v_dim, int32_t
     P.pool.D = pool->head_dim;
     P.fd_G = make_fastdiv((uint32_t)(q_heads / pool->num_heads));
     P.e4m3 = pool->elem_bytes == 1;
+    P.token_major = token_major(pool);
     P.Dv = v_dim;
     P.n_reqs = n_reqs;
     P.max_queries = max_queries;

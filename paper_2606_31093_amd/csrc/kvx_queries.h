@@ -114,10 +114,10 @@ __device__ __forceinline__ int64_t scalar(int64_t x) {
                      (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
 }
 
-// Part of a unit: positions [begin, end) for block b of cache head h.
+// Part of a unit: positions [begin, end) for block b of a group of cache heads.
 struct Piece {
     kvx_queries_req rec;
-    int32_t h, b;
+    int32_t group, b;
     uint32_t begin, end;
     int64_t place;               // of its partial results; -1: it is the whole unit
 };
@@ -257,20 +257,37 @@ struct Queries {
         if (lane == 0) rows.there[ring][slot] = there;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
+    // Which row and 16-byte chunk of it a lane's load x takes.  Where rows have a power of two of
+    // chunks, successive loads are R rows apart, and the permutation of a row is that of its
+    // bits: only the first load's are kept.
+    static constexpr bool REGULAR = (SRC & (SRC - 1)) == 0;
+    static constexpr int R = 64 * TEAM / SRC;
+    int row0, chunk0;
+    __device__ __forceinline__ void place(int x, int &row, int &chunk) const {
+        if constexpr (REGULAR) {
+            row = row0 + x * R;
+            chunk = E4M3 ? chunk0 : chunk0 ^ swirl(x * R);
+        } else {
+            const uint32_t u = (x * TEAM + part) * 64 + lane_again();
+            row = u / SRC;
+            chunk = u % SRC;
+            if (!E4M3) chunk ^= swirl(row);
+        }
+    }
     // Asks for this wavefront's share of a tile's rows, zeros where there is none and behind head_dim.
-    __device__ __forceinline__ void load(int buf, const int64_t *off_of) {
+    // WHOLE: all rows are there, and full.
+    template <bool WHOLE>
+    __device__ __forceinline__ void load_rows(int buf, const int64_t *off_of) {
         const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)(lds + buf * tile_bytes);
-        const int ln = lane_again();
 #pragma unroll
         for (int x = 0; x < LOADS; ++x) {
             const int piece = x * TEAM + part;
             if (ALL_LOADS % TEAM && piece >= ALL_LOADS) continue;
-            const uint32_t u = piece * 64 + ln, row = u / SRC;
-            uint32_t chunk = u % SRC;
-            if (!E4M3) chunk ^= swirl(row);
+            int row, chunk;
+            place(x, row, chunk);
             const int64_t off = off_of[row];
-            const bool ok = off >= 0 && (int)chunk < have;
-            const char *k = ok ? kbase + off + 16 * chunk : reinterpret_cast<const char *>(&kvx_zeros);
+            const bool ok = WHOLE || (off >= 0 && chunk < have);
+            const char *k = ok ? kbase + off + (uint32_t)(16 * chunk) : reinterpret_cast<const char *>(&kvx_zeros);
             const char *v = ok ? k + s_c : k;
             if constexpr (E4M3) {
                 staged[x][0] = *reinterpret_cast<const u32x4 *>(k);
@@ -282,16 +299,20 @@ struct Queries {
             }
         }
     }
+    __device__ __forceinline__ void load(int buf, const int64_t *off_of, uint64_t there) {
+        if (there == ALL && have == SRC) load_rows<true>(buf, off_of);
+        else load_rows<false>(buf, off_of);
+    }
     // e4m3: what load() has brought, widened, to LDS.
     __device__ __forceinline__ void put(int buf) {
         if constexpr (E4M3) {
             char *to = lds + buf * tile_bytes;
-            const int ln = lane_again();
 #pragma unroll
             for (int x = 0; x < LOADS; ++x) {
-                const int piece = x * TEAM + part;
-                if (ALL_LOADS % TEAM && piece >= ALL_LOADS) continue;
-                const int u = piece * 64 + ln, row = u / SRC, chunk = u % SRC * 2;
+                if (ALL_LOADS % TEAM && x * TEAM + part >= ALL_LOADS) continue;
+                int row, chunk;
+                place(x, row, chunk);
+                chunk *= 2;
 #pragma unroll
                 for (int kv = 0; kv < 2; ++kv) {
                     if (kv && !two) continue;
@@ -330,6 +351,8 @@ struct Queries {
         const int mine = wave % SPLIT;
 #pragma unroll
         for (int k = 0; k < TURNS / 2; ++k) k_at[k] = c * PITCH + 16 * ((2 * (mine * KS + k) + e) ^ swirl(c));
+        row0 = (part * 64 + lane) / SRC;
+        chunk0 = (part * 64 + lane) % SRC ^ (E4M3 ? 0 : swirl(row0));
         const int l = lane & 15;
 #pragma unroll
         for (int d = 0; d < TURNS / 4; ++d)
@@ -381,7 +404,7 @@ struct Queries {
         end = piece.end;
         first = rec.start;
         bad = 0;
-        int x0, streams, h_rows;
+        int x0, streams, h_rows, h, stream;       // the wavefront's cache head, its place among those of the head
         bool active;
         // This lane's row; past the last one, that one once more.
         int at;                          // its position
@@ -389,6 +412,7 @@ struct Queries {
         uint64_t drafts = 0;             // and these drafts
         float slope = 0.f, cap2 = 0.f, cap_unit = 0.f, unit;
         bool is_tree, biased;
+        uint32_t past;                   // positions below it are at or behind all rows of the wavefront
         u32x4 qv[KS];
         // Positions that all rows of the wavefront see, that some see, and that all of the
         // workgroup see.  In a tree depths differ within a block: the drafts and the last
@@ -396,9 +420,11 @@ struct Queries {
         Span all, some, block_all;
         {
             const QueriesParams p = again();
-            const int G = p.fd_G.d, h = piece.h, n_rows = rec.n_queries * G;
+            const int G = p.fd_G.d, n_rows = rec.n_queries * G;
             h_rows = n_rows;
-            streams = p.waves / TEAM;
+            streams = TEAM > 1 ? 1 : p.waves / p.heads;
+            stream = TEAM > 1 ? 0 : wave % streams;
+            h = TEAM > 1 ? piece.group : piece.group * p.heads + wave / streams;
             kbase = p.pool.base + h * p.pool.s_h;
             s_p = p.pool.s_p;
             s_c = p.pool.s_c;
@@ -464,6 +490,7 @@ struct Queries {
             };
             Span unused;
             bounds(x0, x0 + 31, all, some);
+            past = base + (is_tree ? 0 : (int)fd_div(p.fd_G, x0 < n_rows ? x0 : n_rows - 1) + 1);
             bounds(block0, block0 + p.rows - 1, block_all, unused);
         }
 
@@ -474,7 +501,7 @@ struct Queries {
             for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
         float m = -INFINITY, l = 0.f;
 
-        uint32_t t0 = begin + (TEAM > 1 ? 0 : wave * TILE);
+        uint32_t t0 = begin + stream * TILE;
         const uint32_t step = TILE * streams;
         if (t0 < end) {
             // Tiles are resolved TEAM at a time, one by each wavefront, while the TEAM before are used;
@@ -482,7 +509,7 @@ struct Queries {
             const uint32_t mine = t0 + part * step;
             resolve(mine, look(mine), 0, part);
             if (TEAM > 1) __syncthreads();
-            load(0, rows.off[0][0]);
+            load(0, rows.off[0][0], scalar((int64_t)rows.there[0][0]));
             put(0);
             int32_t page = look(mine + TEAM * step);
             for (int k = 0; t0 < end; t0 += step, ++k) {
@@ -491,7 +518,7 @@ struct Queries {
                     // the tile before has been used
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                     __builtin_amdgcn_s_barrier();
-                    load(0, rows.off[ring][slot]);
+                    load(0, rows.off[ring][slot], scalar((int64_t)rows.there[ring][slot]));
                     put(0);
                 }
                 arrive();
@@ -500,8 +527,8 @@ struct Queries {
                     page = look(t0 + (2 * TEAM + part) * step);
                 }
                 const bool more = t0 + step < end && !(SPLIT > 1 && once);
-                const int next = k + 1;
-                if (more) load(buf ^ 1, rows.off[next / TEAM & 1][next & (TEAM - 1)]);
+                const int next = k + 1, next_ring = next / TEAM & 1, next_slot = next & (TEAM - 1);
+                if (more) load(buf ^ 1, rows.off[next_ring][next_slot], scalar((int64_t)rows.there[next_ring][next_slot]));
                 const uint64_t here = scalar((int64_t)rows.there[ring][slot]);
                 const char *kt = lds + buf * tile_bytes, *vt = kt + (two ? TILE * PITCH : 0);
                 const bool on = active && t0 < some.hi && t0 + TILE > some.lo;
@@ -550,6 +577,10 @@ struct Queries {
                 }
                 if (on) {
                     if (GENERAL) {
+                        const float far = (float)(at - (int)(t0 + 4 * e));
+                        // all keys lie behind: the bias is linear in the position
+                        const bool behind = biased && t0 + TILE <= past;
+                        float by = 1.f;
                         if (cap_unit > 0.f) {
 #pragma unroll
                             for (int pb = 0; pb < PB; ++pb)
@@ -557,13 +588,22 @@ struct Queries {
                                 for (int i = 0; i < 16; ++i)
                                     s[pb][i] = __builtin_fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + exp2_fast(s[pb][i] * cap_unit)), cap2);
                         } else {
+                            by = unit;
+                        }
+                        if (behind) {
+                            const float from_here = -slope * far;
 #pragma unroll
                             for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
-                                for (int i = 0; i < 16; ++i) s[pb][i] *= unit;
+                                for (int i = 0; i < 16; ++i)
+                                    s[pb][i] = __builtin_fmaf(s[pb][i], by, __builtin_fmaf(slope, (float)(32 * pb + 8 * (i / 4) + i % 4), from_here));
+                        } else {
+#pragma unroll
+                            for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) s[pb][i] *= by;
                         }
-                        if (biased) {
-                            const float far = (float)(at - (int)(t0 + 4 * e));
+                        if (biased && !behind) {
                             if (is_tree && t0 + TILE > (uint32_t)base) {
 #pragma unroll
                                 for (int pb = 0; pb < PB; ++pb)
@@ -696,7 +736,7 @@ struct Queries {
             }
         }
         const QueriesParams p = again();
-        const int G = p.fd_G.d, h = piece.h, block0 = piece.b * p.rows;
+        const int G = p.fd_G.d, block0 = piece.b * p.rows;
         if (bad && p.err) atomicOr(p.err, bad);
         l += __shfl_xor(l, 32);
 
@@ -708,15 +748,17 @@ struct Queries {
                 ml[(wave * 32 + c) * 2 + 1] = l;
             }
             __syncthreads();
+            const int w0 = wave - stream;
             float top = -INFINITY, sum = 0.f;
-            for (int k = 0; k < streams; ++k) top = fmaxf(top, ml[(k * 32 + c) * 2]);
-            for (int k = 0; k < streams; ++k) sum += ml[(k * 32 + c) * 2 + 1] * weight(ml[(k * 32 + c) * 2], top);
+            for (int k = w0; k < w0 + streams; ++k) top = fmaxf(top, ml[(k * 32 + c) * 2]);
+            for (int k = w0; k < w0 + streams; ++k) sum += ml[(k * 32 + c) * 2 + 1] * weight(ml[(k * 32 + c) * 2], top);
             const float f = weight(m, top);
             m = top;
             l = sum;
-            f32x4 *joined = reinterpret_cast<f32x4 *>(all_lds) + lane;         // [value / 4][lane]
+            // [head of the group][value / 4][lane]
+            f32x4 *joined = reinterpret_cast<f32x4 *>(all_lds) + wave / streams * (64 * 4 * DB) + lane;
             for (int turn = 0; turn < streams; ++turn) {
-                if (wave == turn) {
+                if (stream == turn) {
 #pragma unroll
                     for (int d = 0; d < DB; ++d) {
                         o[d] *= f;
@@ -732,7 +774,7 @@ struct Queries {
                 }
                 __syncthreads();
             }
-            if (wave != streams - 1) return;
+            if (stream != streams - 1) return;
         }
         const int x = x0 + c;
         if (x >= h_rows) return;
@@ -754,7 +796,7 @@ struct Queries {
                                                                         V::pack(o[d][4 * j + 2] * f, o[d][4 * j + 3] * f)};
                 }
         } else {
-            const int64_t row = piece.place * p.rows + x - block0;
+            const int64_t row = (piece.place * p.heads + (TEAM > 1 ? 0 : wave / streams)) * p.rows + x - block0;
             if (e == 0 && wave % SPLIT == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * row) = make_float2(m, l);
             float *dst = p.part_o + row * p.Dv;
 #pragma unroll
@@ -780,7 +822,7 @@ __global__ void __launch_bounds__(64 * WAVES, DK <= 128 || SPLIT > 1 ? 2 : 1) kv
     __shared__ __align__(16) f32x4 shared[SPLIT > 1 ? WAVES * 256 : 1];
     __shared__ int64_t sums[WAVES];
     extern __shared__ __align__(256) char lds[];
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), H = p.pool.H;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int tile_bytes = TILE * 2 * DK * p.pool.C;
     Work work{rows[TEAM > 1 ? 0 : wave], depth[wave], lds + (TEAM > 1 ? 0 : wave * 2 * tile_bytes), ml, lds, shared, lane, wave,
               TEAM > 1 ? wave : 0, lane & 31, lane >> 5, p.pool.C == 2, one_tile(DK, p.pool.C), tile_bytes};
@@ -818,7 +860,7 @@ __global__ void __launch_bounds__(64 * WAVES, DK <= 128 || SPLIT > 1 ? 2 : 1) kv
         __syncthreads();
         // successive shares on one die
         share = p.shares % 8 == 0 ? blockIdx.x % 8 * (p.shares / 8) + blockIdx.x / 8 : blockIdx.x;
-        const int64_t total = scalar(before[n]) * H;
+        const int64_t total = scalar(before[n]) * p.groups;
         each = share_of(total, p.shares);
         if (share == 0) {
             if (threadIdx.x == 0) *p.total = total;
@@ -830,20 +872,19 @@ __global__ void __launch_bounds__(64 * WAVES, DK <= 128 || SPLIT > 1 ? 2 : 1) kv
     }
     while (at < stop) {
         const QueriesParams p = again();
-        const int H = p.pool.H;
         const kvx_queries_req *reqs = p.whole ? p.reqs : p.reqs + first;
         Piece piece;
         Span s;
         int64_t here = 1;
         if (p.whole) {
-            // Longest first: a record's last blocks see most.  Blocks of a record and head are n_reqs x H
+            // Longest first: a record's last blocks see most.  Blocks of a record and group are n_reqs x groups
             // workgroups apart: with a multiple of 8 of them on one die, whose cache holds their keys.
-            const int64_t id = first + blockIdx.x, lists = (int64_t)p.n_reqs * H, rank = quotient(id, lists);
-            const int list = (int)(id - rank * lists), r = list / H;
-            piece.h = list - r * H;
+            const int64_t id = first + blockIdx.x, lists = (int64_t)p.n_reqs * p.groups, rank = quotient(id, lists);
+            const int list = (int)(id - rank * lists), r = list / p.groups;
+            piece.group = list - r * p.groups;
             piece.rec = scalar(reqs[r]);
             if (!valid(piece.rec, p)) {
-                if (rank == 0 && piece.h == 0 && threadIdx.x == 0 && p.err) atomicOr(p.err, KVX_DERR_BAD_REQ);
+                if (rank == 0 && piece.group == 0 && threadIdx.x == 0 && p.err) atomicOr(p.err, KVX_DERR_BAD_REQ);
                 return;
             }
             const int blocks = blocks_of(piece.rec, p);
@@ -857,14 +898,14 @@ __global__ void __launch_bounds__(64 * WAVES, DK <= 128 || SPLIT > 1 ? 2 : 1) kv
             int lo = 0, hi = n;          // the record: the last one whose steps begin at or before `at`
             while (hi - lo > 1) {
                 const int mid = (lo + hi) / 2;
-                if (before[mid] * H <= at) lo = mid;
+                if (before[mid] * p.groups <= at) lo = mid;
                 else hi = mid;
             }
             const int r = __builtin_amdgcn_readfirstlane(lo);
-            const int64_t base = scalar(before[r]) * H, per = scalar(before[r + 1]) - scalar(before[r]);
+            const int64_t base = scalar(before[r]) * p.groups, per = scalar(before[r + 1]) - scalar(before[r]);
             piece.rec = scalar(reqs[r]);
-            piece.h = (int)quotient(at - base, per);
-            int64_t in = at - base - piece.h * per;
+            piece.group = (int)quotient(at - base, per);
+            int64_t in = at - base - piece.group * per;
             int steps;
             for (piece.b = 0;; ++piece.b) {
                 s = span_of_block(piece.rec, p, piece.b);
@@ -877,7 +918,7 @@ __global__ void __launch_bounds__(64 * WAVES, DK <= 128 || SPLIT > 1 ? 2 : 1) kv
             piece.begin = (s.lo & -kTile) + (uint32_t)in * p.step;
             const uint32_t to = piece.begin + (uint32_t)here * p.step;
             piece.end = to < s.hi ? to : s.hi;
-            if (in == 0 && threadIdx.x == 0) p.units[((int64_t)r * H + piece.h) * p.blocks + piece.b] = UnitSteps{at, steps};
+            if (in == 0 && threadIdx.x == 0) p.units[((int64_t)r * p.groups + piece.group) * p.blocks + piece.b] = UnitSteps{at, steps};
         }
         if (s.hi <= s.lo) piece.end = piece.begin;
         work.run(piece);

@@ -19,7 +19,7 @@ __global__ void __launch_bounds__(kThreads) kvx_queries_join_kernel(QueriesParam
     const int64_t id = first + blockIdx.x, unit = id / runs;
     const int run = (int)(id - unit * runs), H = p.pool.H, G = p.fd_G.d;
     const int64_t list = unit / p.blocks;
-    const int b = (int)(unit - list * p.blocks), r = (int)(list / H), h = (int)(list - (int64_t)r * H);
+    const int b = (int)(unit - list * p.blocks), r = (int)(list / p.groups), group = (int)(list - (int64_t)r * p.groups);
     const kvx_queries_req rec = p.reqs[r0 + r];
     if (!valid(rec, p) || b >= blocks_of(rec, p)) return;
     const UnitSteps u = p.units[unit];
@@ -27,10 +27,11 @@ __global__ void __launch_bounds__(kThreads) kvx_queries_join_kernel(QueriesParam
     const int64_t k0 = quotient(u.first, each), k1 = quotient(u.first + u.steps - 1, each);
     if (k0 == k1) return;                                // written by the first launch
     const int cols = p.Dv / 4, lines = kThreads / cols, col = threadIdx.x % cols, line = threadIdx.x / cols;
-    const int per = lines / split, mine = line % split;
-    const int x = run * per + line / split;              // row of the block
-    const int64_t row = (int64_t)b * p.rows + x;
-    const bool on = line < per * split && x < p.rows && row < (int64_t)rec.n_queries * G;
+    const int per = lines / split, mine = line % split, slots = p.heads * p.rows;
+    const int x = run * per + line / split;              // row of the block, of each head of the group
+    const int h = group * p.heads + x / p.rows;
+    const int64_t row = (int64_t)b * p.rows + x % p.rows;
+    const bool on = line < per * split && x < slots && row < (int64_t)rec.n_queries * G;
     float m = -INFINITY, l = 0.f;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
     if (on) {
@@ -41,7 +42,7 @@ __global__ void __launch_bounds__(kThreads) kvx_queries_join_kernel(QueriesParam
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int64_t part = k + i * split <= k1 ? k + i * split : k1;
-                const int64_t at = place_of(u.first, part, each, p.shares) * p.rows + x;
+                const int64_t at = place_of(u.first, part, each, p.shares) * slots + x;
                 ml[i] = *reinterpret_cast<const float2 *>(p.part_ml + 2 * at);
                 y[i] = *reinterpret_cast<const f32x4 *>(p.part_o + at * p.Dv + 4 * col);
             }
@@ -111,7 +112,11 @@ void shape(QueriesParams &p, int64_t most) {
     p.team = D > 256 ? 8 : most <= 32 ? 1 : D > 64 && D <= 128 && most <= 128 ? 4 : 8;
     p.waves = p.team > 1 ? p.team : D <= 128 ? 4 : 2;
     p.rows = D > 128 && p.team > 1 ? 128 : 32 * p.team;      // two wavefronts for 32 wide rows
-    p.step = tile_of(p) * (p.waves / p.team);
+    // Rows of the cache that lie side by side, several heads of a position, are read by one workgroup.
+    p.heads = 1;
+    while (p.team == 1 && p.token_major && 2 * p.heads <= p.waves && p.pool.H % (2 * p.heads) == 0) p.heads *= 2;
+    p.groups = p.pool.H / p.heads;
+    p.step = tile_of(p) * (p.team > 1 ? 1 : p.waves / p.heads);
     p.blocks = (int32_t)((most + p.rows - 1) / p.rows);
     if (p.blocks < 1) p.blocks = 1;
 }
@@ -127,19 +132,19 @@ int32_t shares_for(const QueriesParams &p, int64_t units) {
 // Workspace of `units` units.
 int64_t split_bytes(const QueriesParams &p, int64_t units) {
     // two parts a share, its first and its last
-    const int64_t rows = 2 * (int64_t)p.shares * p.rows;
+    const int64_t rows = 2 * (int64_t)p.shares * p.heads * p.rows;
     return 16 + units * (int64_t)sizeof(UnitSteps) + rows * 8 + rows * p.Dv * 4 + 64;
 }
 
 int64_t units_of(const QueriesParams &p) {
-    return (p.n_reqs < kQueriesGroup ? p.n_reqs : (int64_t)kQueriesGroup) * p.pool.H * p.blocks;
+    return (p.n_reqs < kQueriesGroup ? p.n_reqs : (int64_t)kQueriesGroup) * p.groups * p.blocks;
 }
 
 }  // namespace
 
 void plan_queries(QueriesParams &p) {
     shape(p, (int64_t)p.max_queries * p.fd_G.d);
-    p.whole = most_steps(p) <= kWholeSteps || (int64_t)p.n_reqs * p.pool.H * p.blocks >= kWholeUnits;
+    p.whole = most_steps(p) <= kWholeSteps || (int64_t)p.n_reqs * p.groups * p.blocks >= kWholeUnits;
     p.shares = shares_for(p, units_of(p));
 }
 
@@ -166,7 +171,7 @@ int64_t queries_workspace(QueriesParams &p, char *base) {
         at += (bytes + 15) / 16 * 16;
         return x;
     };
-    const int64_t rows = 2 * (int64_t)p.shares * p.rows;
+    const int64_t rows = 2 * (int64_t)p.shares * p.heads * p.rows;
     p.total = reinterpret_cast<int64_t *>(take(16));
     if (p.whole) return at;
     p.units = reinterpret_cast<UnitSteps *>(take(units_of(p) * (int64_t)sizeof(UnitSteps)));
@@ -180,7 +185,7 @@ int launch_queries(const QueriesParams &p, hipStream_t stream) {
                               : (p.e4m3 ? launch_queries_bf16_e4m3 : launch_queries_bf16);
     int e;
     if (p.whole) {
-        const int64_t units = (int64_t)p.n_reqs * p.pool.H * p.blocks;
+        const int64_t units = (int64_t)p.n_reqs * p.groups * p.blocks;
         for (int64_t at = 0; at < units; at += kMaxBlocks) {
             const int64_t n = units - at < kMaxBlocks ? units - at : kMaxBlocks;
             if ((e = launch(p, at, n, stream)) != hipSuccess) return e;
@@ -190,12 +195,13 @@ int launch_queries(const QueriesParams &p, hipStream_t stream) {
     for (int64_t r0 = 0; r0 < p.n_reqs; r0 += kQueriesGroup) {
         const int64_t n = p.n_reqs - r0 < kQueriesGroup ? p.n_reqs - r0 : kQueriesGroup;
         if ((e = launch(p, r0, n, stream)) != hipSuccess) return e;
-        const int64_t units = n * p.pool.H * p.blocks;
+        const int64_t units = n * p.groups * p.blocks;
         // Rows of threads that share a row's parts: as many as there are parts, on average.
         const int lines = kThreads / (p.Dv / 4);
         int split = 1;
         while (2 * split <= lines && units * 8 * split < p.shares) split *= 2;
-        const int rows = p.blocks == 1 && (int64_t)p.max_queries * p.fd_G.d < p.rows ? p.max_queries * p.fd_G.d : p.rows;
+        const int rows = p.heads == 1 && p.blocks == 1 && (int64_t)p.max_queries * p.fd_G.d < p.rows ? p.max_queries * p.fd_G.d
+                                                                                                       : p.heads * p.rows;
         const int32_t runs = (rows + lines / split - 1) / (lines / split);
         const size_t lds = split > 1 ? sizeof(float) * lines * (p.Dv + 2) : 0;
         for (int64_t at = 0; at < units * runs; at += kMaxBlocks) {

@@ -31,17 +31,18 @@ struct QueriesParams {
     const uint64_t *tree;        // nullptr: prompts
     int32_t n_reqs, max_queries, max_tokens;
     uint32_t *err;
-    int32_t f16, e4m3;
+    int32_t f16, e4m3, token_major;
     FastDiv fd_G;
-    // launch: wavefronts of a workgroup, and how many share a tile; rows of a block,
-    // blocks of a record and cache head at most; positions of a step; whether every
-    // unit has its own workgroup (whole), else the shares of the steps
-    int32_t waves, team, rows, blocks, step, whole, shares;
+    // launch: wavefronts of a workgroup, and how many share a tile; cache heads of a
+    // workgroup, and the groups of them; rows of a block, blocks of a record and cache
+    // head at most; positions of a step; whether every unit has its own workgroup
+    // (whole), else the shares of the steps
+    int32_t waves, team, heads, groups, rows, blocks, step, whole, shares;
     // workspace
     int64_t *total;              // steps of the launch
-    UnitSteps *units;            // [record of the launch][cache head][block]
-    float *part_ml;              // [place][row][2]
-    float *part_o;               // [place][row][Dv]
+    UnitSteps *units;            // [record of the launch][group of cache heads][block]
+    float *part_ml;              // [place][head of the group][row][2]
+    float *part_o;               // [place][head of the group][row][Dv]
 };
 
 // The division of a call's work, from the sizes alone; the workspace of a planned
