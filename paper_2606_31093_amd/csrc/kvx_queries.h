@@ -182,6 +182,9 @@ __device__ __forceinline__ float max_of_halves(float x) {
     return fmaxf(bits<float>((uint32_t)y[0]), bits<float>((uint32_t)y[1]));
 }
 
+// A branch that is seldom taken: its code lies elsewhere.
+__device__ __forceinline__ bool seldom(bool x) { return __builtin_expect_with_probability(x, 0, 0.9999); }
+
 // The kernel's parameters, its first argument, read anew: kept from the kernel's begin to
 // its end they would take more scalar registers than there are.
 __device__ __forceinline__ QueriesParams again() {
@@ -300,8 +303,8 @@ struct Queries {
         }
     }
     __device__ __forceinline__ void load(int buf, const int64_t *off_of, uint64_t there) {
-        if (there == ALL && have == SRC) load_rows<true>(buf, off_of);
-        else load_rows<false>(buf, off_of);
+        if (seldom(there != ALL || have != SRC)) load_rows<false>(buf, off_of);
+        else load_rows<true>(buf, off_of);
     }
     // e4m3: what load() has brought, widened, to LDS.
     __device__ __forceinline__ void put(int buf) {
@@ -411,6 +414,8 @@ struct Queries {
         uint32_t lo, hi;                 // it sees [lo, hi)
         uint64_t drafts = 0;             // and these drafts
         float slope = 0.f, cap2 = 0.f, cap_unit = 0.f, unit;
+        uint32_t slopes[2] = {0, 0};
+        bool linear = false;
         bool is_tree, biased;
         uint32_t past;                   // positions below it are at or behind all rows of the wavefront
         u32x4 qv[KS];
@@ -470,7 +475,14 @@ struct Queries {
             lo = p.window && near > rec.start ? near : rec.start;
             const int seen = is_tree ? base : at + 1 > rec.prefix ? at + 1 : rec.prefix;
             hi = seen < rec.end ? seen : rec.end;
-            if (biased) slope = p.slopes[h * G + g] * kLog2e;
+            if (biased) {
+                slope = p.slopes[h * G + g] * kLog2e;
+                // in three parts of the rows' type, for a product with whole numbers up to 63
+                const float x = slope / unit, a = V::lo(V::pack(x, 0.f)), b = V::lo(V::pack(x - a, 0.f));
+                slopes[0] = V::pack(a, b);
+                slopes[1] = V::pack(x - a - b, 0.f);
+                linear = cap_unit == 0.f && !__any(!(fabsf(x) < 1024.f));
+            }
             const char *src = p.q.base + (rec.row_off + i) * p.q.s_row + (int64_t)(h * G + g) * p.q.s_head;
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
@@ -522,7 +534,7 @@ struct Queries {
                     put(0);
                 }
                 arrive();
-                if (slot == 0) {
+                if (TEAM > 1 ? seldom(slot == 0) : true) {
                     resolve(t0 + (TEAM + part) * step, page, ring ^ 1, part);
                     page = look(t0 + (2 * TEAM + part) * step);
                 }
@@ -536,6 +548,8 @@ struct Queries {
                 const bool team_edge = here != ALL || t0 < block_all.lo || t0 + TILE > block_all.hi;
                 f32x16 s[PB];            // scores, then weights
                 uint64_t sees = ALL;
+                // all keys lie behind, and none of the bias has to follow a cap: it is linear in the position
+                const bool straight = GENERAL && linear && t0 + TILE <= past;
 #pragma unroll
                 for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
@@ -550,6 +564,14 @@ struct Queries {
                         u32x4 a[AHEAD + 1];
 #pragma unroll
                         for (int u = 0; u < AHEAD; ++u) a[u] = keys(kt, u % PB, u / PB);
+                        if (GENERAL && straight && wave % SPLIT == 0) {
+                            // slope * (position within the tile) as one more step of the product
+#pragma unroll
+                            for (int pb = 0; pb < PB; ++pb) {
+                                const uint32_t off = V::pack((float)(32 * pb + c), (float)(32 * pb + c));
+                                s[pb] = mfma32<F16>(e == 0 ? u32x4{off, off & 0xffff, 0, 0} : u32x4{0, 0, 0, 0}, u32x4{slopes[0], slopes[1], 0, 0}, s[pb]);
+                            }
+                        }
                         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                         for (int u = 0; u < KS * PB; ++u) {
@@ -575,56 +597,42 @@ struct Queries {
                         for (int j = 0; j < 4; ++j) s[0][4 * i + j] += x[j];
                     }
                 }
+                float from = unit, shift = 0.f;  // scores are s * from + shift
                 if (on) {
                     if (GENERAL) {
-                        const float far = (float)(at - (int)(t0 + 4 * e));
-                        // all keys lie behind: the bias is linear in the position
-                        const bool behind = biased && t0 + TILE <= past;
-                        float by = 1.f;
-                        if (cap_unit > 0.f) {
+                        if (seldom(cap_unit > 0.f)) {
+                            // cap tanh(x) = cap - 2 cap / (1 + e^2x)
 #pragma unroll
                             for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
-                                for (int i = 0; i < 16; ++i)
-                                    s[pb][i] = __builtin_fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + exp2_fast(s[pb][i] * cap_unit)), cap2);
-                        } else {
-                            by = unit;
+                                for (int i = 0; i < 16; ++i) s[pb][i] = __builtin_amdgcn_rcpf(-1.f - exp2_fast(s[pb][i] * cap_unit));
+                            from = 2.f * cap2;
+                            shift = cap2;
                         }
-                        if (behind) {
-                            const float from_here = -slope * far;
+                        if (straight) {
+                            shift = -slope * (float)(at - (int)t0);      // the rest of the bias is in the product
+                        } else if (seldom(biased)) {
+                            const float far = (float)(at - (int)(t0 + 4 * e));
+                            const bool by_depth = is_tree && t0 + TILE > (uint32_t)base;
 #pragma unroll
                             for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
-                                for (int i = 0; i < 16; ++i)
-                                    s[pb][i] = __builtin_fmaf(s[pb][i], by, __builtin_fmaf(slope, (float)(32 * pb + 8 * (i / 4) + i % 4), from_here));
-                        } else {
-#pragma unroll
-                            for (int pb = 0; pb < PB; ++pb)
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) s[pb][i] *= by;
-                        }
-                        if (biased && !behind) {
-                            if (is_tree && t0 + TILE > (uint32_t)base) {
-#pragma unroll
-                                for (int pb = 0; pb < PB; ++pb)
-#pragma unroll
-                                    for (int i = 0; i < 16; ++i) {
-                                        const int off = 32 * pb + 8 * (i / 4) + i % 4, j = (int)(t0 + 4 * e + off) - base;
+                                for (int i = 0; i < 16; ++i) {
+                                    const int off = 32 * pb + 8 * (i / 4) + i % 4;
+                                    float d = far - (float)off;
+                                    if (by_depth) {
+                                        if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                                        const int j = (int)(t0 + 4 * e + off) - base;
                                         const bool draft = j >= 0 && j < rec.n_queries;
-                                        const float d = draft ? (float)(at - base) - depth[draft ? j : 0] : far - (float)off;
-                                        s[pb][i] = __builtin_fmaf(-slope, fabsf(d), s[pb][i]);
+                                        if (draft) d = (float)(at - base) - depth[j];
                                     }
-                            } else {
-#pragma unroll
-                                for (int pb = 0; pb < PB; ++pb)
-#pragma unroll
-                                    for (int i = 0; i < 16; ++i)
-                                        s[pb][i] = __builtin_fmaf(-slope, fabsf(far - (float)(32 * pb + 8 * (i / 4) + i % 4)), s[pb][i]);
-                            }
+                                    s[pb][i] = __builtin_fmaf(-slope, fabsf(d), __builtin_fmaf(s[pb][i], from, shift));
+                                }
+                            from = 1.f;
+                            shift = 0.f;
                         }
                     }
-                    const float from = GENERAL ? 1.f : unit;
-                    if (edge) {
+                    if (seldom(edge)) {
                         uint64_t v = ones((int64_t)hi - t0) & ~ones((int64_t)lo - t0);
                         const int64_t to = (int64_t)base - t0;
                         if (is_tree && to < 64 && to > -64) v |= to >= 0 ? drafts << to : drafts >> -to;
@@ -643,8 +651,8 @@ struct Queries {
                         for (int i = 0; i < 16; i += 8)
 #pragma unroll
                             for (int j = 0; j < 4; ++j) tops[j] = max3(tops[j], s[pb][i + 2 * j], s[pb][i + 2 * j + 1]);
-                    float top = max3(tops[0], tops[1], fmaxf(tops[2], tops[3])) * from;
-                    if (__any(top - kLift<F16> > m + kSlack)) {
+                    float top = __builtin_fmaf(max3(tops[0], tops[1], fmaxf(tops[2], tops[3])), from, shift);
+                    if (seldom(__any(top - kLift<F16> > m + kSlack))) {
                         top = max_of_halves(top);
                         const float raised = fmaxf(m, top - kLift<F16>), f = weight(m, raised);
                         m = raised;
@@ -652,24 +660,24 @@ struct Queries {
 #pragma unroll
                         for (int d = 0; d < DB; ++d) o[d] *= f;
                     }
-                    const float ref = m == -INFINITY ? 0.f : m;      // then every score is -inf
+                    const float ref = shift - (m == -INFINITY ? 0.f : m);      // without any, every score is -inf
                     float sums[2] = {0.f, 0.f};
 #pragma unroll
                     for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            s[pb][i] = exp2_fast(__builtin_fmaf(s[pb][i], from, -ref));
+                            s[pb][i] = exp2_fast(__builtin_fmaf(s[pb][i], from, ref));
                             sums[i % 2] += s[pb][i];
                         }
                     l += sums[0] + sums[1];
                 }
-                if (team_edge) {
+                if (seldom(team_edge)) {
                     // The tile is the team's: it looks over its values together.
                     constexpr int MINE = TILE / TEAM;
                     char *v = const_cast<char *>(vt);
                     bool found = any_spoilt(v, part * MINE, MINE);
                     if (TEAM > 1) found = __syncthreads_or(found);
-                    if (found) {
+                    if (seldom(found)) {
                         const uint64_t spoilt_rows = spoilt(v, 0, TILE);
                         for (uint64_t left = spoilt_rows; left && on; left &= left - 1) {
                             const int r = __ffsll((unsigned long long)left) - 1;
@@ -680,7 +688,8 @@ struct Queries {
                             x = __shfl(x, owner);
                             if (!(sees >> r & 1)) continue;
 #pragma unroll
-                            for (int d = 0; d < DB; ++d)
+                            for (int d = 0; d < DB; ++d) {
+                                __builtin_amdgcn_sched_barrier(0);       // seldom run: few registers
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) {
                                     const u32x2 y = *reinterpret_cast<const u32x2 *>(v + r * PITCH + 16 * ((4 * (wave % SPLIT * DB + d) + i) ^ swirl(r)) + 8 * e);
@@ -689,6 +698,7 @@ struct Queries {
                                     o[d][4 * i + 2] += x * V::lo(y[1]);
                                     o[d][4 * i + 3] += x * V::hi(y[1]);
                                 }
+                            }
                         }
                         if (TEAM > 1) __syncthreads();
                         for (int r = part * MINE; r < (part + 1) * MINE; ++r)
@@ -880,7 +890,8 @@ __global__ void __launch_bounds__(64 * WAVES, DK <= 128 || SPLIT > 1 ? 2 : 1) kv
             // Longest first: a record's last blocks see most.  Blocks of a record and group are n_reqs x groups
             // workgroups apart: with a multiple of 8 of them on one die, whose cache holds their keys.
             const int64_t id = first + blockIdx.x, lists = (int64_t)p.n_reqs * p.groups, rank = quotient(id, lists);
-            const int list = (int)(id - rank * lists), r = list / p.groups;
+            // Of several records each die takes every eighth block, so that long ones are no die's alone.
+            const int list = (int)((id - rank * lists + (p.n_reqs > 1 ? rank : 0)) % lists), r = list / p.groups;
             piece.group = list - r * p.groups;
             piece.rec = scalar(reqs[r]);
             if (!valid(piece.rec, p)) {
