@@ -44,7 +44,7 @@ int launch_queries_f16_e4m3(const QueriesParams &p, int64_t first, int64_t n, hi
 #define KVX_AHEAD 4
 #endif
 #ifndef KVX_AHEAD_SPLIT
-#define KVX_AHEAD_SPLIT 3
+#define KVX_AHEAD_SPLIT 2
 #endif
 namespace {
 
@@ -222,6 +222,11 @@ struct Queries {
     };
     Rows &rows;                  // the team's
     float *depth;                // [64], the wavefront's
+    // What a lane's row sees is needed at the edges only, and kept in LDS.
+    struct Sight {
+        uint64_t drafts;         // of the drafts
+        uint32_t lo, hi;         // and of the positions before them [lo, hi)
+    } *sight;                    // [64], the wavefront's
     char *lds;                   // [2][rows of K, rows of V if there are two], the team's
     float *ml;                   // [wavefronts][32][2]
     char *all_lds;               // the workgroup's
@@ -242,12 +247,13 @@ struct Queries {
     __device__ __forceinline__ uint64_t entry(uint32_t t) const { return (uint64_t)rec.pt_off + fd_div(fd_T, t); }
     // the page id of position t0 + lane
     __device__ __forceinline__ int32_t look(uint32_t t0) const {
-        const uint32_t t = t0 + lane;
+        const uint32_t t = t0 + lane_again();
         const uint64_t idx = entry(t < end ? t : end - 1);
         return pt[idx < (uint64_t)pt_len ? idx : 0];
     }
     // A tile's row offsets, to place `slot` of half `ring`.
     __device__ __forceinline__ void resolve(uint32_t t0, int32_t page, int ring, int slot) {
+        const int lane = lane_again();
         const uint32_t t = t0 + lane;
         const bool in = lane < TILE && t >= first && t < end;
         const uint32_t at = t < end ? t : end - 1;
@@ -349,28 +355,39 @@ struct Queries {
     // - K: the lane's row, chunks 2 k + e from the wavefront's first step on
     // - V, 32 columns from 32 db on: 16 lanes give the addresses of 4 rows x 16 elements,
     //   positions 32 pb + 16 s + 4 e + x, and 8 behind, x < 4
-    int k_at[TURNS / 2], v_at[TURNS / 4][2];
+    // Where a row has 16 places the others follow from one by an exclusive or, tiles lying at
+    // multiples of 256 bytes.
+    int k_at[APART ? TURNS / 2 : 1], v_at[APART ? TURNS / 4 : 1];
     __device__ __forceinline__ void address() {
-        const int mine = wave % SPLIT;
-#pragma unroll
-        for (int k = 0; k < TURNS / 2; ++k) k_at[k] = c * PITCH + 16 * ((2 * (mine * KS + k) + e) ^ swirl(c));
+        const int mine = wave % SPLIT, l = lane & 15, row = 4 * e + l / 4;
         row0 = (part * 64 + lane) / SRC;
         chunk0 = (part * 64 + lane) % SRC ^ (E4M3 ? 0 : swirl(row0));
-        const int l = lane & 15;
 #pragma unroll
-        for (int d = 0; d < TURNS / 4; ++d)
+        for (int k = 0; k < (APART ? TURNS / 2 : 1); ++k) k_at[k] = c * PITCH + 16 * ((2 * (mine * KS + k) + e) ^ swirl(c));
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const int row = 4 * e + l / 4 + 8 * x;
-                v_at[d][x] = row * PITCH + 16 * ((4 * (mine * DB + d) + (lane >> 4 & 1) * 2 + (l >> 1 & 1)) ^ swirl(row)) + (l & 1) * 8;
-            }
+        for (int d = 0; d < (APART ? TURNS / 4 : 1); ++d)
+            v_at[d] = row * PITCH + 16 * ((4 * (mine * DB + d) + (lane >> 4 & 1) * 2 + (l >> 1 & 1)) ^ swirl(row)) + (l & 1) * 8;
     }
-    __device__ __forceinline__ u32x4 keys(const char *k, int pb, int step) const {
-        return *reinterpret_cast<const u32x4 *>(k + k_at[step % (TURNS / 2)] + (32 * pb * PITCH + step / (TURNS / 2) * 16 * TURNS));
+    // lowest addresses of a tile's reads
+    __device__ __forceinline__ void at_tile(const char *k, const char *v, uint32_t *ka, uint32_t *va) const {
+        const uint32_t kt = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)k;
+        const uint32_t vt = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)v;
+#pragma unroll
+        for (int i = 0; i < (APART ? TURNS / 2 : 1); ++i) ka[i] = kt + k_at[i];
+#pragma unroll
+        for (int i = 0; i < (APART ? TURNS / 4 : 1); ++i) va[i] = vt + v_at[i];
     }
-    __device__ __forceinline__ u32x4 columns(const char *v, int pb, int s, int db) const {
-        const int far = (32 * pb + 16 * s) * PITCH + db / (TURNS / 4) * 16 * TURNS;
-        const char *a = v + v_at[db % (TURNS / 4)][0] + far, *b = v + v_at[db % (TURNS / 4)][1] + far;
+    typedef const __attribute__((address_space(3))) char *Lds;
+    __device__ __forceinline__ u32x4 keys(const uint32_t *ka, int pb, int step) const {
+        const int turn = step % (TURNS / 2), far = 32 * pb * PITCH + step / (TURNS / 2) * 16 * TURNS;
+        const Lds at = (Lds)(APART ? ka[turn % (APART ? TURNS / 2 : 1)] : ka[0] ^ 32 * turn);
+        return *(const __attribute__((address_space(3))) u32x4 *)(at + far);
+    }
+    __device__ __forceinline__ u32x4 columns(const uint32_t *va, int pb, int s, int db) const {
+        const int turn = db % (TURNS / 4), far = (32 * pb + 16 * s) * PITCH + db / (TURNS / 4) * 16 * TURNS;
+        const uint32_t at = APART ? va[turn % (APART ? TURNS / 4 : 1)] : va[0] ^ 64 * turn;
+        // 8 rows on the permutation differs in its second bit
+        const Lds a = (Lds)at + far, b = (Lds)(at ^ 32) + far + 8 * PITCH;
         const u32x2 x = bits<u32x2>(__builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)a));
         const u32x2 y = bits<u32x2>(__builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)b));
         return u32x4{x[0], x[1], y[0], y[1]};
@@ -379,6 +396,7 @@ struct Queries {
     // Rows r0 .. r0 + n - 1 of V that hold values which are not finite.
     __device__ __forceinline__ uint64_t spoilt(const char *v, int r0, int n) const {
         uint64_t found_rows = 0;
+        const int lane = lane_again();
         for (int r = r0; r < r0 + n; ++r) {
             bool found = false;
             if (lane < DV / 8) {
@@ -391,7 +409,8 @@ struct Queries {
     }
     __device__ __forceinline__ bool any_spoilt(const char *v, int r0, int n) const {
         bool found = false;
-#pragma unroll 4
+        const int lane = lane_again();
+#pragma unroll 1
         for (int u = lane; u < n * (DV / 8); u += 64) {
             const int r = r0 + u / (DV / 8), chunk = u % (DV / 8);
             const u32x4 w = *reinterpret_cast<const u32x4 *>(v + r * PITCH + 16 * (chunk ^ swirl(r)));
@@ -411,8 +430,6 @@ struct Queries {
         bool active;
         // This lane's row; past the last one, that one once more.
         int at;                          // its position
-        uint32_t lo, hi;                 // it sees [lo, hi)
-        uint64_t drafts = 0;             // and these drafts
         float slope = 0.f, cap2 = 0.f, cap_unit = 0.f, unit;
         uint32_t slopes[2] = {0, 0};
         bool linear = false;
@@ -462,6 +479,7 @@ struct Queries {
             }
             const int x = x0 + c, row = x < n_rows ? x : n_rows - 1;
             const int i = fd_div(p.fd_G, row), g = row - i * G;
+            uint64_t drafts = 0;
             at = base + i;
             if (is_tree) {
                 const int mine = (int)depth[i];
@@ -472,9 +490,9 @@ struct Queries {
                         if (mine - (int)depth[j] >= p.window) drafts &= ~(1ull << j);
             }
             const int near = at - p.window + 1;
-            lo = p.window && near > rec.start ? near : rec.start;
             const int seen = is_tree ? base : at + 1 > rec.prefix ? at + 1 : rec.prefix;
-            hi = seen < rec.end ? seen : rec.end;
+            sight[lane] = Sight{drafts, (uint32_t)(p.window && near > rec.start ? near : rec.start),
+                                (uint32_t)(seen < rec.end ? seen : rec.end)};
             if (biased) {
                 slope = p.slopes[h * G + g] * kLog2e;
                 // in three parts of the rows' type, for a product with whole numbers up to 63
@@ -483,12 +501,12 @@ struct Queries {
                 slopes[1] = V::pack(x - a - b, 0.f);
                 linear = cap_unit == 0.f && !__any(!(fabsf(x) < 1024.f));
             }
-            const char *src = p.q.base + (rec.row_off + i) * p.q.s_row + (int64_t)(h * G + g) * p.q.s_head;
+            const int d0 = 16 * (wave % SPLIT * KS) + 8 * (lane_again() >> 5), left = none ? 0 : p.pool.D - d0;
+            const char *src = p.q.base + (rec.row_off + i) * p.q.s_row + (int64_t)(h * G + g) * p.q.s_head + 2 * d0;
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                const int d = 16 * (wave % SPLIT * KS + k) + 8 * e;
                 qv[k] = u32x4{0, 0, 0, 0};
-                if (d < p.pool.D && !none) qv[k] = *reinterpret_cast<const u32x4 *>(src + 2 * d);
+                if (16 * k < left) qv[k] = *reinterpret_cast<const u32x4 *>(src + 32 * k);
 #pragma unroll
                 for (int w = 0; w < 4; ++w) qv[k][w] ^= flip;
             }
@@ -543,6 +561,8 @@ struct Queries {
                 if (more) load(buf ^ 1, rows.off[next_ring][next_slot], scalar((int64_t)rows.there[next_ring][next_slot]));
                 const uint64_t here = scalar((int64_t)rows.there[ring][slot]);
                 const char *kt = lds + buf * tile_bytes, *vt = kt + (two ? TILE * PITCH : 0);
+                uint32_t ka[APART ? TURNS / 2 : 1], va[APART ? TURNS / 4 : 1];
+                at_tile(kt, vt, ka, va);
                 const bool on = active && t0 < some.hi && t0 + TILE > some.lo;
                 const bool edge = here != ALL || t0 < all.lo || t0 + TILE > all.hi;        // some row does not see all
                 const bool team_edge = here != ALL || t0 < block_all.lo || t0 + TILE > block_all.hi;
@@ -559,23 +579,25 @@ struct Queries {
 #pragma unroll
                         for (int j = 0; j < KS; ++j)
 #pragma unroll
-                            for (int pb = 0; pb < PB; ++pb) s[pb] = mfma32<F16>(keys(kt, pb, j), qv[j], s[pb]);
+                            for (int pb = 0; pb < PB; ++pb) s[pb] = mfma32<F16>(keys(ka, pb, j), qv[j], s[pb]);
                     } else {
                         u32x4 a[AHEAD + 1];
 #pragma unroll
-                        for (int u = 0; u < AHEAD; ++u) a[u] = keys(kt, u % PB, u / PB);
+                        for (int u = 0; u < AHEAD; ++u) a[u] = keys(ka, u % PB, u / PB);
                         if (GENERAL && straight && wave % SPLIT == 0) {
                             // slope * (position within the tile) as one more step of the product
 #pragma unroll
                             for (int pb = 0; pb < PB; ++pb) {
-                                const uint32_t off = V::pack((float)(32 * pb + c), (float)(32 * pb + c));
-                                s[pb] = mfma32<F16>(e == 0 ? u32x4{off, off & 0xffff, 0, 0} : u32x4{0, 0, 0, 0}, u32x4{slopes[0], slopes[1], 0, 0}, s[pb]);
+                                const int ln = lane_again();
+                                const float row = 32 * pb + (ln & 31);
+                                const uint32_t off = V::pack(row, row);
+                                s[pb] = mfma32<F16>(ln < 32 ? u32x4{off, off & 0xffff, 0, 0} : u32x4{0, 0, 0, 0}, u32x4{slopes[0], slopes[1], 0, 0}, s[pb]);
                             }
                         }
                         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                         for (int u = 0; u < KS * PB; ++u) {
-                            if (u + AHEAD < KS * PB) a[(u + AHEAD) % (AHEAD + 1)] = keys(kt, (u + AHEAD) % PB, (u + AHEAD) / PB);
+                            if (u + AHEAD < KS * PB) a[(u + AHEAD) % (AHEAD + 1)] = keys(ka, (u + AHEAD) % PB, (u + AHEAD) / PB);
                             s[u % PB] = mfma32<F16>(a[u % (AHEAD + 1)], qv[u / PB], s[u % PB]);
                             __builtin_amdgcn_sched_barrier(0);
                         }
@@ -612,6 +634,7 @@ struct Queries {
                         if (straight) {
                             shift = -slope * (float)(at - (int)t0);      // the rest of the bias is in the product
                         } else if (seldom(biased)) {
+                            const int e = lane_again() >> 5;
                             const float far = (float)(at - (int)(t0 + 4 * e));
                             const bool by_depth = is_tree && t0 + TILE > (uint32_t)base;
 #pragma unroll
@@ -633,11 +656,13 @@ struct Queries {
                         }
                     }
                     if (seldom(edge)) {
-                        uint64_t v = ones((int64_t)hi - t0) & ~ones((int64_t)lo - t0);
+                        const int ln = lane_again();
+                        const Sight mine = sight[ln];
+                        uint64_t v = ones((int64_t)mine.hi - t0) & ~ones((int64_t)mine.lo - t0);
                         const int64_t to = (int64_t)base - t0;
-                        if (is_tree && to < 64 && to > -64) v |= to >= 0 ? drafts << to : drafts >> -to;
+                        if (is_tree && to < 64 && to > -64) v |= to >= 0 ? mine.drafts << to : mine.drafts >> -to;
                         sees = v & here;
-                        const uint64_t shown = sees >> (4 * e);
+                        const uint64_t shown = sees >> (4 * (ln >> 5));
 #pragma unroll
                         for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
@@ -675,6 +700,7 @@ struct Queries {
                     // The tile is the team's: it looks over its values together.
                     constexpr int MINE = TILE / TEAM;
                     char *v = const_cast<char *>(vt);
+                    const int lane = lane_again(), c = lane & 31, e = lane >> 5;
                     bool found = any_spoilt(v, part * MINE, MINE);
                     if (TEAM > 1) found = __syncthreads_or(found);
                     if (seldom(found)) {
@@ -723,19 +749,19 @@ struct Queries {
                         for (int u = 0; u < 2 * PB; ++u)
 #pragma unroll
                             for (int d = 0; d < DB; ++d) {
-                                const u32x4 v = columns(vt, u / 2, u % 2, d);
+                                const u32x4 v = columns(va, u / 2, u % 2, d);
                                 o[d] = mfma32<F16>(v, w[u], o[d]);
                                 if (PARTS) o[d] = mfma32<F16>(v, rest[u], o[d]);
                             }
                     } else {
                         u32x4 v[AHEAD + 1];
 #pragma unroll
-                        for (int x = 0; x < AHEAD; ++x) v[x] = columns(vt, x / DB / 2, x / DB % 2, x % DB);
+                        for (int x = 0; x < AHEAD; ++x) v[x] = columns(va, x / DB / 2, x / DB % 2, x % DB);
                         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                         for (int x = 0; x < 2 * PB * DB; ++x) {
                             const int y = x + AHEAD;
-                            if (y < 2 * PB * DB) v[y % (AHEAD + 1)] = columns(vt, y / DB / 2, y / DB % 2, y % DB);
+                            if (y < 2 * PB * DB) v[y % (AHEAD + 1)] = columns(va, y / DB / 2, y / DB % 2, y % DB);
                             o[x % DB] = mfma32<F16>(v[x % (AHEAD + 1)], w[x / DB], o[x % DB]);
                             if (PARTS) o[x % DB] = mfma32<F16>(v[x % (AHEAD + 1)], rest[x / DB], o[x % DB]);
                             __builtin_amdgcn_sched_barrier(0);
@@ -786,37 +812,34 @@ struct Queries {
             }
             if (stream != streams - 1) return;
         }
-        const int x = x0 + c;
+        const int ln = lane_again(), half = ln >> 5, x = x0 + (ln & 31);
         if (x >= h_rows) return;
         const int i = fd_div(p.fd_G, x), head = h * G + x - i * G;
+        const int mine = 32 * DB * (wave % SPLIT);           // this wavefront's first value; a lane has 4 of every 8
         if (piece.place < 0) {
             const float v_scale = p.scales ? p.scales[(p.pool.C - 1) * p.pool.H + h] : 1.f;
             const float f = l == 0.f ? 0.f : v_scale / l;
-            if (p.lse && e == 0 && wave % SPLIT == 0)
+            if (p.lse && half == 0 && mine == 0)
                 p.lse[(rec.row_off + i) * p.pool.H * G + head] =
                     l > 0.f || l != l ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
-            char *dst = p.out.base + (rec.row_off + i) * p.out.s_row + head * p.out.s_head;
+            char *dst = p.out.base + (rec.row_off + i) * p.out.s_row + head * p.out.s_head + 2 * (mine + 4 * half);
 #pragma unroll
             for (int d = 0; d < DB; ++d)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int to = 32 * (wave % SPLIT * DB + d) + 8 * j + 4 * e;
-                    if (to < p.Dv)
-                        *reinterpret_cast<u32x2 *>(dst + 2 * to) = u32x2{V::pack(o[d][4 * j] * f, o[d][4 * j + 1] * f),
-                                                                        V::pack(o[d][4 * j + 2] * f, o[d][4 * j + 3] * f)};
-                }
+                for (int j = 0; j < 4; ++j)
+                    if (mine + 32 * d + 8 * j < p.Dv)
+                        *reinterpret_cast<u32x2 *>(dst + 64 * d + 16 * j) = u32x2{V::pack(o[d][4 * j] * f, o[d][4 * j + 1] * f),
+                                                                                 V::pack(o[d][4 * j + 2] * f, o[d][4 * j + 3] * f)};
         } else {
             const int64_t row = (piece.place * p.heads + (TEAM > 1 ? 0 : wave / streams)) * p.rows + x - block0;
-            if (e == 0 && wave % SPLIT == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * row) = make_float2(m, l);
-            float *dst = p.part_o + row * p.Dv;
+            if (half == 0 && mine == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * row) = make_float2(m, l);
+            float *dst = p.part_o + row * p.Dv + mine + 4 * half;
 #pragma unroll
             for (int d = 0; d < DB; ++d)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int to = 32 * (wave % SPLIT * DB + d) + 8 * j + 4 * e;
-                    if (to < p.Dv)
-                        *reinterpret_cast<f32x4 *>(dst + to) = f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
-                }
+                for (int j = 0; j < 4; ++j)
+                    if (mine + 32 * d + 8 * j < p.Dv)
+                        *reinterpret_cast<f32x4 *>(dst + 32 * d + 8 * j) = f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
         }
     }
 };
@@ -828,13 +851,14 @@ __global__ void __launch_bounds__(64 * WAVES, DK <= 128 || SPLIT > 1 ? 2 : 1) kv
     __shared__ int64_t before[kQueriesGroup + 1];        // steps of one cache head of the records before
     __shared__ __align__(16) typename Work::Rows rows[WAVES / TEAM];
     __shared__ float depth[WAVES][KVX_MAX_DRAFTS];
+    __shared__ typename Work::Sight sight[WAVES][64];
     __shared__ float ml[TEAM == 1 ? WAVES * 32 * 2 : 1];
     __shared__ __align__(16) f32x4 shared[SPLIT > 1 ? WAVES * 256 : 1];
     __shared__ int64_t sums[WAVES];
     extern __shared__ __align__(256) char lds[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int tile_bytes = TILE * 2 * DK * p.pool.C;
-    Work work{rows[TEAM > 1 ? 0 : wave], depth[wave], lds + (TEAM > 1 ? 0 : wave * 2 * tile_bytes), ml, lds, shared, lane, wave,
+    Work work{rows[TEAM > 1 ? 0 : wave], depth[wave], sight[wave], lds + (TEAM > 1 ? 0 : wave * 2 * tile_bytes), ml, lds, shared, lane, wave,
               TEAM > 1 ? wave : 0, lane & 31, lane >> 5, p.pool.C == 2, one_tile(DK, p.pool.C), tile_bytes};
     work.address();
     // Two wavefronts of a workgroup lie on a SIMD: with one of them preferred, their products and
