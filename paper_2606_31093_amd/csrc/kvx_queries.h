@@ -229,6 +229,7 @@ struct Queries {
     } *sight;                    // [64], the wavefront's
     char *lds;                   // [2][rows of K, rows of V if there are two], the team's
     float *ml;                   // [wavefronts][32][2]
+    int32_t (*flags)[TEAM];      // [2]
     char *all_lds;               // the workgroup's
     f32x4 *shared;               // [wavefront][4][64]: scores that wavefronts of the same rows add up
     int lane, wave, part, c, e;  // part: of the team
@@ -393,6 +394,16 @@ struct Queries {
         return u32x4{x[0], x[1], y[0], y[1]};
     }
 
+    // Whether x holds for one of the team's wavefronts; `turn` differs from call to call.  The
+    // loads that are on their way are not waited for.
+    __device__ __forceinline__ bool any_of_team(bool x, int turn) const {
+        if (lane == 0) flags[turn][part] = x;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        return __any(flags[turn][lane & (TEAM - 1)]);
+    }
+
     // Rows r0 .. r0 + n - 1 of V that hold values which are not finite.
     __device__ __forceinline__ uint64_t spoilt(const char *v, int r0, int n) const {
         uint64_t found_rows = 0;
@@ -434,6 +445,8 @@ struct Queries {
         uint32_t slopes[2] = {0, 0};
         bool linear = false;
         bool is_tree, biased;
+        uint32_t t0, step;               // this wavefront's tile, and from one to the next
+        int32_t page0 = 0, page = 0;     // page ids of the first tiles to resolve, and the next
         uint32_t past;                   // positions below it are at or behind all rows of the wavefront
         u32x4 qv[KS];
         // Positions that all rows of the wavefront see, that some see, and that all of the
@@ -456,6 +469,12 @@ struct Queries {
             fd_T = p.pool.fd_T;
             N = p.pool.N;
             have = (E4M3 ? 1 : 2) * p.pool.D / 16;
+            t0 = begin + stream * TILE;
+            step = TILE * streams;
+            if (t0 < end) {
+                page0 = look(t0 + part * step);
+                page = look(t0 + (TEAM + part) * step);
+            }
             is_tree = p.tree;
             biased = GENERAL && p.slopes;
             // Scores are taken times unit > 0: a sign goes into the queries.
@@ -531,17 +550,14 @@ struct Queries {
             for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
         float m = -INFINITY, l = 0.f;
 
-        uint32_t t0 = begin + stream * TILE;
-        const uint32_t step = TILE * streams;
         if (t0 < end) {
             // Tiles are resolved TEAM at a time, one by each wavefront, while the TEAM before are used;
             // their page ids are asked for as much earlier.
             const uint32_t mine = t0 + part * step;
-            resolve(mine, look(mine), 0, part);
+            resolve(mine, page0, 0, part);
             if (TEAM > 1) __syncthreads();
             load(0, rows.off[0][0], scalar((int64_t)rows.there[0][0]));
             put(0);
-            int32_t page = look(mine + TEAM * step);
             for (int k = 0; t0 < end; t0 += step, ++k) {
                 const int buf = SPLIT > 1 && once ? 0 : k & 1, slot = k & (TEAM - 1), ring = k / TEAM & 1;
                 if (SPLIT > 1 && once && k > 0) {
@@ -702,7 +718,7 @@ struct Queries {
                     char *v = const_cast<char *>(vt);
                     const int lane = lane_again(), c = lane & 31, e = lane >> 5;
                     bool found = any_spoilt(v, part * MINE, MINE);
-                    if (TEAM > 1) found = __syncthreads_or(found);
+                    if (TEAM > 1) found = any_of_team(found, k & 1);
                     if (seldom(found)) {
                         const uint64_t spoilt_rows = spoilt(v, 0, TILE);
                         for (uint64_t left = spoilt_rows; left && on; left &= left - 1) {
@@ -853,12 +869,13 @@ __global__ void __launch_bounds__(64 * WAVES, DK <= 128 || SPLIT > 1 ? 2 : 1) kv
     __shared__ float depth[WAVES][KVX_MAX_DRAFTS];
     __shared__ typename Work::Sight sight[WAVES][64];
     __shared__ float ml[TEAM == 1 ? WAVES * 32 * 2 : 1];
+    __shared__ int32_t flags[2][TEAM];
     __shared__ __align__(16) f32x4 shared[SPLIT > 1 ? WAVES * 256 : 1];
     __shared__ int64_t sums[WAVES];
     extern __shared__ __align__(256) char lds[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int tile_bytes = TILE * 2 * DK * p.pool.C;
-    Work work{rows[TEAM > 1 ? 0 : wave], depth[wave], sight[wave], lds + (TEAM > 1 ? 0 : wave * 2 * tile_bytes), ml, lds, shared, lane, wave,
+    Work work{rows[TEAM > 1 ? 0 : wave], depth[wave], sight[wave], lds + (TEAM > 1 ? 0 : wave * 2 * tile_bytes), ml, flags, lds, shared, lane, wave,
               TEAM > 1 ? wave : 0, lane & 31, lane >> 5, p.pool.C == 2, one_tile(DK, p.pool.C), tile_bytes};
     work.address();
     // Two wavefronts of a workgroup lie on a SIMD: with one of them preferred, their products and

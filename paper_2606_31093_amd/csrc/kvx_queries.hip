@@ -8,90 +8,99 @@ namespace kvx {
 namespace {
 
 constexpr int kThreads = 256;
+#ifndef KVX_JB
+#define KVX_JB 2048
+#endif
+constexpr int kJoinBlocks = KVX_JB;
 
 // A workgroup joins some rows of a unit: out = sum 2^(m_c - M) o_c / sum 2^(m_c - M) l_c.
 // Dv / 4 threads side by side take a row's values; `split` such rows of threads share its
-// parts and add up in LDS.
+// parts and add up in LDS; each takes `turns` rows one after the other.
 template <bool F16>
 __global__ void __launch_bounds__(kThreads) kvx_queries_join_kernel(QueriesParams p, int64_t r0, int64_t first, int32_t runs,
-                                                                    int32_t split) {
+                                                                    int32_t split, int32_t turns) {
     extern __shared__ __align__(16) float sums[];        // [row of threads][Dv], then their m and l
-    const int64_t id = first + blockIdx.x, unit = id / runs;
+    const int64_t id = first + blockIdx.x, unit = quotient(id, runs);
     const int run = (int)(id - unit * runs), H = p.pool.H, G = p.fd_G.d;
-    const int64_t list = unit / p.blocks;
-    const int b = (int)(unit - list * p.blocks), r = (int)(list / p.groups), group = (int)(list - (int64_t)r * p.groups);
+    const int64_t list = quotient(unit, p.blocks);
+    const int b = (int)(unit - list * p.blocks), r = (int)quotient(list, p.groups), group = (int)(list - (int64_t)r * p.groups);
     const kvx_queries_req rec = p.reqs[r0 + r];
-    if (!valid(rec, p) || b >= blocks_of(rec, p)) return;
-    const UnitSteps u = p.units[unit];
+    const UnitSteps u = p.units[unit];                   // of no meaning where there is no such unit
     const int64_t each = share_of(*p.total, p.shares);
+    if (!valid(rec, p) || b >= blocks_of(rec, p)) return;
     const int64_t k0 = quotient(u.first, each), k1 = quotient(u.first + u.steps - 1, each);
     if (k0 == k1) return;                                // written by the first launch
     const int cols = p.Dv / 4, lines = kThreads / cols, col = threadIdx.x % cols, line = threadIdx.x / cols;
     const int per = lines / split, mine = line % split, slots = p.heads * p.rows;
-    const int x = run * per + line / split;              // row of the block, of each head of the group
-    const int h = group * p.heads + x / p.rows;
-    const int64_t row = (int64_t)b * p.rows + x % p.rows;
-    const bool on = line < per * split && x < slots && row < (int64_t)rec.n_queries * G;
-    float m = -INFINITY, l = 0.f;
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    if (on) {
-        for (int64_t k = k0 + mine; k <= k1; k += 8 * split) {
-            f32x4 y[8];
-            float2 ml[8];
-            // all on their way at once; past the end the last one, without weight
+    for (int turn = 0; turn < turns; ++turn) {
+        const int x = (run * turns + turn) * per + line / split;       // row of the block, of each head of the group
+        const int h = group * p.heads + x / p.rows;
+        const int64_t row = (int64_t)b * p.rows + x % p.rows;
+        const bool on = line < per * split && x < slots && row < (int64_t)rec.n_queries * G;
+        float m = -INFINITY, l = 0.f;
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        if (on) {
+            for (int64_t k = k0 + mine; k <= k1; k += 4 * split) {
+                f32x4 y[4];
+                float2 ml[4];
+                // all on their way at once
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int64_t part = k + i * split <= k1 ? k + i * split : k1;
-                const int64_t at = place_of(u.first, part, each, p.shares) * slots + x;
-                ml[i] = *reinterpret_cast<const float2 *>(p.part_ml + 2 * at);
-                y[i] = *reinterpret_cast<const f32x4 *>(p.part_o + at * p.Dv + 4 * col);
+                for (int i = 0; i < 4; ++i) {
+                    ml[i] = make_float2(-INFINITY, 0.f);
+                    y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    if (k + i * split > k1) continue;
+                    const int64_t at = place_of(u.first, k + i * split, each, p.shares) * slots + x;
+                    ml[i] = *reinterpret_cast<const float2 *>(p.part_ml + 2 * at);
+                    y[i] = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p.part_o + at * p.Dv + 4 * col));
+                }
+                float top = m;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, ml[i].x);
+                const float f = weight(m, top);
+                m = top;
+                l *= f;
+                sum *= f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float w = weight(ml[i].x, m);
+                    l += ml[i].y * w;
+                    sum += y[i] * w;
+                }
             }
-            float top = m;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top = fmaxf(top, ml[i].x);
-            const float f = weight(m, top);
+        }
+        if (split > 1) {
+            float *ml = sums + (int64_t)lines * p.Dv;
+            if (turn > 0) __syncthreads();
+            if (line < lines) {
+                *reinterpret_cast<f32x4 *>(sums + line * p.Dv + 4 * col) = sum;
+                if (col == 0) {
+                    ml[2 * line] = m;
+                    ml[2 * line + 1] = l;
+                }
+            }
+            __syncthreads();
+            if (!on || mine != 0) continue;
+            float top = -INFINITY;
+            for (int k = 0; k < split; ++k) top = fmaxf(top, ml[2 * (line + k)]);
             m = top;
-            l *= f;
-            sum *= f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (k + i * split > k1) continue;
-                const float w = weight(ml[i].x, m);
-                l += ml[i].y * w;
-                sum += y[i] * w;
+            l = 0.f;
+            sum = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int k = 0; k < split; ++k) {
+                const float w = weight(ml[2 * (line + k)], m);
+                l += ml[2 * (line + k) + 1] * w;
+                sum += *reinterpret_cast<const f32x4 *>(sums + (line + k) * p.Dv + 4 * col) * w;
             }
         }
+        if (!on) continue;
+        const int i = (int)fd_div(p.fd_G, (uint32_t)row), head = h * G + (int)(row - (int64_t)i * G);
+        if (p.lse && col == 0)
+            p.lse[(rec.row_off + i) * H * G + head] =
+                l > 0.f || l != l ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+        const float v_scale = p.scales ? p.scales[(p.pool.C - 1) * H + h] : 1.f;
+        sum *= l == 0.f ? 0.f : v_scale / l;
+        char *dst = p.out.base + (rec.row_off + i) * p.out.s_row + head * p.out.s_head;
+        *reinterpret_cast<u32x2 *>(dst + 8 * col) = u32x2{Half<F16>::pack(sum[0], sum[1]), Half<F16>::pack(sum[2], sum[3])};
     }
-    if (split > 1) {
-        float *ml = sums + (int64_t)lines * p.Dv;
-        if (line < lines) {
-            *reinterpret_cast<f32x4 *>(sums + line * p.Dv + 4 * col) = sum;
-            if (col == 0) {
-                ml[2 * line] = m;
-                ml[2 * line + 1] = l;
-            }
-        }
-        __syncthreads();
-        if (!on || mine != 0) return;
-        float top = -INFINITY;
-        for (int k = 0; k < split; ++k) top = fmaxf(top, ml[2 * (line + k)]);
-        m = top;
-        l = 0.f;
-        sum = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int k = 0; k < split; ++k) {
-            const float w = weight(ml[2 * (line + k)], m);
-            l += ml[2 * (line + k) + 1] * w;
-            sum += *reinterpret_cast<const f32x4 *>(sums + (line + k) * p.Dv + 4 * col) * w;
-        }
-    }
-    if (!on) return;
-    const int i = (int)(row / G), head = h * G + (int)(row - (int64_t)i * G);
-    if (p.lse && col == 0)
-        p.lse[(rec.row_off + i) * H * G + head] = l > 0.f || l != l ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
-    const float v_scale = p.scales ? p.scales[(p.pool.C - 1) * H + h] : 1.f;
-    sum *= l == 0.f ? 0.f : v_scale / l;
-    char *dst = p.out.base + (rec.row_off + i) * p.out.s_row + head * p.out.s_head;
-    *reinterpret_cast<u32x2 *>(dst + 8 * col) = u32x2{Half<F16>::pack(sum[0], sum[1]), Half<F16>::pack(sum[2], sum[3])};
 }
 
 // Workgroups that the device holds at a time, by their LDS and registers: its 256 compute
@@ -99,7 +108,10 @@ __global__ void __launch_bounds__(kThreads) kvx_queries_join_kernel(QueriesParam
 int resident(const QueriesParams &p) { return (p.team == 4 && p.pool.D <= 128) || (p.team == 1 && p.pool.D <= 64) ? 512 : 256; }
 // Units of up to this many steps, or this many units and more, are not split.
 constexpr int kWholeSteps = 8;
-constexpr int kWholeUnits = 1024;
+#ifndef KVX_WU
+#define KVX_WU 1024
+#endif
+constexpr int kWholeUnits = KVX_WU;
 // Fewer steps than this are not worth a share.
 constexpr int kLeastShare = 4;
 
@@ -109,7 +121,7 @@ int tile_of(const QueriesParams &p) { return p.team == 1 || p.pool.D > 128 ? 32 
 void shape(QueriesParams &p, int64_t most) {
     const int D = p.pool.D;
     // Up to 32 rows: wavefronts take positions of their own; as many as LDS holds tiles for.
-    p.team = D > 256 ? 8 : most <= 32 ? 1 : D > 64 && D <= 128 && most <= 128 ? 4 : 8;
+    p.team = D > 256 ? 8 : most <= 32 ? 1 : D > 64 && D <= 128 && (most <= 128 || p.max_tokens <= 1024) ? 4 : 8;
     p.waves = p.team > 1 ? p.team : D <= 128 ? 4 : 2;
     p.rows = D > 128 && p.team > 1 ? 128 : 32 * p.team;      // two wavefronts for 32 wide rows
     // Rows of the cache that lie side by side, several heads of a position, are read by one workgroup.
@@ -202,12 +214,16 @@ int launch_queries(const QueriesParams &p, hipStream_t stream) {
         while (2 * split <= lines && units * 8 * split < p.shares) split *= 2;
         const int rows = p.heads == 1 && p.blocks == 1 && (int64_t)p.max_queries * p.fd_G.d < p.rows ? p.max_queries * p.fd_G.d
                                                                                                        : p.heads * p.rows;
-        const int32_t runs = (rows + lines / split - 1) / (lines / split);
+        // several rows a thread where there are more than the device holds threads for
+        const int per = lines / split;
+        int turns = 1;
+        while (turns < 8 && units * rows > (int64_t)kJoinBlocks * turns * per) turns *= 2;
+        const int32_t runs = (rows + per * turns - 1) / (per * turns);
         const size_t lds = split > 1 ? sizeof(float) * lines * (p.Dv + 2) : 0;
         for (int64_t at = 0; at < units * runs; at += kMaxBlocks) {
             const int64_t some = units * runs - at < kMaxBlocks ? units * runs - at : kMaxBlocks;
             hipLaunchKernelGGL(p.f16 ? kvx_queries_join_kernel<true> : kvx_queries_join_kernel<false>, dim3((uint32_t)some),
-                               dim3(kThreads), lds, stream, p, r0, at, runs, split);
+                               dim3(kThreads), lds, stream, p, r0, at, runs, split, turns);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
     }
