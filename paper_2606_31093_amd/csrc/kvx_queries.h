@@ -197,14 +197,18 @@ __device__ __forceinline__ QueriesParams again() {
 // that share a tile (all of the workgroup; or 1: each takes tiles of its own for the same
 // 32 rows, and they join at the end); SPLIT: wavefronts that share 32 rows (wide rows: a
 // query and its outputs would not leave registers for a second wavefront on the SIMD;
-// each takes a part of the elements for the scores, which they add up through LDS, and a
-// part of the values); TILE: positions; GENERAL: scores may be capped or biased.
+// each takes a part of the values, and for the scores half of the positions, whose weights
+// they pass each other through LDS, or, where a query takes too many registers, half of
+// the elements, and they add the scores up); TILE: positions; GENERAL: scores may be
+// capped or biased.
 template <bool F16, bool E4M3, int DK, int DV, int TEAM, int SPLIT, int TILE, bool GENERAL>
 struct Queries {
     typedef Half<F16> V;
     // of a wavefront: steps of 16 elements of K, blocks of 32 values
-    static constexpr int KS = DK / 16 / SPLIT, DB = DV / 32 / SPLIT;
-    static constexpr int PB = TILE / 32, PITCH = 2 * DK;
+    static constexpr bool HALVES = SPLIT > 1 && DK <= 256;
+    static constexpr int KS = HALVES ? DK / 16 : DK / 16 / SPLIT, DB = DV / 32 / SPLIT;
+    // blocks of 32 positions, those a wavefront scores and all that it takes values of
+    static constexpr int PB = TILE / 32 / (HALVES ? SPLIT : 1), PV = TILE / 32, PITCH = 2 * DK;
     static constexpr int SRC = DK * (E4M3 ? 1 : 2) / 16;       // 16-byte chunks of a row in memory
     // loads of a wavefront for a tile's K or V, of them all a wavefront's at most
     static constexpr int ALL_LOADS = TILE * SRC / 64, LOADS = (ALL_LOADS + TEAM - 1) / TEAM;
@@ -221,17 +225,19 @@ struct Queries {
         uint64_t there[2][TEAM];
     };
     Rows &rows;                  // the team's
-    float *depth;                // [64], the wavefront's
+    float *depth;                // [64]
     // What a lane's row sees is needed at the edges only, and kept in LDS.
     struct Sight {
         uint64_t drafts;         // of the drafts
         uint32_t lo, hi;         // and of the positions before them [lo, hi)
-    } *sight;                    // [64], the wavefront's
+    } *sight;                    // [32], the wavefront's rows
     char *lds;                   // [2][rows of K, rows of V if there are two], the team's
     float *ml;                   // [wavefronts][32][2]
-    int32_t (*flags)[TEAM];      // [2]
+    int32_t (*flags)[TEAM];      // [4]: of tiles in turns, of two questions
     char *all_lds;               // the workgroup's
-    f32x4 *shared;               // [wavefront][4][64]: scores that wavefronts of the same rows add up
+    f32x4 *shared;               // [wavefront][4][64]: scores that wavefronts of the same rows add up, or
+                                 // [wavefront][2][64]: weights that they pass each other
+    float *tops;                 // [wavefront][32]: what they agree on, of each row
     int lane, wave, part, c, e;  // part: of the team
     bool two, once;              // V apart from K; LDS has room for one tile only
     int tile_bytes;
@@ -356,6 +362,8 @@ struct Queries {
     // - K: the lane's row, chunks 2 k + e from the wavefront's first step on
     // - V, 32 columns from 32 db on: 16 lanes give the addresses of 4 rows x 16 elements,
     //   positions 32 pb + 16 s + 4 e + x, and 8 behind, x < 4
+    // the first position of a tile that the wavefront scores
+    __device__ __forceinline__ int own() const { return HALVES ? 32 * PB * (wave % SPLIT) : 0; }
     // Where a row has 16 places the others follow from one by an exclusive or, tiles lying at
     // multiples of 256 bytes.
     int k_at[APART ? TURNS / 2 : 1], v_at[APART ? TURNS / 4 : 1];
@@ -364,7 +372,8 @@ struct Queries {
         row0 = (part * 64 + lane) / SRC;
         chunk0 = (part * 64 + lane) % SRC ^ (E4M3 ? 0 : swirl(row0));
 #pragma unroll
-        for (int k = 0; k < (APART ? TURNS / 2 : 1); ++k) k_at[k] = c * PITCH + 16 * ((2 * (mine * KS + k) + e) ^ swirl(c));
+        for (int k = 0; k < (APART ? TURNS / 2 : 1); ++k)
+            k_at[k] = (c + own()) * PITCH + 16 * ((2 * ((HALVES ? 0 : mine * KS) + k) + e) ^ swirl(c));
 #pragma unroll
         for (int d = 0; d < (APART ? TURNS / 4 : 1); ++d)
             v_at[d] = row * PITCH + 16 * ((4 * (mine * DB + d) + (lane >> 4 & 1) * 2 + (l >> 1 & 1)) ^ swirl(row)) + (l & 1) * 8;
@@ -428,6 +437,48 @@ struct Queries {
             found |= not_finite<F16>(w[0]) || not_finite<F16>(w[1]) || not_finite<F16>(w[2]) || not_finite<F16>(w[3]);
         }
         return __any(found);
+    }
+
+    // The highest score of this lane's.
+    static __device__ __forceinline__ float top_of(const f32x16 *s, float from, float shift) {
+        float top[4] = {s[0][0], s[0][1], s[0][2], s[0][3]};
+#pragma unroll
+        for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+            for (int i = 0; i < 16; i += 8)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) top[j] = max3(top[j], s[pb][i + 2 * j], s[pb][i + 2 * j + 1]);
+        return __builtin_fmaf(max3(top[0], top[1], fmaxf(top[2], top[3])), from, shift);
+    }
+    static __device__ __forceinline__ void raise(float to, float &m, float &l, f32x16 *o) {
+        const float f = weight(m, to);
+        m = to;
+        l *= f;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[d] *= f;
+    }
+    // Scores to weights against m; their sum.
+    static __device__ __forceinline__ float weigh(f32x16 *s, float from, float shift, float m) {
+        const float ref = shift - (m == -INFINITY ? 0.f : m);      // without any, every score is -inf
+        float sums[2] = {0.f, 0.f};
+#pragma unroll
+        for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[pb][i] = exp2_fast(__builtin_fmaf(s[pb][i], from, ref));
+                sums[i % 2] += s[pb][i];
+            }
+        return sums[0] + sums[1];
+    }
+    static __device__ __forceinline__ void pack_weights(const f32x16 *s, u32x4 *w, u32x4 *rest) {
+#pragma unroll
+        for (int u = 0; u < 2 * PB; ++u) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = s[u / 2][8 * (u % 2) + i];
+            if (PARTS) split<F16>(x, w[u], rest[u]);
+            else w[u] = u32x4{V::pack(x[0], x[1]), V::pack(x[2], x[3]), V::pack(x[4], x[5]), V::pack(x[6], x[7])};
+        }
     }
 
     __device__ __forceinline__ void run(const Piece &piece) {
@@ -510,7 +561,7 @@ struct Queries {
             }
             const int near = at - p.window + 1;
             const int seen = is_tree ? base : at + 1 > rec.prefix ? at + 1 : rec.prefix;
-            sight[lane] = Sight{drafts, (uint32_t)(p.window && near > rec.start ? near : rec.start),
+            sight[c] = Sight{drafts, (uint32_t)(p.window && near > rec.start ? near : rec.start),
                                 (uint32_t)(seen < rec.end ? seen : rec.end)};
             if (biased) {
                 slope = p.slopes[h * G + g] * kLog2e;
@@ -520,7 +571,7 @@ struct Queries {
                 slopes[1] = V::pack(x - a - b, 0.f);
                 linear = cap_unit == 0.f && !__any(!(fabsf(x) < 1024.f));
             }
-            const int d0 = 16 * (wave % SPLIT * KS) + 8 * (lane_again() >> 5), left = none ? 0 : p.pool.D - d0;
+            const int d0 = 16 * (HALVES ? 0 : wave % SPLIT * KS) + 8 * (lane_again() >> 5), left = none ? 0 : p.pool.D - d0;
             const char *src = p.q.base + (rec.row_off + i) * p.q.s_row + (int64_t)(h * G + g) * p.q.s_head + 2 * d0;
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
@@ -600,12 +651,12 @@ struct Queries {
                         u32x4 a[AHEAD + 1];
 #pragma unroll
                         for (int u = 0; u < AHEAD; ++u) a[u] = keys(ka, u % PB, u / PB);
-                        if (GENERAL && straight && wave % SPLIT == 0) {
+                        if (GENERAL && straight && (HALVES || wave % SPLIT == 0)) {
                             // slope * (position within the tile) as one more step of the product
 #pragma unroll
                             for (int pb = 0; pb < PB; ++pb) {
                                 const int ln = lane_again();
-                                const float row = 32 * pb + (ln & 31);
+                                const float row = own() + 32 * pb + (ln & 31);
                                 const uint32_t off = V::pack(row, row);
                                 s[pb] = mfma32<F16>(ln < 32 ? u32x4{off, off & 0xffff, 0, 0} : u32x4{0, 0, 0, 0}, u32x4{slopes[0], slopes[1], 0, 0}, s[pb]);
                             }
@@ -619,7 +670,7 @@ struct Queries {
                         }
                     }
                 }
-                if constexpr (SPLIT > 1) {
+                if constexpr (SPLIT > 1 && !HALVES) {
                     static_assert(PB == 1 && SPLIT == 2, "pairs");
                     f32x4 *mine = shared + wave * 256 + lane;
 #pragma unroll
@@ -651,7 +702,8 @@ struct Queries {
                             shift = -slope * (float)(at - (int)t0);      // the rest of the bias is in the product
                         } else if (seldom(biased)) {
                             const int e = lane_again() >> 5;
-                            const float far = (float)(at - (int)(t0 + 4 * e));
+                            const int t = t0 + own() + 4 * e;
+                            const float far = (float)(at - t);
                             const bool by_depth = is_tree && t0 + TILE > (uint32_t)base;
 #pragma unroll
                             for (int pb = 0; pb < PB; ++pb)
@@ -661,7 +713,7 @@ struct Queries {
                                     float d = far - (float)off;
                                     if (by_depth) {
                                         if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
-                                        const int j = (int)(t0 + 4 * e + off) - base;
+                                        const int j = t + off - base;
                                         const bool draft = j >= 0 && j < rec.n_queries;
                                         if (draft) d = (float)(at - base) - depth[j];
                                     }
@@ -673,44 +725,72 @@ struct Queries {
                     }
                     if (seldom(edge)) {
                         const int ln = lane_again();
-                        const Sight mine = sight[ln];
+                        const Sight mine = sight[ln & 31];
                         uint64_t v = ones((int64_t)mine.hi - t0) & ~ones((int64_t)mine.lo - t0);
                         const int64_t to = (int64_t)base - t0;
                         if (is_tree && to < 64 && to > -64) v |= to >= 0 ? mine.drafts << to : mine.drafts >> -to;
                         sees = v & here;
-                        const uint64_t shown = sees >> (4 * (ln >> 5));
+                        const uint64_t shown = sees >> (own() + 4 * (ln >> 5));
 #pragma unroll
                         for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
                             for (int i = 0; i < 16; ++i)
                                 if (!((uint32_t)(shown >> (32 * pb)) >> (8 * (i / 4) + i % 4) & 1)) s[pb][i] = -INFINITY;
                     }
-                    float tops[4] = {s[0][0], s[0][1], s[0][2], s[0][3]};
-#pragma unroll
-                    for (int pb = 0; pb < PB; ++pb)
-#pragma unroll
-                        for (int i = 0; i < 16; i += 8)
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) tops[j] = max3(tops[j], s[pb][i + 2 * j], s[pb][i + 2 * j + 1]);
-                    float top = __builtin_fmaf(max3(tops[0], tops[1], fmaxf(tops[2], tops[3])), from, shift);
-                    if (seldom(__any(top - kLift<F16> > m + kSlack))) {
-                        top = max_of_halves(top);
-                        const float raised = fmaxf(m, top - kLift<F16>), f = weight(m, raised);
-                        m = raised;
-                        l *= f;
-#pragma unroll
-                        for (int d = 0; d < DB; ++d) o[d] *= f;
-                    }
-                    const float ref = shift - (m == -INFINITY ? 0.f : m);      // without any, every score is -inf
-                    float sums[2] = {0.f, 0.f};
-#pragma unroll
-                    for (int pb = 0; pb < PB; ++pb)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            s[pb][i] = exp2_fast(__builtin_fmaf(s[pb][i], from, ref));
-                            sums[i % 2] += s[pb][i];
+                    if constexpr (!HALVES) {
+                        float top = top_of(s, from, shift);
+                        if (seldom(__any(top - kLift<F16> > m + kSlack))) {
+                            top = max_of_halves(top);
+                            raise(fmaxf(m, top - kLift<F16>), m, l, o);
                         }
-                    l += sums[0] + sums[1];
+                        l += weigh(s, from, shift, m);
+                    }
+                }
+                u32x4 w[2 * PV], rest[2 * PV];   // weights of 8 positions, in one part or two
+                if constexpr (HALVES) {
+                    // Weights against the reference that both wavefronts of the rows have; where one of the
+                    // team's finds scores too far above, both raise theirs, and weigh once more.
+                    static_assert(PB == 1 && SPLIT == 2, "pairs");
+                    u32x4 *mine = reinterpret_cast<u32x4 *>(shared) + wave * 128 + lane;
+                    const u32x4 *others = reinterpret_cast<const u32x4 *>(shared) + (wave ^ 1) * 128 + lane;
+                    const f32x16 raw = s[0];
+                    float sum = 0.f;
+                    const auto pass = [&]() __attribute__((always_inline)) {
+                        s[0] = raw;
+                        sum = weigh(s, from, shift, m);
+                        pack_weights(s, w, rest);
+                        mine[0] = w[0];
+                        mine[64] = w[1];
+                    };
+                    bool far_above = false;
+                    if (on) {
+                        const float top = max_of_halves(top_of(s, from, shift));
+                        far_above = __any(top - kLift<F16> > m + kSlack);
+                        if (lane < 32) tops[wave * 32 + lane] = top;
+                        pass();
+                    }
+                    if (seldom(any_of_team(far_above, k & 1))) {
+                        if (on) {
+                            const float top = fmaxf(tops[wave * 32 + c], tops[(wave ^ 1) * 32 + c]);
+                            raise(fmaxf(m, top - kLift<F16> > m + kSlack ? top - kLift<F16> : m), m, l, o);
+                            pass();
+                        }
+                        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                        __builtin_amdgcn_s_barrier();
+                        asm volatile("" ::: "memory");
+                    }
+                    l += sum;
+                    if (on) {
+                        const bool second = wave & 1;
+                        const u32x4 a = others[0], b = others[64], x = w[0], y = w[1];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            w[0][i] = second ? a[i] : x[i];
+                            w[1][i] = second ? b[i] : y[i];
+                            w[2][i] = second ? x[i] : a[i];
+                            w[3][i] = second ? y[i] : b[i];
+                        }
+                    }
                 }
                 if (seldom(team_edge)) {
                     // The tile is the team's: it looks over its values together.
@@ -718,16 +798,25 @@ struct Queries {
                     char *v = const_cast<char *>(vt);
                     const int lane = lane_again(), c = lane & 31, e = lane >> 5;
                     bool found = any_spoilt(v, part * MINE, MINE);
-                    if (TEAM > 1) found = any_of_team(found, k & 1);
+                    if (TEAM > 1) found = any_of_team(found, 2 + (k & 1));
                     if (seldom(found)) {
                         const uint64_t spoilt_rows = spoilt(v, 0, TILE);
                         for (uint64_t left = spoilt_rows; left && on; left &= left - 1) {
                             const int r = __ffsll((unsigned long long)left) - 1;
-                            const int held = r / 32 * 16 + r % 32 / 8 * 4 + r % 4, owner = c + 32 * (r / 4 % 2);
+                            const int owner = c + 32 * (r / 4 % 2);
                             float x = 0.f;
+                            if constexpr (HALVES) {
+                                uint32_t two = 0;            // as they are held for the product
 #pragma unroll
-                            for (int i = 0; i < 16 * PB; ++i) x = i == held ? s[i / 16][i % 16] : x;
-                            x = __shfl(x, owner);
+                                for (int i = 0; i < 8 * PV; ++i) two = i == r / 16 * 4 + r / 8 % 2 * 2 + r / 2 % 2 ? w[i / 4][i % 4] : two;
+                                two = __shfl(two, owner);
+                                x = r % 2 ? V::hi(two) : V::lo(two);
+                            } else {
+                                const int held = r / 32 * 16 + r % 32 / 8 * 4 + r % 4;
+#pragma unroll
+                                for (int i = 0; i < 16 * PB; ++i) x = i == held ? s[i / 16][i % 16] : x;
+                                x = __shfl(x, owner);
+                            }
                             if (!(sees >> r & 1)) continue;
 #pragma unroll
                             for (int d = 0; d < DB; ++d) {
@@ -751,18 +840,10 @@ struct Queries {
                     }
                 }
                 if (on) {
-                    u32x4 w[2 * PB], rest[2 * PB];
-#pragma unroll
-                    for (int u = 0; u < 2 * PB; ++u) {
-                        float x[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) x[i] = s[u / 2][8 * (u % 2) + i];
-                        if (PARTS) split<F16>(x, w[u], rest[u]);
-                        else w[u] = u32x4{V::pack(x[0], x[1]), V::pack(x[2], x[3]), V::pack(x[4], x[5]), V::pack(x[6], x[7])};
-                    }
+                    if constexpr (!HALVES) pack_weights(s, w, rest);
                     if constexpr (AHEAD == 0) {
 #pragma unroll
-                        for (int u = 0; u < 2 * PB; ++u)
+                        for (int u = 0; u < 2 * PV; ++u)
 #pragma unroll
                             for (int d = 0; d < DB; ++d) {
                                 const u32x4 v = columns(va, u / 2, u % 2, d);
@@ -775,9 +856,9 @@ struct Queries {
                         for (int x = 0; x < AHEAD; ++x) v[x] = columns(va, x / DB / 2, x / DB % 2, x % DB);
                         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                        for (int x = 0; x < 2 * PB * DB; ++x) {
+                        for (int x = 0; x < 2 * PV * DB; ++x) {
                             const int y = x + AHEAD;
-                            if (y < 2 * PB * DB) v[y % (AHEAD + 1)] = columns(va, y / DB / 2, y / DB % 2, y % DB);
+                            if (y < 2 * PV * DB) v[y % (AHEAD + 1)] = columns(va, y / DB / 2, y / DB % 2, y % DB);
                             o[x % DB] = mfma32<F16>(v[x % (AHEAD + 1)], w[x / DB], o[x % DB]);
                             if (PARTS) o[x % DB] = mfma32<F16>(v[x % (AHEAD + 1)], rest[x / DB], o[x % DB]);
                             __builtin_amdgcn_sched_barrier(0);
@@ -791,6 +872,13 @@ struct Queries {
         const int G = p.fd_G.d, block0 = piece.b * p.rows;
         if (bad && p.err) atomicOr(p.err, bad);
         l += __shfl_xor(l, 32);
+        if constexpr (HALVES) {
+            // each has the sum of its half of the positions
+            __syncthreads();
+            if (lane < 32) tops[wave * 32 + lane] = l;
+            __syncthreads();
+            l += tops[(wave ^ 1) * 32 + c];
+        }
 
         // Join the wavefronts of the same rows: each scales to the common maximum, then they
         // add up in LDS, one after the other.
@@ -866,16 +954,17 @@ __global__ void __launch_bounds__(64 * WAVES, DK <= 128 || SPLIT > 1 ? 2 : 1) kv
     typedef Queries<F16, E4M3, DK, DV, TEAM, SPLIT, TILE, GENERAL> Work;
     __shared__ int64_t before[kQueriesGroup + 1];        // steps of one cache head of the records before
     __shared__ __align__(16) typename Work::Rows rows[WAVES / TEAM];
-    __shared__ float depth[WAVES][KVX_MAX_DRAFTS];
-    __shared__ typename Work::Sight sight[WAVES][64];
+    __shared__ float depth[KVX_MAX_DRAFTS];              // every wavefront writes the same
+    __shared__ typename Work::Sight sight[WAVES / SPLIT][32];
+    __shared__ float tops[SPLIT > 1 ? WAVES * 32 : 1];
     __shared__ float ml[TEAM == 1 ? WAVES * 32 * 2 : 1];
-    __shared__ int32_t flags[2][TEAM];
-    __shared__ __align__(16) f32x4 shared[SPLIT > 1 ? WAVES * 256 : 1];
+    __shared__ int32_t flags[4][TEAM];
+    __shared__ __align__(16) f32x4 shared[SPLIT == 1 ? 1 : DK <= 256 ? WAVES * 128 : WAVES * 256];
     __shared__ int64_t sums[WAVES];
     extern __shared__ __align__(256) char lds[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int tile_bytes = TILE * 2 * DK * p.pool.C;
-    Work work{rows[TEAM > 1 ? 0 : wave], depth[wave], sight[wave], lds + (TEAM > 1 ? 0 : wave * 2 * tile_bytes), ml, flags, lds, shared, lane, wave,
+    Work work{rows[TEAM > 1 ? 0 : wave], depth, sight[wave / SPLIT], lds + (TEAM > 1 ? 0 : wave * 2 * tile_bytes), ml, flags, lds, shared, tops, lane, wave,
               TEAM > 1 ? wave : 0, lane & 31, lane >> 5, p.pool.C == 2, one_tile(DK, p.pool.C), tile_bytes};
     work.address();
     // Two wavefronts of a workgroup lie on a SIMD: with one of them preferred, their products and
@@ -1003,7 +1092,7 @@ int launch_type(const QueriesParams &p, int64_t first, int64_t n, hipStream_t st
     if (D <= 128)
         return p.team == 4 ? launch_form<F16, E4M3, 128, 128, 4, 4, 1, 64>(p, first, n, stream)
                            : launch_form<F16, E4M3, 128, 128, 8, 8, 1, 64>(p, first, n, stream);
-    return launch_form<F16, E4M3, 256, 256, 8, 8, 2, 32>(p, first, n, stream);
+    return launch_form<F16, E4M3, 256, 256, 8, 8, 2, 64>(p, first, n, stream);
 }
 
 }  // namespace

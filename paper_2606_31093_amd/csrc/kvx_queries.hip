@@ -115,7 +115,7 @@ constexpr int kWholeUnits = KVX_WU;
 // Fewer steps than this are not worth a share.
 constexpr int kLeastShare = 4;
 
-int tile_of(const QueriesParams &p) { return p.team == 1 || p.pool.D > 128 ? 32 : 64; }
+int tile_of(const QueriesParams &p) { return p.team == 1 || p.pool.D > 256 ? 32 : 64; }
 
 // The kernel for records of up to `most` rows a cache head, and its shape.
 void shape(QueriesParams &p, int64_t most) {

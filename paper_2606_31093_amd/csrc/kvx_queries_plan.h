@@ -8,7 +8,7 @@ namespace kvx {
 
 // Records of one launch with shares.
 #ifndef KVX_QUERIES_GROUP
-#define KVX_QUERIES_GROUP 512
+#define KVX_QUERIES_GROUP 256
 #endif
 constexpr int kQueriesGroup = KVX_QUERIES_GROUP;
 
