@@ -90,12 +90,28 @@ __device__ __forceinline__ Span span_of_block(const kvx_queries_req &q, const Qu
     return span_of_rows(q, p, (uint32_t)b * p.rows, (uint32_t)b * p.rows + p.rows - 1);
 }
 
-// Steps of one cache head of a record.
-__device__ __forceinline__ int64_t steps_of_head(const kvx_queries_req &q, const QueriesParams &p) {
+// What a unit costs beside its tiles (the way from its record to the first tile, and the
+// outputs), in steps that come before its first: shares of equal steps are then done in
+// about equal time.
+#ifndef KVX_UNIT_STEPS
+#define KVX_UNIT_STEPS 4
+#endif
+constexpr int kUnitSteps = KVX_UNIT_STEPS;
+
+// Steps of the blocks of 64 from b0 on of a record and group, a block a lane.
+__device__ __forceinline__ int steps_of_lane(const kvx_queries_req &q, const QueriesParams &p, int b0, int lane, int blocks) {
+    const int b = b0 + lane;
+    return b < blocks ? kUnitSteps + steps_of(span_of_block(q, p, b), p) : 0;
+}
+
+// Steps of one group of cache heads of a record, by a wavefront.
+__device__ __forceinline__ int64_t steps_of_group(const kvx_queries_req &q, const QueriesParams &p, int lane) {
     if (!valid(q, p)) return 0;
     int64_t sum = 0;
-    const int n = blocks_of(q, p);
-    for (int b = 0; b < n; ++b) sum += steps_of(span_of_block(q, p, b), p);
+    const int blocks = blocks_of(q, p);
+    for (int b = 0; b < blocks; b += 64) sum += steps_of_lane(q, p, b, lane, blocks);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
     return sum;
 }
 
@@ -960,7 +976,6 @@ __global__ void __launch_bounds__(64 * WAVES, DK <= 128 || SPLIT > 1 ? 2 : 1) kv
     __shared__ float ml[TEAM == 1 ? WAVES * 32 * 2 : 1];
     __shared__ int32_t flags[4][TEAM];
     __shared__ __align__(16) f32x4 shared[SPLIT == 1 ? 1 : DK <= 256 ? WAVES * 128 : WAVES * 256];
-    __shared__ int64_t sums[WAVES];
     extern __shared__ __align__(256) char lds[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int tile_bytes = TILE * 2 * DK * p.pool.C;
@@ -974,61 +989,75 @@ __global__ void __launch_bounds__(64 * WAVES, DK <= 128 || SPLIT > 1 ? 2 : 1) kv
     int64_t at = 0, stop = 1, each = 0;
     int share = 0;
     if (!p.whole) {
-        // steps of the records before each
-        const int threads = blockDim.x, some = (n + threads - 1) / threads;
-        int64_t sum = 0;
-        for (int r = threadIdx.x * some; r < (int)(threadIdx.x + 1) * some && r < n; ++r) {
-            before[r] = steps_of_head(reqs[r], p);
-            sum += before[r];
+        // steps of a group of cache heads of the records before each
+        if (p.blocks <= 8) {
+            // few blocks a record: a thread each, whose reads are on their way together
+            for (int r = threadIdx.x; r < n; r += 64 * WAVES) {
+                const kvx_queries_req q = reqs[r];
+                int64_t sum = 0;
+                const int count = valid(q, p) ? blocks_of(q, p) : 0;
+                for (int b = 0; b < count; ++b) sum += kUnitSteps + steps_of(span_of_block(q, p, b), p);
+                before[r] = sum;
+            }
+        } else {
+            for (int r = wave; r < n; r += WAVES) {
+                const int64_t x = steps_of_group(scalar(reqs[r]), p, lane);
+                if (lane == 0) before[r] = x;
+            }
         }
-        int64_t upto = sum;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int64_t x = __shfl_up(upto, d);
-            if (lane >= d) upto += x;
-        }
-        if (lane == 63) sums[wave] = upto;
         __syncthreads();
-        for (int k = 0; k < wave; ++k) upto += sums[k];
-        upto -= sum;
-        for (int r = threadIdx.x * some; r < (int)(threadIdx.x + 1) * some && r < n; ++r) {
-            const int64_t x = before[r];
-            before[r] = upto;
-            upto += x;
+        if (wave == 0) {
+            int64_t upto = 0;
+            for (int r0 = 0; r0 < n; r0 += 64) {
+                const int64_t x = r0 + lane < n ? before[r0 + lane] : 0;
+                int64_t sum = x;
+#pragma unroll
+                for (int d = 1; d < 64; d <<= 1) {
+                    const int64_t y = __shfl_up(sum, d);
+                    if (lane >= d) sum += y;
+                }
+                if (r0 + lane < n) before[r0 + lane] = upto + sum - x;
+                upto += __shfl(sum, 63);
+            }
+            if (lane == 0) before[n] = upto;
         }
-        if ((int)threadIdx.x == threads - 1) before[n] = upto;
         __syncthreads();
         // successive shares on one die
         share = p.shares % 8 == 0 ? blockIdx.x % 8 * (p.shares / 8) + blockIdx.x / 8 : blockIdx.x;
         const int64_t total = scalar(before[n]) * p.groups;
         each = share_of(total, p.shares);
         if (share == 0) {
-            if (threadIdx.x == 0) *p.total = total;
+            if (threadIdx.x == 0) *p.each = each;
             for (int r = threadIdx.x; r < n; r += blockDim.x)
                 if (p.err && !valid(reqs[r], p)) atomicOr(p.err, KVX_DERR_BAD_REQ);
         }
         at = share * each;
         stop = at + each < total ? at + each : total;
+        if (p.by_share && threadIdx.x == 0) p.cuts[share] = Cut{0, 0, -1, 0, 0, 0};
     }
+    // the unit that was taken last, of a record that is kept
+    Piece piece;
+    int r = -1, blocks = 0;
     while (at < stop) {
         const QueriesParams p = again();
         const kvx_queries_req *reqs = p.whole ? p.reqs : p.reqs + first;
-        Piece piece;
         Span s;
         int64_t here = 1;
+        bool some = true;
         if (p.whole) {
             // Longest first: a record's last blocks see most.  Blocks of a record and group are n_reqs x groups
             // workgroups apart: with a multiple of 8 of them on one die, whose cache holds their keys.
             const int64_t id = first + blockIdx.x, lists = (int64_t)p.n_reqs * p.groups, rank = quotient(id, lists);
             // Of several records each die takes every eighth block, so that long ones are no die's alone.
-            const int list = (int)((id - rank * lists + (p.n_reqs > 1 ? rank : 0)) % lists), r = list / p.groups;
+            const int list = (int)((id - rank * lists + (p.n_reqs > 1 ? rank : 0)) % lists);
+            r = list / p.groups;
             piece.group = list - r * p.groups;
             piece.rec = scalar(reqs[r]);
             if (!valid(piece.rec, p)) {
                 if (rank == 0 && piece.group == 0 && threadIdx.x == 0 && p.err) atomicOr(p.err, KVX_DERR_BAD_REQ);
                 return;
             }
-            const int blocks = blocks_of(piece.rec, p);
+            blocks = blocks_of(piece.rec, p);
             if (rank >= blocks) return;
             piece.b = blocks - 1 - (int)rank;
             s = span_of_block(piece.rec, p, piece.b);
@@ -1036,33 +1065,56 @@ __global__ void __launch_bounds__(64 * WAVES, DK <= 128 || SPLIT > 1 ? 2 : 1) kv
             piece.begin = s.lo & -kTile;
             piece.end = s.hi;
         } else {
-            int lo = 0, hi = n;          // the record: the last one whose steps begin at or before `at`
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) / 2;
-                if (before[mid] * p.groups <= at) lo = mid;
-                else hi = mid;
+            int64_t in = 0;              // steps of the unit before `at`
+            if (r >= 0 && piece.b + 1 < blocks) {
+                ++piece.b;
+            } else {
+                int lo = 0, hi = n;      // the record: the last one whose steps begin at or before `at`
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) / 2;
+                    if (before[mid] * p.groups <= at) lo = mid;
+                    else hi = mid;
+                }
+                r = __builtin_amdgcn_readfirstlane(lo);
+                const int64_t base = scalar(before[r]) * p.groups, per = scalar(before[r + 1]) - scalar(before[r]);
+                piece.rec = scalar(reqs[r]);
+                piece.group = (int)quotient(at - base, per);
+                in = at - base - piece.group * per;
+                blocks = blocks_of(piece.rec, p);
+                for (int b0 = 0;; b0 += 64) {        // the block, of 64 at a time
+                    const int mine = steps_of_lane(piece.rec, p, b0, lane, blocks);
+                    int64_t upto = mine;
+#pragma unroll
+                    for (int d = 1; d < 64; d <<= 1) {
+                        const int64_t y = __shfl_up(upto, d);
+                        if (lane >= d) upto += y;
+                    }
+                    const uint64_t past = __ballot(upto > in);
+                    if (past) {
+                        const int lane_of = __ffsll((unsigned long long)past) - 1;
+                        piece.b = b0 + lane_of;
+                        in -= scalar(__shfl(upto - mine, lane_of));
+                        break;
+                    }
+                    in -= scalar(__shfl(upto, 63));
+                }
             }
-            const int r = __builtin_amdgcn_readfirstlane(lo);
-            const int64_t base = scalar(before[r]) * p.groups, per = scalar(before[r + 1]) - scalar(before[r]);
-            piece.rec = scalar(reqs[r]);
-            piece.group = (int)quotient(at - base, per);
-            int64_t in = at - base - piece.group * per;
-            int steps;
-            for (piece.b = 0;; ++piece.b) {
-                s = span_of_block(piece.rec, p, piece.b);
-                steps = steps_of(s, p);
-                if (in < steps) break;
-                in -= steps;
-            }
+            s = span_of_block(piece.rec, p, piece.b);
+            const int steps = kUnitSteps + steps_of(s, p);
             here = stop - at < steps - in ? stop - at : steps - in;
-            piece.place = here < steps ? place_of(at - in, share, each, p.shares) : -1;
-            piece.begin = (s.lo & -kTile) + (uint32_t)in * p.step;
-            const uint32_t to = piece.begin + (uint32_t)here * p.step;
-            piece.end = to < s.hi ? to : s.hi;
-            if (in == 0 && threadIdx.x == 0) p.units[((int64_t)r * p.groups + piece.group) * p.blocks + piece.b] = UnitSteps{at, steps};
+            const int64_t first_tile = at - in + kUnitSteps;
+            const int64_t from = in > kUnitSteps ? in - kUnitSteps : 0, to = in + here - kUnitSteps;     // tiles
+            some = to > from;
+            piece.place = from > 0 || to < steps - kUnitSteps ? place_of(first_tile, share, each, p.shares) : -1;
+            piece.begin = (s.lo & -kTile) + (uint32_t)from * p.step;
+            const uint32_t end = (s.lo & -kTile) + (uint32_t)to * p.step;
+            piece.end = end < s.hi ? end : s.hi;
+            if (threadIdx.x == 0 && (p.by_share ? in > kUnitSteps : some && from == 0))
+                p.cuts[p.by_share ? share : (r * p.groups + piece.group) * p.blocks + piece.b] =
+                    Cut{first_tile, at - in + steps - 1, r, piece.group, piece.b, 0};
         }
         if (s.hi <= s.lo) piece.end = piece.begin;
-        work.run(piece);
+        if (some) work.run(piece);
         at += here;
         __syncthreads();                 // the next piece uses the same LDS
     }

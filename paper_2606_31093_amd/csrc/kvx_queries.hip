@@ -17,19 +17,20 @@ constexpr int kJoinBlocks = KVX_JB;
 // Dv / 4 threads side by side take a row's values; `split` such rows of threads share its
 // parts and add up in LDS; each takes `turns` rows one after the other.
 template <bool F16>
-__global__ void __launch_bounds__(kThreads) kvx_queries_join_kernel(QueriesParams p, int64_t r0, int64_t first, int32_t runs,
-                                                                    int32_t split, int32_t turns) {
+__global__ void __launch_bounds__(kThreads) kvx_queries_join_kernel(QueriesParams p, int64_t r0, int32_t runs, int32_t split,
+                                                                    int32_t turns) {
     extern __shared__ __align__(16) float sums[];        // [row of threads][Dv], then their m and l
-    const int64_t id = first + blockIdx.x, unit = quotient(id, runs);
-    const int run = (int)(id - unit * runs), H = p.pool.H, G = p.fd_G.d;
-    const int64_t list = quotient(unit, p.blocks);
-    const int b = (int)(unit - list * p.blocks), r = (int)quotient(list, p.groups), group = (int)(list - (int64_t)r * p.groups);
-    const kvx_queries_req rec = p.reqs[r0 + r];
-    const UnitSteps u = p.units[unit];                   // of no meaning where there is no such unit
-    const int64_t each = share_of(*p.total, p.shares);
+    const int64_t each = *p.each;
+    const int id = blockIdx.x / (uint32_t)runs, run = blockIdx.x - id * runs, H = p.pool.H, G = p.fd_G.d;
+    const Cut u = p.cuts[id];                            // by units, of no meaning where there is no such unit
+    const int list = id / p.blocks, of = p.by_share ? u.record : list / p.groups;
+    if (of < 0) return;
+    const kvx_queries_req rec = p.reqs[r0 + of];
+    const int b = p.by_share ? u.block : id - list * p.blocks, group = p.by_share ? u.group : list - of * p.groups;
     if (!valid(rec, p) || b >= blocks_of(rec, p)) return;
-    const int64_t k0 = quotient(u.first, each), k1 = quotient(u.first + u.steps - 1, each);
-    if (k0 == k1) return;                                // written by the first launch
+    // Parts in shares k0 .. k1; of those that begin inside the unit the first is its own.
+    const int64_t k0 = quotient(u.first, each), k1 = quotient(u.last, each);
+    if (k0 == k1 || (p.by_share && id != k0 + 1)) return;        // one part: written by the first launch
     const int cols = p.Dv / 4, lines = kThreads / cols, col = threadIdx.x % cols, line = threadIdx.x / cols;
     const int per = lines / split, mine = line % split, slots = p.heads * p.rows;
     for (int turn = 0; turn < turns; ++turn) {
@@ -106,12 +107,14 @@ __global__ void __launch_bounds__(kThreads) kvx_queries_join_kernel(QueriesParam
 // Workgroups that the device holds at a time, by their LDS and registers: its 256 compute
 // units have room for one, or for two of four wavefronts.
 int resident(const QueriesParams &p) { return (p.team == 4 && p.pool.D <= 128) || (p.team == 1 && p.pool.D <= 64) ? 512 : 256; }
-// Units of up to this many steps, or this many units and more, are not split.
+// Units of up to this many steps are not split.
 constexpr int kWholeSteps = 8;
-#ifndef KVX_WU
-#define KVX_WU 1024
-#endif
-constexpr int kWholeUnits = KVX_WU;
+// Nor are units so many and more of one record, or of short ones: the device deals them out
+// as it gets free.
+constexpr int kWholeUnits = 1024;
+// Records of up to this many positions: four wavefronts a workgroup, two of which begin and
+// end at different times.
+constexpr int kShort = 1024;
 // Fewer steps than this are not worth a share.
 constexpr int kLeastShare = 4;
 
@@ -121,7 +124,7 @@ int tile_of(const QueriesParams &p) { return p.team == 1 || p.pool.D > 256 ? 32 
 void shape(QueriesParams &p, int64_t most) {
     const int D = p.pool.D;
     // Up to 32 rows: wavefronts take positions of their own; as many as LDS holds tiles for.
-    p.team = D > 256 ? 8 : most <= 32 ? 1 : D > 64 && D <= 128 && (most <= 128 || p.max_tokens <= 1024) ? 4 : 8;
+    p.team = D > 256 ? 8 : most <= 32 ? 1 : D > 64 && D <= 128 && (most <= 128 || p.max_tokens <= kShort) ? 4 : 8;
     p.waves = p.team > 1 ? p.team : D <= 128 ? 4 : 2;
     p.rows = D > 128 && p.team > 1 ? 128 : 32 * p.team;      // two wavefronts for 32 wide rows
     // Rows of the cache that lie side by side, several heads of a position, are read by one workgroup.
@@ -141,11 +144,11 @@ int32_t shares_for(const QueriesParams &p, int64_t units) {
     return (int32_t)(n < resident(p) ? (n > 0 ? n : 1) : resident(p));
 }
 
-// Workspace of `units` units.
-int64_t split_bytes(const QueriesParams &p, int64_t units) {
+// Workspace of the shares.
+int64_t split_bytes(const QueriesParams &p) {
     // two parts a share, its first and its last
     const int64_t rows = 2 * (int64_t)p.shares * p.heads * p.rows;
-    return 16 + units * (int64_t)sizeof(UnitSteps) + rows * 8 + rows * p.Dv * 4 + 64;
+    return 64 + (int64_t)p.shares * (int64_t)sizeof(Cut) + rows * 8 + rows * p.Dv * 4;
 }
 
 int64_t units_of(const QueriesParams &p) {
@@ -156,23 +159,25 @@ int64_t units_of(const QueriesParams &p) {
 
 void plan_queries(QueriesParams &p) {
     shape(p, (int64_t)p.max_queries * p.fd_G.d);
-    p.whole = most_steps(p) <= kWholeSteps || (int64_t)p.n_reqs * p.groups * p.blocks >= kWholeUnits;
+    const int64_t units = (int64_t)p.n_reqs * p.groups * p.blocks;
+    p.whole = most_steps(p) <= kWholeSteps || (units >= kWholeUnits && (p.n_reqs == 1 || p.max_tokens <= kShort));
     p.shares = shares_for(p, units_of(p));
+    p.by_share = units_of(p) > p.shares;
 }
 
 int64_t queries_workspace_most(const QueriesParams &p0) {
-    // Fewer queries may take another kernel, fewer records or positions make more or less whole:
-    // of each kernel the most units that are split.
+    // Fewer queries may take another kernel, fewer records or positions fewer shares.
     const int64_t most = (int64_t)p0.max_queries * p0.fd_G.d;
     int64_t bytes = 0;
-    for (const int64_t rows : {most < 32 ? most : 32, most < 128 ? most : 128, most}) {
-        QueriesParams p = p0;
-        shape(p, rows);
-        const int64_t units = units_of(p) < kWholeUnits ? units_of(p) : kWholeUnits;
-        p.shares = shares_for(p, units);
-        const int64_t need = split_bytes(p, units);
-        if (need > bytes) bytes = need;
-    }
+    for (const int64_t rows : {most < 32 ? most : 32, most < 128 ? most : 128, most})
+        for (const int32_t tokens : {p0.max_tokens, p0.max_tokens < kShort ? p0.max_tokens : kShort}) {
+            QueriesParams p = p0;
+            p.max_tokens = tokens;
+            shape(p, rows);
+            p.shares = shares_for(p, units_of(p));
+            const int64_t need = split_bytes(p);
+            if (need > bytes) bytes = need;
+        }
     return bytes;
 }
 
@@ -184,9 +189,9 @@ int64_t queries_workspace(QueriesParams &p, char *base) {
         return x;
     };
     const int64_t rows = 2 * (int64_t)p.shares * p.heads * p.rows;
-    p.total = reinterpret_cast<int64_t *>(take(16));
     if (p.whole) return at;
-    p.units = reinterpret_cast<UnitSteps *>(take(units_of(p) * (int64_t)sizeof(UnitSteps)));
+    p.each = reinterpret_cast<int64_t *>(take(16));
+    p.cuts = reinterpret_cast<Cut *>(take(p.shares * (int64_t)sizeof(Cut)));
     p.part_ml = reinterpret_cast<float *>(take(rows * 8));
     p.part_o = reinterpret_cast<float *>(take(rows * p.Dv * 4));
     return at;
@@ -216,14 +221,14 @@ int launch_queries(const QueriesParams &p, hipStream_t stream) {
                                                                                                        : p.heads * p.rows;
         // several rows a thread where there are more than the device holds threads for
         const int per = lines / split;
+        const int64_t joined = units < p.shares ? units : p.shares;
         int turns = 1;
-        while (turns < 8 && units * rows > (int64_t)kJoinBlocks * turns * per) turns *= 2;
+        while (turns < 8 && joined * rows > (int64_t)kJoinBlocks * turns * per) turns *= 2;
         const int32_t runs = (rows + per * turns - 1) / (per * turns);
-        const size_t lds = split > 1 ? sizeof(float) * lines * (p.Dv + 2) : 0;
-        for (int64_t at = 0; at < units * runs; at += kMaxBlocks) {
-            const int64_t some = units * runs - at < kMaxBlocks ? units * runs - at : kMaxBlocks;
-            hipLaunchKernelGGL(p.f16 ? kvx_queries_join_kernel<true> : kvx_queries_join_kernel<false>, dim3((uint32_t)some),
-                               dim3(kThreads), lds, stream, p, r0, at, runs, split, turns);
+        if (p.shares > 1) {
+            const size_t lds = split > 1 ? sizeof(float) * lines * (p.Dv + 2) : 0;
+            hipLaunchKernelGGL(p.f16 ? kvx_queries_join_kernel<true> : kvx_queries_join_kernel<false>,
+                               dim3((uint32_t)((p.by_share ? p.shares : units) * runs)), dim3(kThreads), lds, stream, p, r0, runs, split, turns);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
     }

@@ -12,9 +12,11 @@ namespace kvx {
 #endif
 constexpr int kQueriesGroup = KVX_QUERIES_GROUP;
 
-// Where a unit's steps lie among all steps of a launch with shares.
-struct UnitSteps {
-    int64_t first, steps;
+// A unit that may lie in several shares: of all steps of a launch its first tile's and its
+// last; record -1: none.
+struct Cut {
+    int64_t first, last;
+    int32_t record, group, block, reserved;
 };
 
 struct QueriesParams {
@@ -37,10 +39,11 @@ struct QueriesParams {
     // workgroup, and the groups of them; rows of a block, blocks of a record and cache
     // head at most; positions of a step; whether every unit has its own workgroup
     // (whole), else the shares of the steps
-    int32_t waves, team, heads, groups, rows, blocks, step, whole, shares;
+    int32_t waves, team, heads, groups, rows, blocks, step, whole, shares, by_share;
     // workspace
-    int64_t *total;              // steps of the launch
-    UnitSteps *units;            // [record of the launch][group of cache heads][block]
+    Cut *cuts;                   // [record of the launch][group][block], or where there are more of them
+                                 // than shares, [share]: the one that it begins inside
+    int64_t *each;               // steps of a share
     float *part_ml;              // [place][head of the group][row][2]
     float *part_o;               // [place][head of the group][row][Dv]
 };
