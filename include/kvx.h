@@ -729,6 +729,7 @@ typedef struct kvx_queries_req {
  * in 32 bits.
  * q heads, head_dim and v_dim as kvx_attend; max_queries x G at most 2^30.  lse:
  * num_rows of q x q heads floats, or NULL.  Rows of no record keep what they hold.
+ * out and lse must not overlap what is read.
  * workspace: kvx_queries_workspace() bytes for the same arguments, or more,
  * 16-byte aligned; what it holds before a call does not matter.  Calls that may
  * run at the same time need one each. */
