@@ -144,6 +144,13 @@ __device__ __forceinline__ int64_t place_of(int64_t first, int64_t k, int64_t ea
     return first > k * each ? shares + k : k;
 }
 
+// Partial results of 32 rows from `row` on, of values 32 d to 32 d + 31: [j][row c][half e][4], for the
+// values 8 j + 4 e + x, as a lane has them.
+__host__ __device__ constexpr int wide_blocks(int dv) { return (dv + 31) / 32; }
+__device__ __forceinline__ float *part_of(const QueriesParams &p, int64_t row, int d) {
+    return p.part_o + (row * wide_blocks(p.Dv) + 32 * d) * 32;
+}
+
 __device__ __forceinline__ int64_t share_of(int64_t total, int64_t shares) {
     const int64_t each = quotient(total + shares - 1, shares);
     return each < 1 ? 1 : each;
@@ -973,13 +980,16 @@ struct Queries {
         } else {
             const int64_t row = (piece.place * p.heads + (TEAM > 1 ? 0 : wave / streams)) * p.rows + x - block0;
             if (half == 0 && mine == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * row) = make_float2(m, l);
-            float *dst = p.part_o + row * p.Dv + mine + 4 * half;
+            // a wavefront's 1024 bytes side by side
+            const int64_t block = row - (ln & 31);
+            const int at = 4 * (2 * (ln & 31) + half);
 #pragma unroll
             for (int d = 0; d < DB; ++d)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     if (mine + 32 * d + 8 * j < p.Dv)
-                        *reinterpret_cast<f32x4 *>(dst + 32 * d + 8 * j) = f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
+                        *reinterpret_cast<f32x4 *>(part_of(p, block, mine / 32 + d) + 256 * j + at) =
+                            f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
         }
     }
 };

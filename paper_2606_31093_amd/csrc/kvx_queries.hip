@@ -7,19 +7,17 @@
 namespace kvx {
 namespace {
 
-constexpr int kThreads = 256;
-#ifndef KVX_JB
-#define KVX_JB 2048
-#endif
-constexpr int kJoinBlocks = KVX_JB;
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
 
-// A workgroup joins some rows of a unit: out = sum 2^(m_c - M) o_c / sum 2^(m_c - M) l_c.
-// Dv / 4 threads side by side take a row's values; `split` such rows of threads share its
-// parts and add up in LDS; each takes `turns` rows one after the other.
+// A wavefront joins 32 rows x 32 values of a unit, or fewer rows and more values: out = sum 2^(m_c - M) o_c / sum 2^(m_c - M) l_c.
+// `split` wavefronts share the parts and add up in LDS.  Of 32 values lane 2 c + e has 8 j + 4 e .. + 3
+// (j < 4) of row c, as the first kernel's lane (c, e) stored them.
 template <bool F16>
 __global__ void __launch_bounds__(kThreads) kvx_queries_join_kernel(QueriesParams p, int64_t r0, int32_t runs, int32_t split,
-                                                                    int32_t turns) {
-    extern __shared__ __align__(16) float sums[];        // [row of threads][Dv], then their m and l
+                                                                    int32_t lines, int32_t row_blocks) {
+    __shared__ f32x4 sums[kWaves][4][64];
+    __shared__ float2 tops[kWaves][64];
     const int64_t each = *p.each;
     const int id = blockIdx.x / (uint32_t)runs, run = blockIdx.x - id * runs, H = p.pool.H, G = p.fd_G.d;
     const Cut u = p.cuts[id];                            // by units, of no meaning where there is no such unit
@@ -31,76 +29,82 @@ __global__ void __launch_bounds__(kThreads) kvx_queries_join_kernel(QueriesParam
     // Parts in shares k0 .. k1; of those that begin inside the unit the first is its own.
     const int64_t k0 = quotient(u.first, each), k1 = quotient(u.last, each);
     if (k0 == k1 || (p.by_share && id != k0 + 1)) return;        // one part: written by the first launch
-    const int cols = p.Dv / 4, lines = kThreads / cols, col = threadIdx.x % cols, line = threadIdx.x / cols;
-    const int per = lines / split, mine = line % split, slots = p.heads * p.rows;
-    for (int turn = 0; turn < turns; ++turn) {
-        const int x = (run * turns + turn) * per + line / split;       // row of the block, of each head of the group
-        const int h = group * p.heads + x / p.rows;
-        const int64_t row = (int64_t)b * p.rows + x % p.rows;
-        const bool on = line < per * split && x < slots && row < (int64_t)rec.n_queries * G;
-        float m = -INFINITY, l = 0.f;
-        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-        if (on) {
-            for (int64_t k = k0 + mine; k <= k1; k += 4 * split) {
-                f32x4 y[4];
-                float2 ml[4];
-                // all on their way at once
+    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, c = lane / 2 % lines, e = lane % 2;
+    const int item = (run * kWaves + wave) / split, mine = wave % split, side = 32 / lines;
+    const int wide = wide_blocks(p.Dv), turns = (wide + side - 1) / side;
+    const int d = item % turns * side + lane / 2 / lines, rb = item / turns % row_blocks, head_of = item / turns / row_blocks;
+    const int64_t row = (int64_t)b * p.rows + rb * 32 + c;
+    const bool on = head_of < p.heads && d < wide && row < (int64_t)rec.n_queries * G;
+    float m = -INFINITY, l = 0.f;
+    f32x4 sum[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    ml[i] = make_float2(-INFINITY, 0.f);
-                    y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-                    if (k + i * split > k1) continue;
-                    const int64_t at = place_of(u.first, k + i * split, each, p.shares) * slots + x;
-                    ml[i] = *reinterpret_cast<const float2 *>(p.part_ml + 2 * at);
-                    y[i] = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p.part_o + at * p.Dv + 4 * col));
-                }
-                float top = m;
+    for (int j = 0; j < 4; ++j) sum[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (on) {
+        const int64_t slots = p.heads * p.rows, slot = head_of * p.rows + rb * 32;
+        for (int64_t k = k0 + mine; k <= k1; k += 2 * split) {
+            f32x4 y[2][4];
+            float2 ml[2];
+            // all on their way at once
 #pragma unroll
-                for (int i = 0; i < 4; ++i) top = fmaxf(top, ml[i].x);
-                const float f = weight(m, top);
-                m = top;
-                l *= f;
-                sum *= f;
+            for (int i = 0; i < 2; ++i) {
+                ml[i] = make_float2(-INFINITY, 0.f);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float w = weight(ml[i].x, m);
-                    l += ml[i].y * w;
-                    sum += y[i] * w;
-                }
+                for (int j = 0; j < 4; ++j) y[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (k + i * split > k1) continue;
+                const int64_t at = place_of(u.first, k + i * split, each, p.shares) * slots + slot;
+                ml[i] = *reinterpret_cast<const float2 *>(p.part_ml + 2 * (at + c));
+                const float *from = part_of(p, at, d) + 4 * (2 * c + e);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (32 * d + 8 * j < p.Dv) y[i][j] = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(from + 256 * j));
             }
-        }
-        if (split > 1) {
-            float *ml = sums + (int64_t)lines * p.Dv;
-            if (turn > 0) __syncthreads();
-            if (line < lines) {
-                *reinterpret_cast<f32x4 *>(sums + line * p.Dv + 4 * col) = sum;
-                if (col == 0) {
-                    ml[2 * line] = m;
-                    ml[2 * line + 1] = l;
-                }
-            }
-            __syncthreads();
-            if (!on || mine != 0) continue;
-            float top = -INFINITY;
-            for (int k = 0; k < split; ++k) top = fmaxf(top, ml[2 * (line + k)]);
+            const float top = fmaxf(m, fmaxf(ml[0].x, ml[1].x)), f = weight(m, top), w0 = weight(ml[0].x, top), w1 = weight(ml[1].x, top);
             m = top;
-            l = 0.f;
-            sum = f32x4{0.f, 0.f, 0.f, 0.f};
-            for (int k = 0; k < split; ++k) {
-                const float w = weight(ml[2 * (line + k)], m);
-                l += ml[2 * (line + k) + 1] * w;
-                sum += *reinterpret_cast<const f32x4 *>(sums + (line + k) * p.Dv + 4 * col) * w;
-            }
+            l = l * f + ml[0].y * w0 + ml[1].y * w1;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum[j] = sum[j] * f + y[0][j] * w0 + y[1][j] * w1;
         }
-        if (!on) continue;
-        const int i = (int)fd_div(p.fd_G, (uint32_t)row), head = h * G + (int)(row - (int64_t)i * G);
-        if (p.lse && col == 0)
-            p.lse[(rec.row_off + i) * H * G + head] =
-                l > 0.f || l != l ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
-        const float v_scale = p.scales ? p.scales[(p.pool.C - 1) * H + h] : 1.f;
-        sum *= l == 0.f ? 0.f : v_scale / l;
-        char *dst = p.out.base + (rec.row_off + i) * p.out.s_row + head * p.out.s_head;
-        *reinterpret_cast<u32x2 *>(dst + 8 * col) = u32x2{Half<F16>::pack(sum[0], sum[1]), Half<F16>::pack(sum[2], sum[3])};
+    }
+    if (split > 1) {
+        tops[wave][lane] = make_float2(m, l);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sums[wave][j][lane] = sum[j];
+        __syncthreads();
+        if (mine != 0) return;
+        float top = m;
+        for (int k = 1; k < split; ++k) top = fmaxf(top, tops[wave + k][lane].x);
+        const float f = weight(m, top);
+        l *= f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[j] *= f;
+        for (int k = 1; k < split; ++k) {
+            const float w = weight(tops[wave + k][lane].x, top);
+            l += tops[wave + k][lane].y * w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum[j] += sums[wave + k][j][lane] * w;
+        }
+        m = top;
+    }
+    if (!on) return;
+    const int h = group * p.heads + head_of, i = (int)fd_div(p.fd_G, (uint32_t)row), head = h * G + (int)(row - (int64_t)i * G);
+    if (p.lse && d == 0 && e == 0)
+        p.lse[(rec.row_off + i) * H * G + head] =
+            l > 0.f || l != l ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    const float v_scale = p.scales ? p.scales[(p.pool.C - 1) * H + h] : 1.f;
+    const float f = l == 0.f ? 0.f : v_scale / l;
+    char *dst = p.out.base + (rec.row_off + i) * p.out.s_row + head * p.out.s_head + 2 * (32 * d + 8 * e);
+#pragma unroll
+    for (int j = 0; j < 4; j += 2) {                     // whole eights, every second one a lane's
+        u32x2 x[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const f32x4 y = sum[j + k] * f;
+            x[k] = u32x2{Half<F16>::pack(y[0], y[1]), Half<F16>::pack(y[2], y[3])};
+        }
+        const u32x2 own = e ? x[1] : x[0], give = e ? x[0] : x[1];
+        const u32x2 got = {(uint32_t)__shfl_xor((int)give[0], 1), (uint32_t)__shfl_xor((int)give[1], 1)};
+        if (32 * d + 8 * (j + e) < p.Dv)
+            *reinterpret_cast<u32x4 *>(dst + 16 * j) = e ? u32x4{got[0], got[1], own[0], own[1]} : u32x4{own[0], own[1], got[0], got[1]};
     }
 }
 
@@ -148,7 +152,7 @@ int32_t shares_for(const QueriesParams &p, int64_t units) {
 int64_t split_bytes(const QueriesParams &p) {
     // two parts a share, its first and its last
     const int64_t rows = 2 * (int64_t)p.shares * p.heads * p.rows;
-    return 64 + (int64_t)p.shares * (int64_t)sizeof(Cut) + rows * 8 + rows * p.Dv * 4;
+    return 64 + (int64_t)p.shares * (int64_t)sizeof(Cut) + rows * 8 + rows * wide_blocks(p.Dv) * 128;
 }
 
 int64_t units_of(const QueriesParams &p) {
@@ -193,7 +197,7 @@ int64_t queries_workspace(QueriesParams &p, char *base) {
     p.each = reinterpret_cast<int64_t *>(take(16));
     p.cuts = reinterpret_cast<Cut *>(take(p.shares * (int64_t)sizeof(Cut)));
     p.part_ml = reinterpret_cast<float *>(take(rows * 8));
-    p.part_o = reinterpret_cast<float *>(take(rows * p.Dv * 4));
+    p.part_o = reinterpret_cast<float *>(take(rows * wide_blocks(p.Dv) * 128));
     return at;
 }
 
@@ -213,22 +217,19 @@ int launch_queries(const QueriesParams &p, hipStream_t stream) {
         const int64_t n = p.n_reqs - r0 < kQueriesGroup ? p.n_reqs - r0 : kQueriesGroup;
         if ((e = launch(p, r0, n, stream)) != hipSuccess) return e;
         const int64_t units = n * p.groups * p.blocks;
-        // Rows of threads that share a row's parts: as many as there are parts, on average.
-        const int lines = kThreads / (p.Dv / 4);
-        int split = 1;
-        while (2 * split <= lines && units * 8 * split < p.shares) split *= 2;
-        const int rows = p.heads == 1 && p.blocks == 1 && (int64_t)p.max_queries * p.fd_G.d < p.rows ? p.max_queries * p.fd_G.d
-                                                                                                       : p.heads * p.rows;
-        // several rows a thread where there are more than the device holds threads for
-        const int per = lines / split;
-        const int64_t joined = units < p.shares ? units : p.shares;
-        int turns = 1;
-        while (turns < 8 && joined * rows > (int64_t)kJoinBlocks * turns * per) turns *= 2;
-        const int32_t runs = (rows + per * turns - 1) / (per * turns);
         if (p.shares > 1) {
-            const size_t lds = split > 1 ? sizeof(float) * lines * (p.Dv + 2) : 0;
+            // Wavefronts that share the parts: as many as there are pairs of them, on average.
+            int split = 1;
+            while (split < kWaves && units * 2 * split < p.shares) split *= 2;
+            const int64_t most = (int64_t)p.max_queries * p.fd_G.d;
+            const int32_t row_blocks = ((most < p.rows ? (int)most : p.rows) + 31) / 32;
+            int32_t lines = 1;
+            while (lines < 32 && lines < most) lines *= 2;
+            const int32_t turns = (wide_blocks(p.Dv) * lines + 31) / 32;
+            const int32_t runs = (p.heads * row_blocks * turns * split + kWaves - 1) / kWaves;
             hipLaunchKernelGGL(p.f16 ? kvx_queries_join_kernel<true> : kvx_queries_join_kernel<false>,
-                               dim3((uint32_t)((p.by_share ? p.shares : units) * runs)), dim3(kThreads), lds, stream, p, r0, runs, split, turns);
+                               dim3((uint32_t)((p.by_share ? p.shares : units) * runs)), dim3(kThreads), 0, stream, p, r0, runs, split,
+                               lines, row_blocks);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
     }

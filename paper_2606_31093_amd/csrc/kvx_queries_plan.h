@@ -45,7 +45,7 @@ struct QueriesParams {
                                  // than shares, [share]: the one that it begins inside
     int64_t *each;               // steps of a share
     float *part_ml;              // [place][head of the group][row][2]
-    float *part_o;               // [place][head of the group][row][Dv]
+    float *part_o;               // [place][head of the group][row / 32][value / 32][4][32][2][4]
 };
 
 // The division of a call's work, from the sizes alone; the workspace of a planned
