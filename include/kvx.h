@@ -724,9 +724,9 @@ typedef struct kvx_queries_req {
  * Positions that cannot be resolved take no part.  A query that sees no position
  * (or with every score -inf) gives zeros and lse -inf; what stands in positions
  * that it does not see, NaN and infinities too, does not reach it.
- * w is rounded to the rows' type for its product with V (with up to 32 rows of
- * max_queries x G held in two parts as in kvx_attend); sums, maxima and l are held
- * in 32 bits.
+ * w is rounded to the rows' type for its product with V (with max_queries x G up
+ * to 32 and head_dim up to 256 held in two parts as in kvx_attend); sums, maxima
+ * and l are held in 32 bits.
  * q heads, head_dim and v_dim as kvx_attend; max_queries x G at most 2^30.  lse:
  * num_rows of q x q heads floats, or NULL.  Rows of no record keep what they hold.
  * out and lse must not overlap what is read.

