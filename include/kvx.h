@@ -693,7 +693,7 @@ int kvx_append_normed(const kvx_pool *pool, int32_t layer, const float *scales,
 typedef struct kvx_scores {
     const float *slopes;         /* device, one for each query head; NULL: none */
     float scale;
-    float cap;                   /* 0: not capped; else > 0 */
+    float cap;                   /* 0: not capped; else in (0, 2^100] */
     int32_t window;              /* 0: none; else >= 1 */
     int32_t reserved;            /* 0 */
 } kvx_scores;

@@ -237,7 +237,7 @@ int view_norm(const kvx_norm *n, const char *name, Known &known, HeadNorm &out) 
 int check_scores(const kvx_scores *x) {
     if (!x) return fail(KVX_ERR_NULL, "scores is NULL");
     if (x->reserved != 0) return fail(KVX_ERR_RANGE, "scores: reserved field must be 0");
-    if (!(x->cap >= 0.f) || std::isinf(x->cap)) return fail(KVX_ERR_RANGE, "scores: cap must be 0 (none) or positive");
+    if (!(x->cap >= 0.f && x->cap <= 0x1p100f)) return fail(KVX_ERR_RANGE, "scores: cap must be 0 (none) or in (0, 2^100]");
     if (x->window < 0) return fail(KVX_ERR_RANGE, "scores: window %d must be >= 0", x->window);
     if ((reinterpret_cast<uintptr_t>(x->slopes) & 3u) != 0) return fail(KVX_ERR_ALIGN, "slopes is not 4-byte aligned");
     return KVX_OK;

@@ -194,6 +194,18 @@ __device__ __forceinline__ bool not_finite(uint32_t w) {
 // Whether LDS has room for one tile only.
 __host__ __device__ constexpr bool one_tile(int dk, int kv) { return dk > 256 && kv == 2; }
 
+// Caps above this, in units of log2: cap - 2 cap / (1 + e^2x) would lose the digits of scores
+// far below the cap, up to 2^-22 of it.
+constexpr float kWideCap = 256.f;
+
+// tanh x to 2^-19 of it, z = 2 x log2 e: below 1/4 its series (the next term is 2^-27 of it), else
+// 1 - 2 / (1 + e^2x).
+__device__ __forceinline__ float tanh_of(float x, float z) {
+    const float y = x * x;
+    const float small = x + x * y * (-1.f / 3 + y * (2.f / 15 + y * (-17.f / 315 + y * (62.f / 2835))));
+    return fabsf(x) < 0.25f ? small : 1.f + 2.f * __builtin_amdgcn_rcpf(-1.f - exp2_fast(z));
+}
+
 // The larger of three; what is not a number counts for nothing.
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float x;
@@ -574,6 +586,7 @@ struct Queries {
             if (GENERAL && p.cap > 0.f) {
                 cap2 = p.cap * kLog2e;
                 cap_unit = 2.f * unit / p.cap;
+                if (cap_unit > 3e38f) cap_unit = 3e38f;      // a score of 0 stays one
             }
             const int block0 = piece.b * p.rows;
             x0 = block0 + part / SPLIT * 32;
@@ -720,7 +733,17 @@ struct Queries {
                 float from = unit, shift = 0.f;  // scores are s * from + shift
                 if (on) {
                     if (GENERAL) {
-                        if (seldom(cap_unit > 0.f)) {
+                        if (seldom(cap2 > kWideCap)) {
+                            const float near = 0.5f * kLn2 * cap_unit;
+#pragma unroll
+                            for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) {
+                                    if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                                    s[pb][i] = cap2 * tanh_of(s[pb][i] * near, s[pb][i] * cap_unit);
+                                }
+                            from = 1.f;
+                        } else if (seldom(cap_unit > 0.f)) {
                             // cap tanh(x) = cap - 2 cap / (1 + e^2x)
 #pragma unroll
                             for (int pb = 0; pb < PB; ++pb)

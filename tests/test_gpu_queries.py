@@ -212,7 +212,7 @@ def random_tree(rng, n, empty=False):
 
 
 def queries_case(seed, spec, kind, cache, recs, G, v_dim=None, scale=None, cap=0.0, slopes=False, window=0, tree=False,
-                 spoil=False, size=1.0, gap=0, workspace=None, call_args=None, expect=0, pt_edit=None, strided=False):
+                 spoil=False, size=1.0, gap=0, workspace=None, call_args=None, expect=0, pt_edit=None, strided=False, wide_cap=False):
     """recs: (start, end, n_queries, prefix); gap: rows between records that belong to none."""
     rng = np.random.default_rng(seed)
     H, C, D = spec.H, spec.C, spec.D
@@ -267,16 +267,17 @@ def queries_case(seed, spec, kind, cache, recs, G, v_dim=None, scale=None, cap=0
         kvx.kvx_attend_prompt(*head, most_q, most, ws, **args)
     torch.cuda.synchronize()
     assert int(err.item()) == expect
-    check(want, rows_values(view, kind), lse.cpu().numpy().astype(np.float64), kind, D, cap)
+    check(want, rows_values(view, kind), lse.cpu().numpy().astype(np.float64), kind, D, 0.0 if wide_cap else cap,
+          2.0 ** -19 if wide_cap else 0.0)
     if strided:
         assert (out[:, Hq:] == 7).all() and (out[:, :, v:] == 7).all()
 
 
-def check(want, got, got_lse, kind, D, cap=0.0):
+def check(want, got, got_lse, kind, D, cap=0.0, relative=0.0):
     w_out, w_lse, mine, mag, dots, size, sums = want
     assert (got[~mine] == 7).all() and (got_lse[~mine] == 7).all()
     u = U[kind]
-    ds = ((D + 8) * 2.0 ** -24 * dots + 2.0 ** -20 * cap + 2.0 ** -21 * size)[:, None]
+    ds = ((D + 8) * 2.0 ** -24 * dots + 2.0 ** -20 * cap + (2.0 ** -21 + relative) * size)[:, None]
     off = np.abs(got - w_out) - (u * np.abs(w_out) + (1 + u) * (u + 2 * ds + 2.0 ** -20)[..., None] * mag)
     if kind == "f16":
         off -= 2.0 ** -25 + 2.0 ** -32 * sums
@@ -324,6 +325,26 @@ def test_prompt_scores(C, H, D, G, v, cap, slopes, window, kind, cache):
     queries_case(3, spec, kind, cache, RECS, G, v or None, cap=cap, slopes=slopes, window=window, spoil=True, size=4.0)
     few = [(0, 100, 2, 0), (17, 90, 1, 0), (0, 260, 2, 0), (0, 64, 1, 64)]
     queries_case(4, spec, kind, cache, few, G, v or None, cap=cap, slopes=slopes, window=window, spoil=True, size=4.0)
+
+
+@pytest.mark.parametrize("kind,cache", [("bf16", "bf16"), ("f16", "e4m3")])
+@pytest.mark.parametrize("C,H,D,G,v", [(2, 2, 64, 4, 0), (2, 1, 128, 7, 0), (2, 1, 256, 2, 0), (1, 1, 576, 16, 512)])
+@pytest.mark.parametrize("cap,scale", [(200.0, 2.0), (1e6, None), (2.0 ** 100, None)])
+def test_wide_caps(cap, scale, C, H, D, G, v, kind, cache):
+    """Scores far below the cap, and some near it, keep their digits: tanh is off by 22 roundings of 2^-24
+    at 1/4, where the series ends (the sum 1 + e^2x, its reciprocal and 1 less twice that: 11; those of the
+    exponent: 9; the cap's: 2), and by fewer elsewhere, below 2^-19 of it."""
+    spec = PoolSpec(1, C, H, D, T=16, N=60, e=1 if cache == "e4m3" else 2, layout=LAYOUTS[D // 16 % 4])
+    queries_case(5, spec, kind, cache, RECS, G, v or None, scale=scale, cap=cap, slopes=D == 128, size=4.0, wide_cap=True)
+    few = [(0, 100, 2, 0), (17, 90, 1, 0), (0, 260, 2, 0)]
+    queries_case(6, spec, kind, cache, few, G, v or None, scale=scale, cap=cap, size=4.0, wide_cap=True)
+
+
+@pytest.mark.parametrize("D", [64, 256])
+def test_tiny_caps(D):
+    """Scores of 0 under a cap so small that a score over it is infinite: the mean of what is seen."""
+    spec = PoolSpec(1, 2, 1, D, T=16, N=60, e=2, layout="LPCTHD")
+    queries_case(7, spec, "bf16", "bf16", RECS, 2, scale=8.0, cap=1e-39, size=0.0)
 
 
 @pytest.mark.parametrize("kind,cache", TYPES)

@@ -109,7 +109,7 @@ REFUSED = [
     (0, {}), (0, dict(s=scores(FAKE, -1.0, 30.0, 5))), (0, dict(spec=ONE, q=rows(16, 576), out=rows(16, 512))),
     (0, dict(spec=F8, scales=FAKE)),
     (NULL, dict(s=None)), (RANGE, dict(s=scores(reserved=1))), (RANGE, dict(s=scores(cap=-1.0))),
-    (RANGE, dict(s=scores(cap=float("inf")))), (RANGE, dict(s=scores(cap=float("nan")))), (RANGE, dict(s=scores(window=-1))),
+    (RANGE, dict(s=scores(cap=float("inf")))), (RANGE, dict(s=scores(cap=2.0 ** 101))), (RANGE, dict(s=scores(cap=float("nan")))), (RANGE, dict(s=scores(window=-1))),
     (ALIGN, dict(s=scores(FAKE + 2))), (RANGE, dict(most_q=-1)), (RANGE, dict(most_q=(1 << 22) + 1)), (RANGE, dict(most=-1)),
     (RANGE, dict(most=(1 << 22) + 1)), (ALIGN, dict(lse=FAKE + 2)), (SHAPE, dict(out=rows(4, 64))), (SHAPE, dict(out=rows(8, 64, n=9))),
     (SHAPE, dict(out=rows(8, 64, dtype=1))), (SHAPE, dict(out=rows(8, 56))), (SHAPE, dict(q=rows(8, 72), out=rows(8, 64))),
