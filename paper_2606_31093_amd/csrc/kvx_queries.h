@@ -733,24 +733,26 @@ struct Queries {
                 float from = unit, shift = 0.f;  // scores are s * from + shift
                 if (on) {
                     if (GENERAL) {
-                        if (seldom(cap2 > kWideCap)) {
-                            const float near = 0.5f * kLn2 * cap_unit;
+                        if (seldom(cap_unit > 0.f)) {
+                            if (seldom(cap2 > kWideCap)) {
+                                const float near = 0.5f * kLn2 * cap_unit;
 #pragma unroll
-                            for (int pb = 0; pb < PB; ++pb)
+                                for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
-                                for (int i = 0; i < 16; ++i) {
-                                    if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
-                                    s[pb][i] = cap2 * tanh_of(s[pb][i] * near, s[pb][i] * cap_unit);
-                                }
-                            from = 1.f;
-                        } else if (seldom(cap_unit > 0.f)) {
-                            // cap tanh(x) = cap - 2 cap / (1 + e^2x)
+                                    for (int i = 0; i < 16; ++i) {
+                                        if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                                        s[pb][i] = cap2 * tanh_of(s[pb][i] * near, s[pb][i] * cap_unit);
+                                    }
+                                from = 1.f;
+                            } else {
+                                // cap tanh(x) = cap - 2 cap / (1 + e^2x)
 #pragma unroll
-                            for (int pb = 0; pb < PB; ++pb)
+                                for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
-                                for (int i = 0; i < 16; ++i) s[pb][i] = __builtin_amdgcn_rcpf(-1.f - exp2_fast(s[pb][i] * cap_unit));
-                            from = 2.f * cap2;
-                            shift = cap2;
+                                    for (int i = 0; i < 16; ++i) s[pb][i] = __builtin_amdgcn_rcpf(-1.f - exp2_fast(s[pb][i] * cap_unit));
+                                from = 2.f * cap2;
+                                shift = cap2;
+                            }
                         }
                         if (straight) {
                             shift = -slope * (float)(at - (int)t0);      // the rest of the bias is in the product
