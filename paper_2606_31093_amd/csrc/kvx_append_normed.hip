@@ -39,8 +39,9 @@ __global__ void __launch_bounds__(kThreads) kvx_append_normed_kernel(NormedParam
     const int32_t first = (int32_t)(blockIdx.x % (uint32_t)p.blocks) * p.tokens;
     const kvx_append_req q = p.reqs[r];
     const int64_t n = q.n_tokens;
-    if (n < 0 || q.reserved != 0 || q.pt_off < 0 || q.row_off < 0 || q.start < 0 || q.position < 0 ||
-        n > p.max_tokens || q.start + n > INT32_MAX || q.position + n > INT32_MAX || q.row_off > p.num_rows - n) {
+    // with positions of their own the record's is not used
+    if (n < 0 || q.reserved != 0 || q.pt_off < 0 || q.row_off < 0 || q.start < 0 || q.position < 0 || n > p.max_tokens ||
+        q.start + n > INT32_MAX || (!p.positions && q.position + n > INT32_MAX) || q.row_off > p.num_rows - n) {
         if (threadIdx.x == 0 && first == 0 && p.err) atomicOr(p.err, KVX_DERR_BAD_REQ);
         return;
     }
@@ -50,12 +51,14 @@ __global__ void __launch_bounds__(kThreads) kvx_append_normed_kernel(NormedParam
     bool bad_axis = false;
     for (int i = threadIdx.x; i < tokens * p.half; i += kThreads) {
         const uint32_t t = fd_div(p.fd_half, i), j = i - t * p.half;
-        int32_t at = q.position + first + (int32_t)t;
+        int32_t at;
         if (p.positions) {
             const int32_t axis = p.axis ? p.axis[j] : 0;
             const bool bad = axis < 0 || axis >= p.num_axes;
             bad_axis |= bad;
             at = p.positions[(bad ? 0 : axis) * p.pos_stride + q.row_off + first + t];
+        } else {
+            at = q.position + first + (int32_t)t;
         }
         const double turns = (double)at * (double)p.freq[j] * 0.15915494309189535;
         float s, c;
