@@ -616,11 +616,13 @@ struct Queries {
                                 (uint32_t)(seen < rec.end ? seen : rec.end)};
             if (biased) {
                 slope = p.slopes[h * G + g] * kLog2e;
-                // in three parts of the rows' type, for a product with whole numbers up to 63
+                // In three parts of the rows' type, for a product with whole numbers up to 63.  In half, whose
+                // values are 2^-24 apart at least, up to 2^-25 is left, in the bias 2^-19 unit: with a large unit
+                // it is added by hand.
                 const float x = slope / unit, a = V::lo(V::pack(x, 0.f)), b = V::lo(V::pack(x - a, 0.f));
                 slopes[0] = V::pack(a, b);
                 slopes[1] = V::pack(x - a - b, 0.f);
-                linear = cap_unit == 0.f && !__any(!(fabsf(x) < 1024.f));
+                linear = cap_unit == 0.f && !__any(!(fabsf(x) < 1024.f)) && !(F16 && unit > 2.f);
             }
             const int d0 = 16 * (HALVES ? 0 : wave % SPLIT * KS) + 8 * (lane_again() >> 5), left = none ? 0 : p.pool.D - d0;
             const char *src = p.q.base + (rec.row_off + i) * p.q.s_row + (int64_t)(h * G + g) * p.q.s_head + 2 * d0;

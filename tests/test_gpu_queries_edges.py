@@ -6,6 +6,7 @@ import torch
 
 import np_decode
 import np_queries as ref
+import test_gpu_queries as base
 from paper_2606_31093_amd import kvx
 from paper_2606_31093_amd.workloads import PoolSpec
 from test_gpu_decode import U, error_word, rows_tensor, rows_values, tensor
@@ -112,3 +113,20 @@ def test_norms_of_zeros_and_what_is_not_finite(inter, off):
         assert torch.isnan(got[0]).all() and (got[1] == 0).all() and torch.isnan(got[3]).all()
         for r in (2, 4):
             assert torch.isnan(got[r, 50]) and (got[r, :50] == 0).all() and (got[r, 51:] == 0).all()
+
+
+# ---------------------------------------------------------------------------
+# kvx_attend_prompt, kvx_attend_tree
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kind,cache", base.TYPES)
+@pytest.mark.parametrize("D,G", [(64, 4), (128, 7), (256, 2)])
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("scale,size", [(2.0 ** 13, 2.0 ** -14), (2.0 ** 17, 2.0 ** -17), (2.0 ** -12, 16.0), (3.0, 0.25)])
+def test_bias_under_large_and_small_scales(scale, size, tree, D, G, kind, cache):
+    """A bias keeps its digits whatever the scale makes of the products: slopes are small beside a large one,
+    large beside a small one."""
+    spec = PoolSpec(1, 2, 1, D, T=16, N=60, e=1 if cache == "e4m3" else 2)
+    recs = [(0, 300, 64, 0), (0, 130, 40, 0), (3, 90, 60, 0)]
+    base.queries_case(3, spec, kind, cache, recs, G, scale=scale, slopes=True, size=size, tree=tree)
+    base.queries_case(4, spec, kind, cache, [(0, 260, 2, 0), (7, 90, 1, 0)], G, scale=scale, slopes=True, size=size, tree=tree)
