@@ -367,7 +367,7 @@ int kvx_append_normed(const kvx_pool *pool, int32_t layer, const float *scales, 
         if (positions->num_axes < 1 || positions->num_axes > 16)
             return fail(KVX_ERR_RANGE, "positions: num_axes %d outside [1, 16]", positions->num_axes);
         if (positions->stride < 0 || (positions->num_axes > 1 && positions->stride < k->num_rows) ||
-            positions->stride > INT64_MAX / 128)
+            positions->stride > INT64_MAX / 128 || k->num_rows > INT64_MAX / 128)
             return fail(KVX_ERR_RANGE, "positions: stride %lld of axes of %lld rows", (long long)positions->stride,
                         (long long)k->num_rows);
         if (!positions->positions && k->num_rows > 0) return fail(KVX_ERR_NULL, "positions is NULL");

@@ -233,3 +233,12 @@ def test_definitions():
                 assert ref.sees(rec, i, t, window, bits) == ref.sees(rec, i, t, window, None)
     x = np.random.default_rng(1).standard_normal((3, 64))
     assert np.allclose((ref.norm(x, np.ones(32), 16, 0.0)[:, 16:48] ** 2).mean(axis=-1), 1)
+
+
+@pytest.mark.parametrize("n", [1 << 57, 1 << 61, 1 << 62, (1 << 63) - 1])
+def test_positions_of_more_rows_than_bytes_count(n):
+    """Rows that share elements (stride 0) may be any number; their positions' bytes have to fit 63 bits."""
+    k = rows(4, 64, n=n, s_row=0)
+    assert normed(q=None, q_out=None, k=k, v=k, pos=positions(stride=0)) == RANGE
+    assert normed(q=None, q_out=None, k=k, v=k, pos=positions(stride=n, axes=3)) == RANGE
+    assert normed(q=None, q_out=None, k=k, v=k) == 0
