@@ -1031,9 +1031,17 @@ __global__ void __launch_bounds__(64 * WAVES, DK <= 128 || SPLIT > 1 ? 2 : 1) kv
     // the other's exponentials fall together, not products and products.
     if (WAVES == 8 && wave < 4) __builtin_amdgcn_s_setprio(1);
     const kvx_queries_req *reqs = p.whole ? p.reqs : p.reqs + first;
-    int64_t at = 0, stop = 1, each = 0;
+    int64_t at = first + blockIdx.x, stop = at + 1, each = 0;        // of units (whole), else of steps
     int share = 0;
-    if (!p.whole) {
+    bool whole = p.whole;
+    if (p.one) {
+        const kvx_queries_req q = scalar(p.reqs[0]);
+        stop = valid(q, p) ? (int64_t)blocks_of(q, p) * p.groups : 0;
+        whole = stop >= kWholeUnits;
+        if (whole && at == 0 && threadIdx.x == 0) *p.each = 0;
+        if (!whole && at >= p.shares) return;
+    }
+    if (!whole) {
         // steps of a group of cache heads of the records before each
         if (p.blocks <= 8) {
             // few blocks a record: a thread each, whose reads are on their way together
@@ -1087,14 +1095,14 @@ __global__ void __launch_bounds__(64 * WAVES, DK <= 128 || SPLIT > 1 ? 2 : 1) kv
         const QueriesParams p = again();
         const kvx_queries_req *reqs = p.whole ? p.reqs : p.reqs + first;
         Span s;
-        int64_t here = 1;
+        int64_t here = gridDim.x;
         bool some = true;
-        if (p.whole) {
+        if (whole) {
             // Longest first: a record's last blocks see most.  Blocks of a record and group are n_reqs x groups
             // workgroups apart: with a multiple of 8 of them on one die, whose cache holds their keys.
-            const int64_t id = first + blockIdx.x, lists = (int64_t)p.n_reqs * p.groups, rank = quotient(id, lists);
+            const int64_t lists = (int64_t)p.n_reqs * p.groups, rank = quotient(at, lists);
             // Of several records each die takes every eighth block, so that long ones are no die's alone.
-            const int list = (int)((id - rank * lists + (p.n_reqs > 1 ? rank : 0)) % lists);
+            const int list = (int)((at - rank * lists + (p.n_reqs > 1 ? rank : 0)) % lists);
             r = list / p.groups;
             piece.group = list - r * p.groups;
             piece.rec = scalar(reqs[r]);
@@ -1172,7 +1180,7 @@ int launch_form(const QueriesParams &p, int64_t first, int64_t n, hipStream_t st
     const auto kernel = general ? kvx_queries_kernel<F16, E4M3, DK, DV, WAVES, TEAM, SPLIT, TILE, true>
                                 : kvx_queries_kernel<F16, E4M3, DK, DV, WAVES, TEAM, SPLIT, TILE, TEAM == 1>;
     const size_t lds = (size_t)(one_tile(DK, p.pool.C) ? 1 : 2) * TILE * 2 * DK * p.pool.C * (p.waves / TEAM);
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.whole ? n : p.shares)), dim3(64 * p.waves), lds, stream, p, first, (int32_t)n);
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)(p.whole ? n : p.one ? p.one : p.shares)), dim3(64 * p.waves), lds, stream, p, first, (int32_t)n);
     return hipGetLastError();
 }
 

@@ -6,8 +6,9 @@
 // the tiles that some row of it sees.  Either every unit has a workgroup of its own, or
 // the launch's steps are dealt out in equal shares, one to each workgroup that the device
 // holds at a time, and a unit that lies in several shares leaves a part (maximum, sum,
-// values, in 32 bits) in each.  Which, is a rule on sizes alone, so that a captured launch
-// serves other lengths; the shares themselves come from the records, on the device.
+// values, in 32 bits) in each.  Which, is a rule on sizes alone, and of one long record on what
+// it holds, so that a captured launch serves other lengths; the shares themselves come from the
+// records, on the device.
 
 #include "kvx_queries.h"
 
@@ -28,6 +29,7 @@ __global__ void __launch_bounds__(kThreads) kvx_queries_join_kernel(QueriesParam
     __shared__ f32x4 sums[kWaves][4][64];
     __shared__ float2 tops[kWaves][64];
     const int64_t each = *p.each;
+    if (each == 0) return;
     const int id = blockIdx.x / (uint32_t)runs, run = blockIdx.x - id * runs, H = p.pool.H, G = p.fd_G.d;
     const Cut u = p.cuts[id];                            // by units, of no meaning where there is no such unit
     const int list = id / p.blocks, of = p.by_share ? u.record : list / p.groups;
@@ -122,12 +124,25 @@ __global__ void __launch_bounds__(kThreads) kvx_queries_join_kernel(QueriesParam
 int resident(const QueriesParams &p) { return (p.team == 4 && p.pool.D <= 128) || (p.team == 1 && p.pool.D <= 64) ? 512 : 256; }
 // Units of up to this many steps are not split: a share's search and the join would cost more.
 constexpr int kWholeSteps = 8;
-// Nor are units so many and more of one record, or of short ones: the device deals them out
-// as it gets free, and those of one cache head, that run at the same time on one die, find their
-// keys in its cache.  A prompt of 8192 takes 2130 us so and 2202 in shares, 16 of 512 90 and 114.
-// Longer ragged ones leave compute units without work at the end: 16 of 333 to 2000, e4m3 and
-// biased, take 495 us so and 387 in shares, four of 1500 81 and 57.
-constexpr int kWholeUnits = 1024;
+// Nor are kWholeUnits and more of one record, or of short ones: the device deals them out as it
+// gets free, and those of one cache head, that run at the same time on one die, find their keys in
+// its cache.  A prompt of 8192 (32 heads of 128 on 8: 1024 units) takes 547 us so and 575 in shares,
+// one of 16384 2150 and 2250, 32 of 512 164 and 181.  Fewer units are uneven among the compute units
+// where all see about as much: 288 behind 60000 positions take 3710 so and 2400 in shares, though a
+// prompt of 4096 152 and 177, whose last blocks are short.  Longer ragged records leave compute units
+// without work at the end: 16 of 333 to 2000, e4m3 and biased, take 495 so and 387 in shares, four
+// of 1500 81 and 57.
+//
+// The units counted here are those of the limits, records may hold fewer.  A workgroup without a
+// unit takes 3 ns, so that short records have at most so many of them beside each record's first
+// block, and shares beyond: under limits of 2^20 queries 32 prompts of 256 take 70 us, 26900 otherwise.
+// With that many units shares are as fast: 64 prompts of 1000 971 us, whole 984.
+constexpr int kWholeMore = 8192;
+// One record's kernel looks how many units there are, and takes one or the other: at most so many
+// workgroups, which go on to a further unit.  One query behind 131072 positions takes 138 us under limits
+// of 16384 (2450 with a workgroup a unit), a chunk of 512 behind 100000 800 (2540).
+constexpr int kOneBlocks = 2048;
+static_assert(kOneBlocks >= 512, "as many as shares");
 // Records of up to this many positions: four wavefronts a workgroup, two of which begin and
 // end at different times, so that one computes while the other waits for its first tile.  16
 // prompts of 512 take 94 us, 102 in eights; one of 300 16.2 and 18.6.  Longer ones share a tile
@@ -179,7 +194,11 @@ int64_t units_of(const QueriesParams &p) {
 void plan_queries(QueriesParams &p) {
     shape(p, (int64_t)p.max_queries * p.fd_G.d);
     const int64_t units = (int64_t)p.n_reqs * p.groups * p.blocks;
-    p.whole = most_steps(p) <= kWholeSteps || (units >= kWholeUnits && (p.n_reqs == 1 || p.max_tokens <= kShort));
+    const bool many = units >= kWholeUnits;
+    p.whole = (most_steps(p) <= kWholeSteps || (many && p.max_tokens <= kShort)) &&
+              units - (int64_t)p.n_reqs * p.groups <= kWholeMore;
+    const int64_t most = kOneBlocks < kMaxBlocks ? kOneBlocks : kMaxBlocks;
+    p.one = !p.whole && many && p.n_reqs == 1 ? (int32_t)(units < most ? units : most) : 0;
     p.shares = shares_for(p, units_of(p));
     p.by_share = units_of(p) > p.shares;
 }

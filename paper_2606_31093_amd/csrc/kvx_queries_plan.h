@@ -12,6 +12,9 @@ namespace kvx {
 #endif
 constexpr int kQueriesGroup = KVX_QUERIES_GROUP;
 
+// So many units of one record, or of short ones, and more have a workgroup each (kvx_queries.hip).
+constexpr int kWholeUnits = 1024;
+
 // A unit that may lie in several shares: of all steps of a launch its first tile's and its
 // last; record -1: none.
 struct Cut {
@@ -38,12 +41,13 @@ struct QueriesParams {
     // launch: wavefronts of a workgroup, and how many share a tile; cache heads of a
     // workgroup, and the groups of them; rows of a block, blocks of a record and cache
     // head at most; positions of a step; whether every unit has its own workgroup
-    // (whole), else the shares of the steps
-    int32_t waves, team, heads, groups, rows, blocks, step, whole, shares, by_share;
+    // (whole), else the shares of the steps; one: workgroups of one record whose queries say
+    // which of the two, 0: not so
+    int32_t waves, team, heads, groups, rows, blocks, step, whole, shares, by_share, one;
     // workspace
     Cut *cuts;                   // [record of the launch][group][block], or where there are more of them
                                  // than shares, [share]: the one that it begins inside
-    int64_t *each;               // steps of a share
+    int64_t *each;               // steps of a share; 0: every unit had its own workgroup
     float *part_ml;              // [place][head of the group][row][2]
     float *part_o;               // [place][head of the group][row / 32][value / 32][4][32][2][4]
 };

@@ -1,5 +1,6 @@
 """Several tokens of a request on the GPU: arguments and values at the ends of their ranges, against
-definitions in 64 bits (np_queries).  Bounds as in test_gpu_queries.py."""
+definitions in 64 bits (np_queries); limits far above what the records hold.  Bounds
+as in test_gpu_queries.py."""
 import numpy as np
 import pytest
 import torch
@@ -7,9 +8,11 @@ import torch
 import np_decode
 import np_queries as ref
 import test_gpu_queries as base
+import test_gpu_queries_forms as forms
 from paper_2606_31093_amd import kvx
 from paper_2606_31093_amd.workloads import PoolSpec
 from test_gpu_decode import U, error_word, rows_tensor, rows_values, tensor
+from test_gpu_queries_forms import several_launches  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -130,3 +133,97 @@ def test_bias_under_large_and_small_scales(scale, size, tree, D, G, kind, cache)
     recs = [(0, 300, 64, 0), (0, 130, 40, 0), (3, 90, 60, 0)]
     base.queries_case(3, spec, kind, cache, recs, G, scale=scale, slopes=True, size=size, tree=tree)
     base.queries_case(4, spec, kind, cache, [(0, 260, 2, 0), (7, 90, 1, 0)], G, scale=scale, slopes=True, size=size, tree=tree)
+
+
+ONE = [
+    # (H, G, D, C, v, record, max_queries, max_tokens, more).  Few blocks under limits of many; as many as have a
+    # workgroup each, exactly and under wider limits; more than there are workgroups; one less than that many
+    (8, 4, 128, 2, 0, (0, 3000, 40, 0), 16384, 20000, {}), (8, 4, 128, 2, 0, (5, 3000, 1, 0), 1 << 22, 1 << 22, {}),
+    (256, 1, 64, 2, 0, (0, 1100, 1024, 0), 1024, 1100, {}), (256, 1, 64, 2, 0, (0, 1100, 1024, 7), 9000, 70000, {}),
+    (256, 1, 64, 2, 0, (0, 2304, 2304, 0), 2304, 2304, {}), (256, 1, 64, 2, 0, (0, 1500, 768, 0), 4096, 4096, {}),
+    (128, 2, 128, 2, 0, (0, 1200, 1100, 0), 1100, 1200, dict(slopes=True)), (64, 2, 256, 2, 0, (0, 1100, 1024, 0), 1024, 1100, dict(cap=30.0)),
+    (64, 2, 256, 2, 0, (0, 1100, 90, 0), 1024, 1100, dict(window=77)), (1, 16, 576, 1, 512, (0, 900, 60, 0), 1 << 20, 5000, {}),
+    (8, 4, 128, 2, 0, (0, 3000, 60, 0), 1 << 20, 5000, dict(tree=True)), (8, 1, 128, 2, 0, (0, 64, 0, 0), 1 << 20, 5000, {}),
+]
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("H,G,D,C,v,rec,most_q,most,more", ONE)
+def test_one_record_under_wide_limits(H, G, D, C, v, rec, most_q, most, more, cache):
+    """What the record holds, not the limits, says whether every block has a workgroup of its own."""
+    spec = PoolSpec(1, C, H, D, T=64, N=-(-rec[1] // 64) + 2, e=1 if cache == "e4m3" else 2)
+    forms.large_case(1, spec, "bf16", cache, [rec], G, v or None, max_queries=most_q, max_tokens=most, **more)
+
+
+@pytest.mark.parametrize("H,G,D,rec,most_q,most", [(256, 1, 64, (0, 1500, 1100, 0), 1100, 1500), (8, 4, 128, (0, 900, 30, 0), 1 << 20, 5000)])
+def test_one_record_in_launches_of_few(several_launches, H, G, D, rec, most_q, most):
+    """At most 1024 workgroups a launch."""
+    spec = PoolSpec(1, 2, H, D, T=64, N=40, e=2)
+    forms.large_case(2, spec, "bf16", "bf16", [rec], G, max_queries=most_q, max_tokens=most)
+
+
+@pytest.mark.parametrize("limits", [(256, 300), (100000, 400), (1 << 20, 512), (4096, 1000)])
+def test_many_records_under_wide_limits(limits):
+    """Short records, up to as many workgroups as they may need and with far more than that."""
+    spec = PoolSpec(1, 2, 4, 128, T=16, N=500, e=2)
+    recs = [(r % 3, 3 + 7 * r, 1 + 5 * r, 0) for r in range(40)]
+    forms.large_case(3, spec, "bf16", "bf16", recs, 4, max_queries=limits[0], max_tokens=limits[1])
+
+
+def test_malformed_record_under_wide_limits():
+    spec = PoolSpec(1, 2, 64, 64, T=16, N=40, e=2)
+    pool, pt = torch.zeros(spec.nbytes, dtype=torch.uint8, device="cuda"), tensor(np.arange(40, dtype=np.int32))
+    q = torch.randn(600, 64, 64, device="cuda").bfloat16()
+    ws = kvx.queries_workspace(spec, 1, 64, 1 << 20, 600)
+    for rec in ((0, 0, 0, 601, 600, 0), (0, 1, 0, 600, 600, 0), (0, 0, 5, 4, 1, 0), (-1, 0, 0, 600, 600, 0)):
+        out, err = torch.full_like(q, 7), error_word()
+        kvx.kvx_attend_prompt(q, out, pool, spec, 0, pt, kvx.device_queries_reqs([rec]), 1 << 20, 600, ws, dev_err=err)
+        assert int(err.item()) == kvx.DERR_BAD_REQ and (out == 7).all()
+
+
+def test_graph_of_other_lengths():
+    """One captured call, replayed for records that take either division and for a malformed one, with eager
+    calls in between: outputs by the definition, and equal bits of equal calls."""
+    spec = PoolSpec(1, 2, 128, 64, T=64, N=60, e=2)
+    H, D, most_q, most = spec.H, spec.D, 2500, 3500
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    pool = torch.randn(spec.elems, generator=g, device="cuda").bfloat16().view(torch.uint8)
+    pt = torch.randperm(60, generator=g, device="cuda").int()
+    q = torch.randn(most_q, H, D, generator=g, device="cuda").bfloat16()
+    out, lse, err = torch.zeros_like(q), torch.zeros(most_q, H, device="cuda"), error_word()
+    reqs = kvx.device_queries_reqs([(0, 0, 0, 1, 1, 0)])
+    ws = kvx.queries_workspace(spec, 1, H, most_q, most)
+
+    def call():
+        kvx.kvx_attend_prompt(q, out, pool, spec, 0, pt, reqs, most_q, most, ws, lse=lse, dev_err=err)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    values = forms.cache_of(pool, spec, "bf16")[0]
+    u = U["bf16"]
+    for rec in [(0, 0, 0, 3400, 1, 0), (0, 0, 0, 2500, 2500, 0), (0, 5, 0, 3000, 2, 0), (0, 0, 0, 3501, 5, 0), (0, 100, 0, 2300, 2048, 0),
+                (0, 0, 100, 3300, 1800, 0)]:
+        reqs.copy_(kvx.device_queries_reqs([rec]))
+        bad = rec[3] > most
+        w_out, w_lse, mag, dots, size = (None,) * 5 if bad else forms.exact(q, values, spec, pt, rec, D ** -0.5, D, None, 0.0, None, 0, None)
+        seen = []
+        for turn in range(4):
+            out.fill_(7), lse.fill_(7), ws.fill_(0xff), err.zero_()
+            torch.cuda.synchronize()
+            graph.replay() if turn % 2 == 0 else call()
+            torch.cuda.synchronize()
+            assert int(err.item()) == (kvx.DERR_BAD_REQ if bad else 0)
+            mine = torch.zeros(most_q, dtype=torch.bool, device="cuda")
+            if not bad:
+                mine[rec[1]:rec[1] + rec[4]] = True
+            assert (out[~mine] == 7).all() and (lse[~mine] == 7).all()
+            seen.append((out.clone(), lse.clone()))
+            assert torch.equal(out, seen[0][0]) and torch.equal(lse, seen[0][1])
+        if not bad:
+            ds = (D + 8) * 2.0 ** -24 * dots + 2.0 ** -21 * size
+            tol = u * w_out.abs() + (1 + u) * (u + 2 * ds + 2.0 ** -20)[..., None] * mag
+            assert ((out[mine].double() - w_out).abs() <= tol).all(), rec
+            assert ((lse[mine].double() - w_lse).abs() <= ds + 2.0 ** -20 * (1 + w_lse.abs())).all(), rec
