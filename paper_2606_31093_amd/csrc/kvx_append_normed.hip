@@ -293,7 +293,7 @@ int launch_append_normed(const NormedParams &p0, hipStream_t stream) {
         const int per = (p.items + lanes - 1) / lanes;
         if (per <= (halves ? 2 : 3) && per * lanes < p.per_lane * p.lanes) p.lanes = lanes, p.per_lane = per;
     }
-    const int per_token = heads * p.lanes * (p.vec ? 1 : 4);
+    const int64_t per_token = (int64_t)heads * p.lanes * (p.vec ? 1 : 4);      // heads: up to 2^23
     int64_t tokens = (4 * kThreads + per_token - 1) / per_token;
     if (p.half && tokens > kMaxHalf / p.half) tokens = kMaxHalf / p.half;
     if (tokens > 64) tokens = 64;

@@ -50,6 +50,20 @@ def test_record_positions_that_are_not_used(off):
     assert call(MOST - 20, None)[2] == 0
 
 
+@pytest.mark.parametrize("off", [0, 3])
+def test_most_heads(off):
+    """A token of 2^26 elements, the most, in heads of 8."""
+    H = 1 << 22
+    spec = PoolSpec(1, 2, H, 8, T=1, N=2, e=2)
+    x = torch.ones(1, 2 * H, 8, device="cuda").bfloat16()
+    pool, err = torch.zeros(spec.nbytes, dtype=torch.uint8, device="cuda"), error_word()
+    kvx.kvx_append_normed(pool, spec, 0, x[:, :H] * 4, x[:, H:] * 3, tensor(np.array([1], np.int32)),
+                          kvx.device_append_reqs([[0, 0, 0, 0, 1]]), 1, rope=kvx.Rope(torch.zeros(1, device="cuda"), off),
+                          k_norm=kvx.Norm(torch.full((8,), 2.0, device="cuda"), 0, 0.0), dev_err=err)
+    got = pool.view(torch.bfloat16).view(2, 2, H, 8)
+    assert int(err.item()) == 0 and not got[0].any() and (got[1, 0] == 2).all() and (got[1, 1] == 3).all()
+
+
 # rows of about 2^e, with one element of 2^one among them (None: none), and the norm's eps
 SIZES = [(66, None, 0.0), (126, None, 1e-6), (126, None, 0.0), (0, 70, 0.0), (0, 100, 1e-5), (-64, None, 0.0), (-70, None, 0.0),
          (-126, None, 0.0), (-132, None, 0.0), (-70, None, 1e-44), (-120, None, 1e-33), (-30, None, 1e-20), (-63, None, 1e-12),
@@ -285,3 +299,20 @@ def test_verified_drafts_and_decoding_within_their_bounds():
             tol = u * (got.abs() + want.abs()) / (1 - u) + 2 * (1 + u) * (u + 2 * ds + 2.0 ** -20) * mag
             assert ((got - want).abs() <= tol).all()
         start += n
+
+
+# ---------------------------------------------------------------------------
+# shapes
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("C,H,D,G,v", [(2, 3, 8, 1, 0), (2, 2, 24, 5, 0), (2, 6, 72, 2, 0), (2, 1, 136, 3, 0), (2, 4, 200, 1, 0), (2, 1, 248, 9, 0),
+                                       (2, 2, 264, 2, 0), (2, 1, 512, 1, 0), (1, 1, 520, 40, 8), (1, 3, 264, 2, 256), (1, 1, 136, 1, 136),
+                                       (2, 1, 16, 200, 0)])
+def test_head_sizes(C, H, D, G, v, kind):
+    """Multiples of 8 that no kernel is made for, few and many query heads of a cache head."""
+    spec = PoolSpec(1, C, H, D, T=16, N=60, e=2, layout="LPCTHD" if G % 2 else "PLCHTD")
+    recs = [(0, 70, 40, 0), (0, 1, 1, 0), (3, 129, 5, 0), (0, 33, 33, 20), (5, 5, 1, 0), (40, 64, 30, 0)]
+    base.queries_case(D, spec, kind, kind, recs, G, v or None, spoil=True, gap=1, cap=9.0 if D % 3 else 0.0, slopes=D % 16 == 8)
+    base.queries_case(D, spec, kind, kind, [(0, 150, 1, 0), (7, 64, 1, 0)], G, v or None, spoil=True, strided=True)
+    base.queries_case(D, spec, kind, kind, [(0, 150, 12, 0), (9, 64, 30, 0)], G, v or None, spoil=True, tree=True)
