@@ -11,10 +11,14 @@
 // norms' weights lie there too.
 //
 // Four prompts of 1024 to 8192 tokens into an e4m3 cache (28 query heads of 128 on 4, all
-// normed, positions on three axes, 260 MB) take 67 us, 3.9 TB/s, as much as kvx_append takes
-// without norms: the division by the cache's scale and the loads' latency, which the
-// wavefronts hide, bound it, not the norm.  With the next row's loads asked for ahead fewer
-// wavefronts fit and it is slower.  64 drafted tokens take 10 us, 12.6 MB.
+// normed, positions on three axes, 260 MB) take 67 to 70 us, 3.9 TB/s, as much as kvx_append takes
+// without norms, and 68 into a bfloat16 one (276 MB): about 42 us of them the vector instructions alone
+// would take (915 a wavefront; a wavefront with a row of an e4m3 cache divides by its scale for all its
+// rows), and 63% of a wavefront's time passes in waits.  The cosines' reads from LDS, 64 bytes apart from lane
+// to lane, conflict in 59% of its cycles, which are few.  With the next row's loads asked for ahead fewer
+// wavefronts fit and it is slower.  MLA's rows (16 heads of 576, 586 MB) take 224 us, 2.6 TB/s.  512
+// drafted tokens take 12 to 13 us, 12.6 MB: 192 workgroups, each of which reads record, page ids and
+// then five rows a group of lanes in turn.
 
 #include "kvx_append.h"
 

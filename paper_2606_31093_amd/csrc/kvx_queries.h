@@ -12,9 +12,10 @@
 // that the next tile is on its way while this one is used.
 //
 // Bounds.  With many rows a tile's products take as long as its reads from LDS, each
-// wavefront reading all of it for its 32 rows: 1.06 PFLOP/s for a prompt of 8192, 32 heads
-// of 128 on 8 (2070 us; a large library product reaches 1.2 on this device), 0.9 for heads
-// of 256, 0.58 for MLA's rows of 576 behind 32768 positions.  Prompts of up to 2000 reach 0.6:
+// wavefront reading all of it for its 32 rows: 1.06 PFLOP/s for a prompt of 16384, 32 heads
+// of 128 on 8 (2070 us; a large library product reaches 1.2 on this device), 1.02 for one of 8192,
+// 0.74 with heads of 64 and 0.87 of 256; 80 and 192 elements take the time of 128 and 256; MLA's rows
+// of 576 0.65 (16 heads, a prompt of 4096) to 0.79 (128).  Prompts of up to 2000 reach 0.6:
 // a unit's first tile and its outputs take as long as three of its steps.  With few rows
 // the cache's bytes bound it: 5 TB/s for a batch of single tokens.  A third and fourth tile
 // on its way, or its lines asked for in the cache two tiles ahead, bring nothing (2150 and
@@ -253,12 +254,12 @@ struct Queries {
     // second product would take half as long again, and a weight's rounding is one of many that average.
     static constexpr bool PARTS = TEAM == 1;
     // Reads of LDS are kept so many products ahead (left alone the compiler waits for each one
-    // where registers are few, or reads more than there are registers for).  A prompt of 8192 takes
+    // where registers are few, or reads more than there are registers for).  A prompt of 16384 takes
     // 2260, 2238 and 2236 us with 2, 4 and 6; rows of 576, whose registers are few, 190, 199 and 207
     // with 2, 3 and 4.
     static constexpr int AHEAD = SPLIT > 1 ? 2 : 4;
     // Tiles are taken from the last to the first where scores may have a bias: it is highest at the end
-    // as a rule, and from the first on sums would be rescaled at nearly every tile.  A prompt of 8192, 32
+    // as a rule, and from the first on sums would be rescaled at nearly every tile.  A prompt of 16384, 32
     // heads of 128, takes 2290 us so and 2450 to 2520 forwards; 16 prompts of up to 2000, e4m3, 441 and
     // 452.  Without a bias it is the same (2098 and 2086).
     static constexpr bool BACK = GENERAL;

@@ -140,13 +140,14 @@ constexpr int kWholeSteps = 8;
 constexpr int kWholeMore = 8192;
 // One record's kernel looks how many units there are, and takes one or the other: at most so many
 // workgroups, which go on to a further unit.  One query behind 131072 positions takes 138 us under limits
-// of 16384 (2450 with a workgroup a unit), a chunk of 512 behind 100000 800 (2540).
+// of 16384 (2450 with a workgroup a unit), a chunk of 512 behind 100000 800 (2540); a prompt of 16384
+// 2057, and 2042 without the look and the second launch, in which nothing is left to do (5 us).
 constexpr int kOneBlocks = 2048;
 static_assert(kOneBlocks >= 512, "as many as shares");
 // Records of up to this many positions: four wavefronts a workgroup, two of which begin and
 // end at different times, so that one computes while the other waits for its first tile.  16
 // prompts of 512 take 94 us, 102 in eights; one of 300 16.2 and 18.6.  Longer ones share a tile
-// among eight: uniform ones of 2000 642 us and 672 in fours, one of 8192 2163 and 2273.
+// among eight: uniform ones of 2000 642 us and 672 in fours, one of 16384 2163 and 2273.
 constexpr int kShort = 1024;
 // Fewer steps than this are not worth a share: its way to the first tile takes as long.
 constexpr int kLeastShare = 4;
